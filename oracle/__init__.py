@@ -273,3 +273,6 @@ def epilogue_reference(kind: int, Y, B, R=None):
 # The non-matmul steps of a backbone / action-expert layer (RMSNorm, rotary embedding,
 # attention): oracle/layer.py.
 from .layer import attention_reference, rmsnorm_reference, rope_reference  # noqa: E402,F401
+
+# The paged key/value cache (slots, norm with rotation and cache write, attention): oracle/paged.py.
+from .paged import paged_attention_reference, paged_slots_reference, qk_norm_rope_reference  # noqa: E402,F401

@@ -1,4 +1,5 @@
-"""Python binding of libembqmm.so (the C ABI declared in include/emb_qmm.h).
+"""Python binding of libembqmm.so (the C ABI declared in include/emb_qmm.h) and of
+libembpaged.so (include/emb_paged.h: the paged key/value cache).
 
 Argument marshalling only: every step of the computation runs in the library's
 CUDA kernels. Functions keep the C names and take either torch tensors (their
@@ -20,6 +21,8 @@ from typing import Iterable, Optional, Sequence
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libembqmm.so")
 HEADER_PATH = os.path.join(_HERE, "..", "include", "emb_qmm.h")
+PAGED_LIB_PATH = os.path.join(_HERE, "libembpaged.so")
+PAGED_HEADER_PATH = os.path.join(_HERE, "..", "include", "emb_paged.h")
 
 EMB_Q8_0 = 0
 EMB_Q4_0 = 1
@@ -33,6 +36,7 @@ EMB_ECUDA = 4
 EMB_ETIMEOUT = 5
 EMB_EUNSUPPORTED = 6
 EMB_MAX_LAYERS = 4096
+EMB_PAGED_WORKSPACE = 64 << 20   # bytes of emb_paged_attention's workspace
 EMB_PRECISE_OPERAND = 0x100   # flag OR-ed into a layer's epilogue (two-operand tensor-core weights)
 
 # layer epilogues (emb_epilogue)
@@ -122,6 +126,31 @@ def lib():
     L.emb_attention.argtypes = [vp, vp, vp, i64, vp, vp, i64, vp, i64, i64, i64, i64, f32, vp]
     L.emb_attention.restype = i32
     _lib = L
+    return L
+
+
+_paged = None
+
+
+def paged_lib():
+    """The loaded paged-cache library; raises if it has not been built."""
+    global _paged
+    if _paged is not None:
+        return _paged
+    if not os.path.exists(PAGED_LIB_PATH):
+        raise RuntimeError(f"{PAGED_LIB_PATH} is missing: run paper_2607_02501_gb300.build() "
+                           "(nvcc, sm_103a) first; there is no non-CUDA implementation")
+    L = ctypes.CDLL(PAGED_LIB_PATH)
+    i64, vp, f32 = ctypes.c_int64, ctypes.c_void_p, ctypes.c_float
+    L.emb_paged_slots.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp]
+    L.emb_qk_norm_rope.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i64, i64, vp, vp, f32, vp, i64, i64,
+                                   ctypes.c_char_p, i64, f32, vp, vp, vp, vp, i64, i64, vp]
+    L.emb_paged_attention.argtypes = [vp, vp, vp, i64, i64, vp, i64, vp, vp, vp, i64, i64, i64, vp, i64, i64,
+                                      i64, f32, f32, i64, vp, ctypes.c_size_t, vp]
+    L.emb_paged_status.argtypes = [vp]
+    for name in ("emb_paged_slots", "emb_qk_norm_rope", "emb_paged_attention", "emb_paged_status"):
+        getattr(L, name).restype = ctypes.c_int
+    _paged = L
     return L
 
 
@@ -354,6 +383,64 @@ def emb_attention(Q, K0, V0, K1, V1, O, n_heads: int, n_kv_heads: int, head_dim:
     _check(lib().emb_attention(_ptr(Q), _ptr(K0), _ptr(V0), n0, _ptr(K1), _ptr(V1), n1, _ptr(O),
                                Q.shape[0], n_heads, n_kv_heads, head_dim, scale, _stream(stream)),
            "emb_attention")
+
+
+def emb_paged_slots(cached, added, free_pages, used, table, q_start, kv_len, slots, positions, used_out,
+                    page_size: int, stream=None) -> None:
+    """cached, added: int32 [R]; free_pages: int32 [n_free]; used, used_out: int32 [1]; table: int32
+    [R][max_pages], filled on; out: q_start int32 [R + 1], kv_len int32 [R], slots int64 [T], positions
+    int32 [T]."""
+    R, max_pages = table.shape
+    _check(paged_lib().emb_paged_slots(
+        cached.data_ptr(), added.data_ptr(), R, free_pages.data_ptr(), free_pages.shape[0], used.data_ptr(), page_size,
+        table.data_ptr(), max_pages, q_start.data_ptr(), kv_len.data_ptr(), slots.data_ptr(), positions.data_ptr(),
+        slots.shape[0], used_out.data_ptr(), _stream(stream)), "emb_paged_slots")
+
+
+def emb_qk_norm_rope(q, k, v, q_out, k_cache, v_cache, slots, positions, q_gamma=None, k_gamma=None,
+                     eps: float = 1e-6, axis_of_pair=None, rot_dim: Optional[int] = None,
+                     base: float = 10000.0, stream=None) -> None:
+    """q: bf16 [T][H * d], k, v: bf16 [T][Hk * d] (rows may be strided); q_out: bf16 [T][H * d]; caches:
+    bf16 [n_pages][page_size][Hk][d]; slots: int64 [T]; positions: int32 [T] or [n_axes][T]; gammas: fp32
+    [d]; axis_of_pair: bytes or integers [rot_dim / 2]; rot_dim: d by default."""
+    n_pages, page_size, Hk, d = k_cache.shape
+    T, width = q.shape
+    axes, pos_stride = (1, T) if positions.dim() == 1 else (positions.shape[0], positions.stride(0))
+    rot = d if rot_dim is None else rot_dim
+    if axis_of_pair is not None:
+        axis_of_pair = bytes(axis_of_pair)
+        if len(axis_of_pair) != rot // 2:
+            raise EmbError(EMB_EINVAL, "emb_qk_norm_rope: axis_of_pair")
+    _check(paged_lib().emb_qk_norm_rope(
+        q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0), T, width // d, Hk, d,
+        _ptr(q_gamma), _ptr(k_gamma), eps, positions.data_ptr(), pos_stride, axes, axis_of_pair, rot, base, slots.data_ptr(),
+        q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), n_pages, page_size, _stream(stream)),
+        "emb_qk_norm_rope")
+
+
+def emb_paged_attention(Q, k_cache, v_cache, table, q_start, kv_len, O, scale: float, max_q: int,
+                        workspace, prefix=None, cap: float = 0.0, window: int = 0, stream=None) -> None:
+    """Q, O: bf16 [T][H * d]; caches: bf16 [n_pages][page_size][Hk][d]; table: int32 [R][max_pages]; q_start:
+    int32 [R + 1]; kv_len, prefix: int32 [R]; workspace: paged_workspace()."""
+    n_pages, page_size, Hk, d = k_cache.shape
+    R, max_pages = table.shape
+    T, width = Q.shape
+    _check(paged_lib().emb_paged_attention(
+        Q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), n_pages, page_size, table.data_ptr(), max_pages,
+        q_start.data_ptr(), kv_len.data_ptr(), _ptr(prefix), R, T, max_q, O.data_ptr(), width // d, Hk, d, scale, cap,
+        window, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)),
+        "emb_paged_attention")
+
+
+def paged_workspace(device=None):
+    """A zero-filled workspace for emb_paged_attention on the current (or given) CUDA device."""
+    import torch
+    return torch.zeros(EMB_PAGED_WORKSPACE, dtype=torch.uint8, device=device if device is not None else "cuda")
+
+
+def emb_paged_status(stream=None) -> int:
+    """Synchronise the stream; return (and clear) the paged-cache library's status code."""
+    return int(paged_lib().emb_paged_status(_stream(stream)))
 
 
 def emb_dequantize_f32(fmt: int, W_blocks, N: int, K: int, out, stream=None) -> None:

@@ -1,7 +1,8 @@
-"""Build libembqmm.so in-tree with nvcc for sm_103a (no cmake, no torch extension).
+"""Build libembqmm.so and libembpaged.so in-tree with nvcc for sm_103a (no cmake, no torch
+extension).
 
-Each .cu is compiled in parallel, then linked into one shared library with the CUDA
-runtime linked statically, so the library needs only the driver at run time.
+Each .cu is compiled in parallel, then linked into its shared library with the CUDA
+runtime linked statically, so the libraries need only the driver at run time.
 """
 from __future__ import annotations
 
@@ -16,6 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libembqmm.so")
 SOURCES = ["api.cu", "quant.cu", "gemv.cu", "gemm_tc.cu", "layer_ops.cu"]
+PAGED_LIB = os.path.join(HERE, "libembpaged.so")
+PAGED_SOURCES = ["paged_api.cu", "paged_cache.cu", "paged_attention.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -36,11 +39,11 @@ def _flags(verbose_ptxas: bool):
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(PAGED_LIB):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(PAGED_LIB))
     deps = [os.path.join(CSRC, n) for n in os.listdir(CSRC)]
-    deps.append(os.path.join(HERE, "..", "include", "emb_qmm.h"))
+    deps += [os.path.join(HERE, "..", "include", n) for n in ("emb_qmm.h", "emb_paged.h")]
     deps.append(os.path.abspath(__file__))
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -58,8 +61,9 @@ def build(force: bool = False, verbose_ptxas: bool = False) -> str:
         r = subprocess.run(cmd, capture_output=True, text=True)
         return src, obj, r
 
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
-        results = list(ex.map(compile_one, SOURCES))
+    sources = SOURCES + PAGED_SOURCES
+    with cf.ThreadPoolExecutor(max_workers=len(sources)) as ex:
+        results = list(ex.map(compile_one, sources))
     failed = False
     for src, _, r in results:
         if r.stdout or r.stderr:
@@ -67,12 +71,14 @@ def build(force: bool = False, verbose_ptxas: bool = False) -> str:
         failed |= r.returncode != 0
     if failed:
         raise RuntimeError("nvcc failed (see messages above)")
-    tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [nvcc, *ARCH, "-shared", "-o", tmp] + [obj for _, obj, _ in results]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"link failed:\n{r.stdout}{r.stderr}")
-    os.replace(tmp, LIB)
+    objects = {src: obj for src, obj, _ in results}
+    for lib, parts in ((LIB, SOURCES), (PAGED_LIB, PAGED_SOURCES)):
+        tmp = lib + f".tmp{os.getpid()}"
+        cmd = [nvcc, *ARCH, "-shared", "-o", tmp] + [objects[src] for src in parts]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"link failed:\n{r.stdout}{r.stderr}")
+        os.replace(tmp, lib)
     return LIB
 
 

@@ -1,0 +1,76 @@
+// Declarations shared by the translation units of libembpaged.so (not installed).
+#pragma once
+
+#include "../../include/emb_paged.h"
+#include "ptx.cuh"
+
+namespace emb {
+
+struct SlotArgs {
+    const int32_t* cached;
+    const int32_t* added;
+    const int32_t* free_pages;
+    const int32_t* used;
+    int32_t* table;
+    int32_t* q_start;
+    int32_t* kv_len;
+    int64_t* slots;
+    int32_t* positions;
+    int32_t* used_out;
+    int64_t n_free, max_pages, n_tokens;
+    int n_req, page_size;
+};
+cudaError_t launch_paged_slots(const SlotArgs& a, cudaStream_t s);
+
+struct QkArgs {
+    const uint16_t* q;
+    const uint16_t* k;
+    const uint16_t* v;
+    const float* q_gamma;
+    const float* k_gamma;
+    const int32_t* positions;
+    const uint8_t* axis_of_pair;  // host, or NULL
+    const int64_t* slots;
+    uint16_t* q_out;
+    uint16_t* k_cache;
+    uint16_t* v_cache;
+    int64_t q_stride, k_stride, v_stride, pos_stride, n_tokens, n_heads, n_kv_heads, head_dim, rot_dim, n_slots;
+    float eps, base;
+};
+cudaError_t launch_qk_norm_rope(const QkArgs& a, cudaStream_t s);
+
+struct PagedAttnArgs {
+    const uint16_t* Q;
+    const uint16_t* k_cache;
+    const uint16_t* v_cache;
+    const int32_t* table;
+    const int32_t* q_start;
+    const int32_t* kv_len;
+    const int32_t* prefix;
+    uint16_t* O;
+    void* workspace;
+    int* status;
+    int64_t n_pages, page_size, max_pages, n_req, n_tokens, max_q, n_heads, n_kv_heads, head_dim, window;
+    float scale, cap;
+};
+// Key tiles of a call, at most (an upper bound from the host's sizes).
+double paged_attention_tiles(const PagedAttnArgs& a);
+cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s);
+
+// A launch with programmatic stream serialisation.
+inline cudaError_t launch_serialised(const void* fn, unsigned grid, unsigned block, size_t smem, cudaStream_t s,
+                                     void** args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelExC(&cfg, fn, args);
+}
+
+}  // namespace emb

@@ -1,0 +1,684 @@
+// Attention of new tokens over a paged key/value cache (definition in include/emb_paged.h). Both kernels take
+// their work from paged_sched.cuh: few query rows per request on mma.sync, many on tcgen05.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <mutex>
+
+#include <cuda.h>
+
+#include "paged_sched.cuh"
+
+namespace emb {
+namespace {
+
+__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+        "{%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 2^x (results below the normal range become zero; -inf gives 0).
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp_fast(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// cap log2(e) tanh(y / 2), y = 2 scale q.k / cap with its base 2: tanh as 1 - 2 / (1 + e^y), within 2^-22 of 1
+__device__ __forceinline__ float capped(float y, float cap2) { return fmaf(-2.0f * cap2, rcp_fast(1.0f + exp2_fast(y)), cap2); }
+
+__device__ __forceinline__ void ldsm_x4(uint32_t saddr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(saddr));
+}
+__device__ __forceinline__ void ldsm_x4_trans(uint32_t saddr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(saddr));
+}
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float2 unpack_bf16x2(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+__device__ __forceinline__ bool not_finite(uint32_t bf16_bits) { return (bf16_bits & 0x7F80u) == 0x7F80u; }
+
+// Rows of O behind the last request's (padding of a recorded step): zeros.
+__device__ __forceinline__ void zero_padding(const PagedParams& p, int D, int tid, int nt) {
+    const int64_t used = min(max(int64_t(p.q_start[p.n_req]), int64_t(0)), p.n_tokens);
+    const int64_t row16 = int64_t(p.H) * D / 8;
+    uint4* o = reinterpret_cast<uint4*>(p.O);
+    for (int64_t i = used * row16 + int64_t(blockIdx.x) * nt + tid; i < p.n_tokens * row16; i += int64_t(gridDim.x) * nt)
+        o[i] = make_uint4(0, 0, 0, 0);
+}
+
+// Adds the partial results of an item that several CTAs shared and stores this CTA's part of its outputs.
+// A partial result is ROWS maxima, ROWS sums and [ROWS][D] values, in CTA order (deterministic).
+template <int D, int ROWS>
+__device__ __forceinline__ void join_store(const PagedParams& p, const PagedJoin& J, const PagedReq& q, int me, int tid, int nt) {
+    constexpr int64_t kSlot = int64_t(ROWS) * (D + 2);
+    const int i0 = J.b * p.QB, rows = min(p.QB, q.n - i0) * p.G;
+    for (int e = me * nt + tid; e < rows * (D / 4); e += J.count * nt) {
+        const int row = e / (D / 4), c = (e - row * (D / 4)) * 4;
+        float M = -INFINITY;
+#pragma unroll 8
+        for (int i = 0; i < J.count; ++i) M = fmaxf(M, __ldcg(p.part + part_slot(J.first + i, J.first) * kSlot + row));
+        const float m0 = M == -INFINITY ? 0.0f : M;
+        float L = 0.0f;
+        float4 o = make_float4(0, 0, 0, 0);
+#pragma unroll 8
+        for (int i = 0; i < J.count; ++i) {
+            const float* s = p.part + part_slot(J.first + i, J.first) * kSlot;
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(s + 2 * ROWS + row * D + c));
+            // weight 0 of a partial without a finite score: its sums are 0, or NaN, which has to show
+            const float w = exp2_fast(__ldcg(s + row) - m0);
+            L = fmaf(__ldcg(s + ROWS + row), w, L);
+            o.x = fmaf(v.x, w, o.x);
+            o.y = fmaf(v.y, w, o.y);
+            o.z = fmaf(v.z, w, o.z);
+            o.w = fmaf(v.w, w, o.w);
+        }
+        const float inv = L == 0.0f ? 0.0f : __fdiv_rn(1.0f, L);
+        uint2 u;
+        u.x = pack_bf16x2(__fmul_rn(o.x, inv), __fmul_rn(o.y, inv));
+        u.y = pack_bf16x2(__fmul_rn(o.z, inv), __fmul_rn(o.w, inv));
+        const int64_t t = q.q0 + i0 + row / p.G;
+        *reinterpret_cast<uint2*>(p.O + (t * p.H + J.g * p.G + row % p.G) * D + c) = u;
+    }
+}
+
+// ------------------------------------------------------------------ few rows: mma.sync
+// A producer warp brings tiles of 64 keys and values by TMA (a box per page, 128-byte swizzled rows) into a ring;
+// four warps compute. WK = 4: an item has 16 rows (queries times heads), every warp takes 16 of a tile's keys, and the
+// warps' results are merged at the item's end. WK = 1: an item has 64 rows, 16 per warp, and every warp takes all
+// keys. Scores, softmax in base 2 with a running maximum and the value product (weights as bf16 hi + lo) stay in
+// registers. HBM bounds it: the cache is read once for 16 or 64 rows.
+constexpr int kFewWarps = 4;
+constexpr int kFewThreads = 32 * (kFewWarps + 1);
+constexpr int kFewTile = 64;
+template <int WK>
+constexpr int kFewRows = 16 * kFewWarps / WK;
+
+template <int D>
+struct FewTraits {
+    static constexpr int kStage = kFewTile * D * 4;  // bytes of keys and values
+    static constexpr int kStages = D == 64 ? 6 : 3;
+    static constexpr int kCtas = D == 256 ? 1 : 2;   // per SM
+    static constexpr int kQPitch = D + 8;            // queries in shared memory (D = 256), bf16 per padded row
+    static constexpr int kQBytes = D == 256 ? 64 * kQPitch * 2 : 0;
+    static constexpr int kSmem = 1024 + kStages * kStage + kQBytes;
+};
+
+template <int D, int WK, bool CAP>
+__global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_kernel(const __grid_constant__ PagedParams p) {
+    using T = FewTraits<D>;
+    constexpr int KS = D / 16, NT = D / 8, NJ = kFewTile / 8 / WK, ROWS = kFewRows<WK>;
+    constexpr bool QS = D == 256;  // queries stay in shared memory: their fragments would not fit the registers
+    constexpr int kSub = kFewTile * 128;  // bytes of a 64-dim part of a tile
+    constexpr int64_t kSlot = int64_t(ROWS) * (D + 2);
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full[T::kStages], empty[T::kStages];
+    __shared__ int abort_flag;
+    __shared__ float warp_m[kFewWarps][16], warp_l[kFewWarps][16];
+    uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < T::kStages; ++i) {
+            ptx::mbar_init(&full[i], 1);
+            ptx::mbar_init(&empty[i], kFewWarps);
+        }
+        abort_flag = 0;
+        ptx::fence_mbar_init();
+        ptx::prefetch_tmap(&p.k_map);
+        ptx::prefetch_tmap(&p.v_map);
+    }
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();  // lengths, queries and the new tokens' keys and values come from earlier launches
+    const PagedStretch st = paged_stretch<kFewTile, kFewThreads>(p);  // (its barriers also publish the mbarriers)
+
+    int r = st.r, g = st.g, b = st.b;
+    uint32_t x = st.x0, off = st.off;
+    uint32_t issued = 0;  // tiles so far (ring position and phase)
+    if (warp == kFewWarps) {
+        // -------------------------------------------------------------------- producer
+        ptx::fence_proxy_async_global();  // (the cache was written by ordinary stores)
+        const int page_size = 1 << p.page_shift, box = min(page_size, kFewTile), n_box = kFewTile / box;
+        while (x < st.x1) {
+            const PagedItem it = paged_item<kFewTile>(p, r, g, b);
+            const uint32_t take = min(st.x1 - x, uint32_t(it.units) - off);
+            const int j1 = min(int(off + take), it.nt);
+            const int32_t* row = p.table + int64_t(r) * p.max_pages;
+            // lane i looks up the page of the tile's box i; boxes that no query sees, and pages that do not
+            // exist, are fetched from behind the cache: zeros
+            auto page_of = [&](int j) {
+                const int key = (it.t0 + j) * kFewTile + lane * box;
+                int page = p.n_pages;
+                if (lane < n_box && j < j1 && key < it.hi && key + box > it.lo) {
+                    page = row[key >> p.page_shift];
+                    if (page < 0 || page > p.n_pages) page = p.n_pages;
+                }
+                return page;
+            };
+            int page = page_of(int(off));
+            for (int j = int(off); j < j1; ++j, ++issued) {
+                const int next = page_of(j + 1);
+                const int s = issued % T::kStages;
+                if (issued >= uint32_t(T::kStages))
+                    ptx::mbar_wait(&empty[s], (issued / T::kStages - 1) & 1, &abort_flag, p.status, kWaitLimitNs);
+                const bool stop = __any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&abort_flag) != 0);
+                uint8_t* k = ring + s * T::kStage;
+                uint8_t* v = k + T::kStage / 2;
+                if (!stop) {
+                    if (ptx::elect_one()) ptx::mbar_arrive_expect_tx(&full[s], T::kStage);
+                    __syncwarp();
+                    const int place = ((it.t0 + j) * kFewTile) & (page_size - 1);
+                    for (int i = 0; i < n_box; ++i) {
+                        const int pg = __shfl_sync(0xffffffffu, page, i);
+                        if (ptx::elect_one()) {
+#pragma unroll
+                            for (int c = 0; c < D / 64; ++c) {
+                                ptx::tma_load_4d(k + c * kSub + i * box * 128, &p.k_map, &full[s], c * 64, g, place, pg);
+                                ptx::tma_load_4d(v + c * kSub + i * box * 128, &p.v_map, &full[s], c * 64, g, place, pg);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                }
+                page = next;
+            }
+            x += take;
+            off = 0;
+            if (x < st.x1) next_item(p, r, g, b, it.q.n);
+        }
+        // every copy must land before this CTA's shared memory is released
+        if (!abort_flag)
+            for (uint32_t i = issued > uint32_t(T::kStages) ? issued - T::kStages : 0; i < issued; ++i)
+                ptx::mbar_wait(&full[i % T::kStages], (i / T::kStages) & 1, &abort_flag, p.status, kWaitLimitNs);
+        return;
+    }
+
+    // ------------------------------------------------------------------------ compute
+    // A wait that gave up sets abort_flag; later waits then return at once, and the loops run to their end (the
+    // outputs are undefined then), so that every barrier still meets all its threads.
+    zero_padding(p, D, threadIdx.x, 32 * kFewWarps);
+    auto bar = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };
+    const int quad = lane >> 2, qc = lane & 3;
+    const int wrow = WK == 1 ? warp * 16 : 0, wkey = WK == 1 ? 0 : warp * 16;
+    const uint32_t ring_u = ptx::smem_u32(ring);
+    __nv_bfloat16* sq = reinterpret_cast<__nv_bfloat16*>(ring + T::kStages * T::kStage) + (QS ? wrow * T::kQPitch : 0);
+    PagedJoin join[2];
+    int joins = 0;
+
+    while (x < st.x1) {
+        const PagedItem it = paged_item<kFewTile>(p, r, g, b);
+        const uint32_t take = min(st.x1 - x, uint32_t(it.units) - off);
+        const int j0 = int(off), j1 = min(int(off + take), it.nt);
+        // this thread's two rows: query and head, keys they see
+        const int rA = wrow + quad, rB = rA + 8, iA = rA / p.G, iB = rB / p.G;
+        const bool okA = iA < it.nq, okB = iB < it.nq;
+        const KeyRange none{0, 0};
+        const KeyRange kA = okA ? query_keys(p, it.q, it.i0 + iA) : none, kB = okB ? query_keys(p, it.q, it.i0 + iB) : none;
+        auto row_of = [&](int i, int rr) { return (int64_t(it.q.q0 + it.i0 + i) * p.H + g * p.G + (rr - i * p.G)) * D; };
+        const int64_t offA = okA ? row_of(iA, rA) : 0, offB = okB ? row_of(iB, rB) : 0;
+
+        uint32_t qf[QS ? 1 : KS][4];
+        if constexpr (!QS) {
+            auto ldq = [&](bool ok, int64_t at) { return ok ? *reinterpret_cast<const uint32_t*>(p.Q + at) : 0u; };
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const int c = ks * 16 + 2 * qc;
+                qf[ks][0] = ldq(okA, offA + c);
+                qf[ks][1] = ldq(okB, offB + c);
+                qf[ks][2] = ldq(okA, offA + c + 8);
+                qf[ks][3] = ldq(okB, offB + c + 8);
+            }
+        } else {
+            // WK = 4: the warps bring four rows each of the 16 they share
+            if constexpr (WK == 4) bar();  // (the last item's rows are done with)
+            else __syncwarp();
+            constexpr int kMine = WK == 4 ? 4 : 16;
+            const int first = WK == 4 ? warp * 4 : 0;
+            for (int e = lane; e < kMine * (D / 8); e += 32) {
+                const int rr = first + e / (D / 8), c = (e % (D / 8)) * 8, i = (wrow + rr) / p.G;
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (i < it.nq) v = *reinterpret_cast<const uint4*>(p.Q + row_of(i, wrow + rr) + c);
+                *reinterpret_cast<uint4*>(sq + rr * T::kQPitch + c) = v;
+            }
+            if constexpr (WK == 4) bar();
+            else __syncwarp();
+        }
+
+        float o[NT][4];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.0f;
+        float mA = -INFINITY, mB = -INFINITY, lA = 0.0f, lB = 0.0f;
+        bool odd = false;  // a value that is not finite was left out of a product
+
+        for (int j = j0; j < j1; ++j, ++issued) {
+            const int s = issued % T::kStages;
+            ptx::mbar_wait(&full[s], (issued / T::kStages) & 1, &abort_flag, p.status, kWaitLimitNs);
+            __syncwarp();
+            const uint32_t kb = ring_u + uint32_t(s * T::kStage), vb = kb + T::kStage / 2;
+            const int key0 = (it.t0 + j) * kFewTile;
+            const bool edge = key0 < it.lo_all || key0 + kFewTile > it.hi_all;
+
+            // S = Q K^T, the warp's keys in n-tiles of 8; one ldmatrix gives the fragments of two k-steps
+            float sc[NJ][4];
+#pragma unroll
+            for (int n = 0; n < NJ; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.0f;
+            const uint32_t krow = kb + uint32_t(wkey + (lane & 7)) * 128;
+#pragma unroll
+            for (int ks = 0; ks < KS; ks += 2) {
+                uint32_t a0[4], a1[4];
+                if constexpr (QS) {
+                    const uint32_t qa = ptx::smem_u32(sq + (lane & 15) * T::kQPitch + ks * 16 + (lane >> 4) * 8);
+                    ldsm_x4(qa, a0);
+                    ldsm_x4(qa + 32, a1);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        a0[i] = qf[ks][i];
+                        a1[i] = qf[ks + 1][i];
+                    }
+                }
+                uint32_t bk[NJ][4];
+                const uint32_t at = krow + (ks / 4) * kSub + (((((ks & 3) * 2) + (lane >> 3)) ^ (lane & 7)) << 4);
+#pragma unroll
+                for (int n = 0; n < NJ; ++n) ldsm_x4(at + n * 1024, bk[n]);
+#pragma unroll
+                for (int n = 0; n < NJ; ++n) mma_16816(sc[n], a0, bk[n][0], bk[n][1]);
+#pragma unroll
+                for (int n = 0; n < NJ; ++n) mma_16816(sc[n], a1, bk[n][2], bk[n][3]);
+            }
+#pragma unroll
+            for (int n = 0; n < NJ; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sc[n][e] = __fmul_rn(sc[n][e], p.scale2);
+                    if constexpr (CAP) sc[n][e] = capped(sc[n][e], p.cap2);
+                }
+            if (edge) {
+#pragma unroll
+                for (int n = 0; n < NJ; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int key = key0 + wkey + n * 8 + 2 * qc + e;
+                        if (key < kA.lo || key >= kA.hi) sc[n][e] = -INFINITY;
+                        if (key < kB.lo || key >= kB.hi) sc[n][2 + e] = -INFINITY;
+                    }
+            }
+            float tA = -INFINITY, tB = -INFINITY;
+#pragma unroll
+            for (int n = 0; n < NJ; ++n) {
+                tA = fmaxf(tA, fmaxf(sc[n][0], sc[n][1]));
+                tB = fmaxf(tB, fmaxf(sc[n][2], sc[n][3]));
+            }
+#pragma unroll
+            for (int i = 1; i <= 2; i <<= 1) {
+                tA = fmaxf(tA, __shfl_xor_sync(0xffffffffu, tA, i));
+                tB = fmaxf(tB, __shfl_xor_sync(0xffffffffu, tB, i));
+            }
+            const float nA = fmaxf(mA, tA), nB = fmaxf(mB, tB);
+            // (a row without a finite score so far subtracts 0: its weights are 2^-inf = 0)
+            const float sA0 = nA == -INFINITY ? 0.0f : nA, sB0 = nB == -INFINITY ? 0.0f : nB;
+            const float cA = exp2_fast(mA - sA0), cB = exp2_fast(mB - sB0);
+            float sA = 0.0f, sB = 0.0f;
+#pragma unroll
+            for (int n = 0; n < NJ; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    sc[n][e] = exp2_fast(sc[n][e] - sA0);
+                    sc[n][2 + e] = exp2_fast(sc[n][2 + e] - sB0);
+                    sA += sc[n][e];
+                    sB += sc[n][2 + e];
+                }
+            lA = lA * cA + sA;  // lane-partial sums; the four lanes of a row are added at the end
+            lB = lB * cB + sB;
+            if (__any_sync(0xffffffffu, nA != mA || nB != mB)) {  // else every factor is 1
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    o[n][0] *= cA;
+                    o[n][1] *= cA;
+                    o[n][2] *= cB;
+                    o[n][3] *= cB;
+                }
+            }
+            mA = nA;
+            mB = nB;
+            // O += P V in k-steps of 16 keys, P as hi + lo
+#pragma unroll
+            for (int kk = 0; kk < NJ / 2; ++kk) {
+                uint32_t ah[4], al[4];
+                const float* s0 = sc[2 * kk];
+                const float* s1 = sc[2 * kk + 1];
+                const float src[4][2] = {{s0[0], s0[1]}, {s0[2], s0[3]}, {s1[0], s1[1]}, {s1[2], s1[3]}};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    ah[i] = pack_bf16x2(src[i][0], src[i][1]);
+                    const float2 h = unpack_bf16x2(ah[i]);
+                    al[i] = pack_bf16x2(__fsub_rn(src[i][0], h.x), __fsub_rn(src[i][1], h.y));
+                }
+                const int kl = wkey + kk * 16 + (lane & 7) + ((lane >> 3) & 1) * 8;
+                const uint32_t vrow = vb + uint32_t(kl) * 128;
+#pragma unroll
+                for (int jj = 0; jj < NT; jj += 4) {
+                    uint32_t bv[2][4];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        ldsm_x4_trans(vrow + (jj / 8) * kSub + ((((jj & 7) + 2 * i + (lane >> 4)) ^ (lane & 7)) << 4), bv[i]);
+                    if (edge) {
+                        // values behind the request's last key are anything; those hidden from some rows may not be
+                        // multiplied by their weights of 0 if they are not finite: such values are left
+                        // out here and added at the end for the rows that see them
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int key = key0 + wkey + kk * 16 + (e & 1) * 8 + 2 * qc;
+                                uint32_t w = bv[i][e];
+                                if (key >= it.q.L) w &= 0xFFFF0000u;
+                                if (key + 1 >= it.q.L) w &= 0x0000FFFFu;
+                                if (not_finite(w)) {
+                                    w &= 0xFFFF0000u;
+                                    odd = true;
+                                }
+                                if (not_finite(w >> 16)) {
+                                    w &= 0x0000FFFFu;
+                                    odd = true;
+                                }
+                                bv[i][e] = w;
+                            }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mma_16816(o[jj + i], ah, bv[i >> 1][2 * (i & 1)], bv[i >> 1][2 * (i & 1) + 1]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mma_16816(o[jj + i], al, bv[i >> 1][2 * (i & 1)], bv[i >> 1][2 * (i & 1) + 1]);
+                }
+            }
+            __syncwarp();
+            // (the last tile's keys make room for the warps' merge first)
+            if (lane == 0 && (WK == 1 || j + 1 < j1)) ptx::mbar_arrive(&empty[s]);
+        }
+#pragma unroll
+        for (int i = 1; i <= 2; i <<= 1) {
+            lA += __shfl_xor_sync(0xffffffffu, lA, i);
+            lB += __shfl_xor_sync(0xffffffffu, lB, i);
+        }
+        if (__any_sync(0xffffffffu, odd)) {
+            for (int key = (it.t0 + j0) * kFewTile; key < min((it.t0 + j1) * kFewTile, it.hi); ++key) {
+                const int in = key & (kFewTile - 1), key0 = key - in;
+                if (!(key0 < it.lo_all || key0 + kFewTile > it.hi_all)) continue;
+                if (WK > 1 && (in < wkey || in >= wkey + 16)) continue;
+                const int page = p.table[int64_t(r) * p.max_pages + (key >> p.page_shift)];
+                if (page < 0 || page >= p.n_pages) continue;
+                const int64_t slot = (int64_t(page) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
+                const uint32_t* v = reinterpret_cast<const uint32_t*>(p.V + (slot * p.Hk + g) * D) + qc;
+                const bool inA = key >= kA.lo && key < kA.hi, inB = key >= kB.lo && key < kB.hi;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const uint32_t w = v[n * 4];
+                    const float2 f = unpack_bf16x2(w);
+                    if (not_finite(w)) {
+                        if (inA) o[n][0] += f.x;
+                        if (inB) o[n][2] += f.x;
+                    }
+                    if (not_finite(w >> 16)) {
+                        if (inA) o[n][1] += f.y;
+                        if (inB) o[n][3] += f.y;
+                    }
+                }
+            }
+        }
+
+        if constexpr (WK == 4) {
+            // warps 2 and 3 hand their results to 0 and 1, then 1 to 0, through the last tile's keys
+            if (j1 > j0) {
+                const int s = (issued - 1) % T::kStages;
+                float* buf = reinterpret_cast<float*>(ring + s * T::kStage);  // [2][16][D]
+#pragma unroll
+                for (int half = 2; half >= 1; half >>= 1) {
+                    bar();  // every warp is done with the keys, or with the buffer
+                    if (warp >= half && warp < 2 * half) {
+                        float* to = buf + (warp - half) * 16 * D;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            *reinterpret_cast<float2*>(to + quad * D + n * 8 + 2 * qc) = make_float2(o[n][0], o[n][1]);
+                            *reinterpret_cast<float2*>(to + (quad + 8) * D + n * 8 + 2 * qc) = make_float2(o[n][2], o[n][3]);
+                        }
+                        if (qc == 0) {
+                            warp_m[warp][quad] = mA;
+                            warp_l[warp][quad] = lA;
+                            warp_m[warp][quad + 8] = mB;
+                            warp_l[warp][quad + 8] = lB;
+                        }
+                    }
+                    bar();
+                    if (warp < half) {
+                        const float* from = buf + warp * 16 * D;
+                        const float yA = warp_m[warp + half][quad], yB = warp_m[warp + half][quad + 8];
+                        const float nA = fmaxf(mA, yA), nB = fmaxf(mB, yB);
+                        const float zA = nA == -INFINITY ? 0.0f : nA, zB = nB == -INFINITY ? 0.0f : nB;
+                        const float cA = exp2_fast(mA - zA), cB = exp2_fast(mB - zB);
+                        const float dA = exp2_fast(yA - zA), dB = exp2_fast(yB - zB);
+                        lA = fmaf(lA, cA, warp_l[warp + half][quad] * dA);
+                        lB = fmaf(lB, cB, warp_l[warp + half][quad + 8] * dB);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const float2 u = *reinterpret_cast<const float2*>(from + quad * D + n * 8 + 2 * qc);
+                            const float2 v = *reinterpret_cast<const float2*>(from + (quad + 8) * D + n * 8 + 2 * qc);
+                            o[n][0] = fmaf(o[n][0], cA, u.x * dA);
+                            o[n][1] = fmaf(o[n][1], cA, u.y * dA);
+                            o[n][2] = fmaf(o[n][2], cB, v.x * dB);
+                            o[n][3] = fmaf(o[n][3], cB, v.y * dB);
+                        }
+                        mA = nA;
+                        mB = nB;
+                    }
+                }
+                ptx::fence_proxy_async_smem();  // before the next copy into this buffer
+                bar();
+                if (lane == 0) ptx::mbar_arrive(&empty[s]);
+            }
+        }
+
+        // every warp holds results (WK = 1), or warp 0 does
+        const bool whole = off == 0 && take == uint32_t(it.units);
+        if (whole) {
+            if (WK == 1 || warp == 0) {
+                const float iv = lA == 0.0f ? 0.0f : __fdiv_rn(1.0f, lA), iw = lB == 0.0f ? 0.0f : __fdiv_rn(1.0f, lB);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int c = n * 8 + 2 * qc;
+                    if (okA) *reinterpret_cast<uint32_t*>(p.O + offA + c) = pack_bf16x2(__fmul_rn(o[n][0], iv), __fmul_rn(o[n][1], iv));
+                    if (okB) *reinterpret_cast<uint32_t*>(p.O + offB + c) = pack_bf16x2(__fmul_rn(o[n][2], iw), __fmul_rn(o[n][3], iw));
+                }
+            }
+        } else {
+            const uint32_t a = x - off;  // the item's first unit
+            PagedJoin J{r, g, b, int(a / st.chunk), 0};
+            J.count = int((a + uint32_t(it.units) - 1) / st.chunk) - J.first + 1;
+            if (WK == 1 || warp == 0) {
+                float* s = p.part + part_slot(int(blockIdx.x), J.first) * kSlot;
+                if (qc == 0) {
+                    if (okA) {
+                        s[rA] = mA;
+                        s[ROWS + rA] = lA;
+                    }
+                    if (okB) {
+                        s[rB] = mB;
+                        s[ROWS + rB] = lB;
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int c = n * 8 + 2 * qc;
+                    if (okA) *reinterpret_cast<float2*>(s + 2 * ROWS + rA * D + c) = make_float2(o[n][0], o[n][1]);
+                    if (okB) *reinterpret_cast<float2*>(s + 2 * ROWS + rB * D + c) = make_float2(o[n][2], o[n][3]);
+                }
+                __threadfence();
+                __syncwarp();
+                if (lane == 0) atomicAdd(p.flags + J.first, 1u);
+            }
+            join[joins++ & 1] = J;
+        }
+        x += take;
+        off = 0;
+        if (x < st.x1) next_item(p, r, g, b, it.q.n);
+    }
+
+    // Every CTA joins its share of the items that it has a part in, once all their parts are there. The CTAs of
+    // the grid are all resident, and each publishes its parts before it waits.
+    for (int k = 0; k < joins; ++k) {
+        const PagedJoin J = k == 0 ? join[0] : join[1];
+        constexpr uint32_t kHolders = WK == 1 ? kFewWarps : 1;
+        const uint32_t parts = kHolders * uint32_t(J.count);
+        bool ok = true;
+        if (lane == 0) ok = join_wait(p.flags + J.first, parts, &abort_flag, p.status);
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        __syncwarp();
+        if (ok) {
+            join_store<D, ROWS>(p, J, paged_req(p, J.r), int(blockIdx.x) - J.first, threadIdx.x, 32 * kFewWarps);
+            __syncwarp();
+            // the last warp to leave hands the flag back at zero
+            if (lane == 0 && atomicAdd(p.flags + J.first, 1u) == parts + uint32_t(kFewWarps * J.count) - 1)
+                ptx::st_relaxed_gpu(p.flags + J.first, 0u);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ host side
+
+using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+    static EncodeTiledFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiledFn>(f);
+    });
+    return fn;
+}
+
+// A cache array as (head_dim, kv head, place in page, page), boxes of 64 dims x `box` places, rows of
+// 128 bytes swizzled.
+bool encode_cache(CUtensorMap* m, const void* base, const PagedAttnArgs& a, uint32_t box) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t D = cuuint64_t(a.head_dim), Hk = cuuint64_t(a.n_kv_heads), P = cuuint64_t(a.page_size);
+    const cuuint64_t dims[4] = {D, Hk, P, cuuint64_t(a.n_pages)};
+    const cuuint64_t strides[3] = {D * 2, Hk * D * 2, P * Hk * D * 2};
+    const cuuint32_t boxes[4] = {64, 1, box, 1}, ones[4] = {1, 1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, boxes, ones,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr size_t kFlagBytes = 4096;
+
+// CTAs that run at once, asked once per device; the opt-in shared memory is a per-device attribute too.
+template <int D, int WK, bool CAP>
+cudaError_t few_resident(int& ctas) {
+    static std::mutex mu;
+    static int known[64] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    std::lock_guard<std::mutex> lock(mu);
+    if (dev >= 0 && dev < 64 && known[dev]) {
+        ctas = known[dev];
+        return cudaSuccess;
+    }
+    auto* kernel = paged_few_kernel<D, WK, CAP>;
+    int per_sm = 0;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FewTraits<D>::kSmem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kFewThreads, FewTraits<D>::kSmem);
+    if (e != cudaSuccess) return e;
+    // a partial result per item border: two per CTA, within the workspace
+    const size_t slot = size_t(kFewRows<WK>) * (D + 2) * 4;
+    const int fit = int((EMB_PAGED_WORKSPACE - kFlagBytes) / (2 * slot));
+    ctas = std::max(1, std::min({std::max(1, per_sm) * std::max(1, device_sm_count()), fit, int(kFlagBytes / 4)}));
+    if (dev >= 0 && dev < 64) known[dev] = ctas;
+    return cudaSuccess;
+}
+
+// Units of work of a call, at most: every block of every request over a full block table.
+double unit_bound(const PagedAttnArgs& a, int qb, int kt) {
+    const double keys = std::min(double(a.max_pages) * double(a.page_size), 2147483647.0);
+    const double blocks = std::floor(double(a.n_tokens) / qb) + double(std::min(a.n_req, a.n_tokens));
+    return double(a.n_kv_heads) * blocks * (std::ceil(keys / kt) + 1.0);
+}
+
+template <int D, int WK, bool CAP>
+cudaError_t launch_few(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
+    int ctas = 0;
+    const cudaError_t e = few_resident<D, WK, CAP>(ctas);
+    if (e != cudaSuccess) return e;
+    p.QB = kFewRows<WK> / p.G;
+    p.min_units = 1;
+    const uint32_t box = uint32_t(std::min<int64_t>(a.page_size, kFewTile));
+    if (!encode_cache(&p.k_map, a.k_cache, a, box) || !encode_cache(&p.v_map, a.v_cache, a, box)) return cudaErrorInvalidValue;
+    void* args[] = {&p};
+    const unsigned grid = unsigned(std::min(double(ctas), unit_bound(a, p.QB, kFewTile)));
+    return launch_serialised(reinterpret_cast<const void*>(paged_few_kernel<D, WK, CAP>), grid, kFewThreads, FewTraits<D>::kSmem, s, args);
+}
+
+template <int D>
+cudaError_t launch_few_d(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
+    const bool one_warp_rows = p.G <= 16 && a.max_q * p.G <= 16;  // a request's rows fit a warp's 16
+    if (a.cap > 0.0f) return one_warp_rows ? launch_few<D, 4, true>(p, a, s) : launch_few<D, 1, true>(p, a, s);
+    return one_warp_rows ? launch_few<D, 4, false>(p, a, s) : launch_few<D, 1, false>(p, a, s);
+}
+
+}  // namespace
+
+double paged_attention_tiles(const PagedAttnArgs& a) { return unit_bound(a, std::max<int>(1, int(16 / (a.n_heads / a.n_kv_heads))), kFewTile); }
+
+cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s) {
+    PagedParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.Q = reinterpret_cast<const __nv_bfloat16*>(a.Q);
+    p.K = reinterpret_cast<const __nv_bfloat16*>(a.k_cache);
+    p.V = reinterpret_cast<const __nv_bfloat16*>(a.v_cache);
+    p.O = reinterpret_cast<__nv_bfloat16*>(a.O);
+    p.table = a.table;
+    p.q_start = a.q_start;
+    p.kv_len = a.kv_len;
+    p.prefix = a.prefix;
+    p.flags = static_cast<uint32_t*>(a.workspace);
+    p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + kFlagBytes);
+    p.status = a.status;
+    p.max_pages = a.max_pages;
+    p.n_tokens = a.n_tokens;
+    p.n_req = int(a.n_req);
+    p.n_pages = int(a.n_pages);
+    while ((int64_t(1) << p.page_shift) < a.page_size) ++p.page_shift;
+    p.kv_limit = int(std::min<int64_t>(a.max_pages * a.page_size, 2147483647));
+    p.window = int(std::min<int64_t>(a.window, 2147483647));
+    p.H = int(a.n_heads);
+    p.Hk = int(a.n_kv_heads);
+    p.G = p.H / p.Hk;
+    constexpr double kLog2e = 1.4426950408889634;
+    p.scale2 = a.cap > 0.0f ? float(2.0 * kLog2e * double(a.scale) / double(a.cap)) : float(kLog2e * double(a.scale));
+    p.cap2 = float(kLog2e * double(a.cap));
+    return a.head_dim == 64    ? launch_few_d<64>(p, a, s)
+           : a.head_dim == 128 ? launch_few_d<128>(p, a, s)
+                               : launch_few_d<256>(p, a, s);
+}
+
+}  // namespace emb
