@@ -18,7 +18,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libembqmm.so")
 SOURCES = ["api.cu", "quant.cu", "gemv.cu", "gemm_tc.cu", "layer_ops.cu"]
 PAGED_LIB = os.path.join(HERE, "libembpaged.so")
-PAGED_SOURCES = ["paged_api.cu", "paged_cache.cu", "paged_attention.cu"]
+PAGED_SOURCES = ["paged_api.cu", "paged_cache.cu", "paged_attention.cu", "paged_many.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -5,9 +5,7 @@
 #include <cstring>
 #include <mutex>
 
-#include <cuda.h>
-
-#include "paged_sched.cuh"
+#include "paged_math.cuh"
 
 namespace emb {
 namespace {
@@ -19,20 +17,6 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// 2^x (results below the normal range become zero; -inf gives 0).
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float rcp_fast(float x) {
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-// cap log2(e) tanh(y / 2), y = 2 scale q.k / cap with its base 2: tanh as 1 - 2 / (1 + e^y), within 2^-22 of 1
-__device__ __forceinline__ float capped(float y, float cap2) { return fmaf(-2.0f * cap2, rcp_fast(1.0f + exp2_fast(y)), cap2); }
-
 __device__ __forceinline__ void ldsm_x4(uint32_t saddr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
@@ -43,59 +27,6 @@ __device__ __forceinline__ void ldsm_x4_trans(uint32_t saddr, uint32_t (&r)[4]) 
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
                  : "r"(saddr));
 }
-__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ float2 unpack_bf16x2(uint32_t w) {
-    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
-}
-__device__ __forceinline__ bool not_finite(uint32_t bf16_bits) { return (bf16_bits & 0x7F80u) == 0x7F80u; }
-
-// Rows of O behind the last request's (padding of a recorded step): zeros.
-__device__ __forceinline__ void zero_padding(const PagedParams& p, int D, int tid, int nt) {
-    const int64_t used = min(max(int64_t(p.q_start[p.n_req]), int64_t(0)), p.n_tokens);
-    const int64_t row16 = int64_t(p.H) * D / 8;
-    uint4* o = reinterpret_cast<uint4*>(p.O);
-    for (int64_t i = used * row16 + int64_t(blockIdx.x) * nt + tid; i < p.n_tokens * row16; i += int64_t(gridDim.x) * nt)
-        o[i] = make_uint4(0, 0, 0, 0);
-}
-
-// Adds the partial results of an item that several CTAs shared and stores this CTA's part of its outputs.
-// A partial result is ROWS maxima, ROWS sums and [ROWS][D] values, in CTA order (deterministic).
-template <int D, int ROWS>
-__device__ __forceinline__ void join_store(const PagedParams& p, const PagedJoin& J, const PagedReq& q, int me, int tid, int nt) {
-    constexpr int64_t kSlot = int64_t(ROWS) * (D + 2);
-    const int i0 = J.b * p.QB, rows = min(p.QB, q.n - i0) * p.G;
-    for (int e = me * nt + tid; e < rows * (D / 4); e += J.count * nt) {
-        const int row = e / (D / 4), c = (e - row * (D / 4)) * 4;
-        float M = -INFINITY;
-#pragma unroll 8
-        for (int i = 0; i < J.count; ++i) M = fmaxf(M, __ldcg(p.part + part_slot(J.first + i, J.first) * kSlot + row));
-        const float m0 = M == -INFINITY ? 0.0f : M;
-        float L = 0.0f;
-        float4 o = make_float4(0, 0, 0, 0);
-#pragma unroll 8
-        for (int i = 0; i < J.count; ++i) {
-            const float* s = p.part + part_slot(J.first + i, J.first) * kSlot;
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(s + 2 * ROWS + row * D + c));
-            // weight 0 of a partial without a finite score: its sums are 0, or NaN, which has to show
-            const float w = exp2_fast(__ldcg(s + row) - m0);
-            L = fmaf(__ldcg(s + ROWS + row), w, L);
-            o.x = fmaf(v.x, w, o.x);
-            o.y = fmaf(v.y, w, o.y);
-            o.z = fmaf(v.z, w, o.z);
-            o.w = fmaf(v.w, w, o.w);
-        }
-        const float inv = L == 0.0f ? 0.0f : __fdiv_rn(1.0f, L);
-        uint2 u;
-        u.x = pack_bf16x2(__fmul_rn(o.x, inv), __fmul_rn(o.y, inv));
-        u.y = pack_bf16x2(__fmul_rn(o.z, inv), __fmul_rn(o.w, inv));
-        const int64_t t = q.q0 + i0 + row / p.G;
-        *reinterpret_cast<uint2*>(p.O + (t * p.H + J.g * p.G + row % p.G) * D + c) = u;
-    }
-}
-
 // ------------------------------------------------------------------ few rows: mma.sync
 // A producer warp brings tiles of 64 keys and values by TMA (a box per page, 128-byte swizzled rows) into a ring;
 // four warps compute. WK = 4: an item has 16 rows (queries times heads), every warp takes 16 of a tile's keys, and the
@@ -575,8 +506,8 @@ EncodeTiledFn encode_fn() {
     return fn;
 }
 
-// A cache array as (head_dim, kv head, place in page, page), boxes of 64 dims x `box` places, rows of
-// 128 bytes swizzled.
+}  // namespace
+
 bool encode_cache(CUtensorMap* m, const void* base, const PagedAttnArgs& a, uint32_t box) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
@@ -589,7 +520,25 @@ bool encode_cache(CUtensorMap* m, const void* base, const PagedAttnArgs& a, uint
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-constexpr size_t kFlagBytes = 4096;
+bool encode_queries(CUtensorMap* m, const PagedAttnArgs& a, uint32_t heads, uint32_t tokens) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t D = cuuint64_t(a.head_dim), H = cuuint64_t(a.n_heads);
+    const cuuint64_t dims[3] = {D, H, cuuint64_t(a.n_tokens)};
+    const cuuint64_t strides[2] = {D * 2, H * D * 2};
+    const cuuint32_t boxes[3] = {64, heads, tokens}, ones[3] = {1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<uint16_t*>(a.Q), dims, strides, boxes, ones,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+double unit_bound(const PagedAttnArgs& a, int qb, int kt) {
+    const double keys = std::min(double(a.max_pages) * double(a.page_size), 2147483647.0);
+    const double blocks = std::floor(double(a.n_tokens) / qb) + double(std::min(a.n_req, a.n_tokens));
+    return double(a.n_kv_heads) * blocks * (std::ceil(keys / kt) + 1.0);
+}
+
+namespace {
 
 // CTAs that run at once, asked once per device; the opt-in shared memory is a per-device attribute too.
 template <int D, int WK, bool CAP>
@@ -611,17 +560,10 @@ cudaError_t few_resident(int& ctas) {
     if (e != cudaSuccess) return e;
     // a partial result per item border: two per CTA, within the workspace
     const size_t slot = size_t(kFewRows<WK>) * (D + 2) * 4;
-    const int fit = int((EMB_PAGED_WORKSPACE - kFlagBytes) / (2 * slot));
-    ctas = std::max(1, std::min({std::max(1, per_sm) * std::max(1, device_sm_count()), fit, int(kFlagBytes / 4)}));
+    const int fit = int((EMB_PAGED_WORKSPACE - kPagedFlagBytes) / (2 * slot));
+    ctas = std::max(1, std::min({std::max(1, per_sm) * std::max(1, device_sm_count()), fit, int(kPagedFlagBytes / 4)}));
     if (dev >= 0 && dev < 64) known[dev] = ctas;
     return cudaSuccess;
-}
-
-// Units of work of a call, at most: every block of every request over a full block table.
-double unit_bound(const PagedAttnArgs& a, int qb, int kt) {
-    const double keys = std::min(double(a.max_pages) * double(a.page_size), 2147483647.0);
-    const double blocks = std::floor(double(a.n_tokens) / qb) + double(std::min(a.n_req, a.n_tokens));
-    return double(a.n_kv_heads) * blocks * (std::ceil(keys / kt) + 1.0);
 }
 
 template <int D, int WK, bool CAP>
@@ -661,7 +603,7 @@ cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s) {
     p.kv_len = a.kv_len;
     p.prefix = a.prefix;
     p.flags = static_cast<uint32_t*>(a.workspace);
-    p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + kFlagBytes);
+    p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + kPagedFlagBytes);
     p.status = a.status;
     p.max_pages = a.max_pages;
     p.n_tokens = a.n_tokens;
@@ -676,6 +618,8 @@ cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s) {
     constexpr double kLog2e = 1.4426950408889634;
     p.scale2 = a.cap > 0.0f ? float(2.0 * kLog2e * double(a.scale) / double(a.cap)) : float(kLog2e * double(a.scale));
     p.cap2 = float(kLog2e * double(a.cap));
+    // a request's rows beyond 64 go to the tensor cores' kernel, which multiplies its scores by a positive scale
+    if (a.max_q * p.G > 64 && a.scale > 0.0f) return launch_paged_many(p, a, s);
     return a.head_dim == 64    ? launch_few_d<64>(p, a, s)
            : a.head_dim == 128 ? launch_few_d<128>(p, a, s)
                                : launch_few_d<256>(p, a, s);

@@ -1,0 +1,578 @@
+// Attention of new tokens over a paged key/value cache, many query rows per request: tcgen05
+// (definition in include/emb_paged.h, work split in paged_sched.cuh).
+//
+// An item has two tiles of up to 128 rows (queries times the heads of one key/value head), or one where heads of 256
+// leave the tensor memory no room for two. Keys and values come in tiles of 128 (64) through one ring of TMA
+// copies, keys and values in turn. One warp issues the MMAs: S = Q K^T from shared memory into tensor memory, and O += P V with
+// P read from tensor memory, where it takes the place of its scores. Each row tile has a warpgroup for its
+// softmax, a thread a row, so a row's maximum and sum need no exchange. While one tile's softmax runs the tensor
+// cores work for the other; with one tile its scores have two places in turn. The running maximum moves only when it
+// grows by more than 2^8 (P and its sums stay far within fp32 and bf16's relative precision), so the output in tensor
+// memory is seldom rescaled.
+#include <algorithm>
+#include <mutex>
+
+#include "paged_math.cuh"
+
+namespace emb {
+namespace {
+
+template <int D>
+struct ManyTraits {
+    static constexpr int NQ = D == 256 ? 1 : 2;        // row tiles of an item
+    static constexpr int KT = D == 256 ? 64 : 128;     // keys of a tile
+    static constexpr int kSoftWarps = 4 * NQ;
+    static constexpr int kThreads = 32 * (kSoftWarps + 2);
+    static constexpr int kQTile = 128 * D * 2;         // bytes of a row tile's queries
+    static constexpr int kSlot = KT * D * 2;           // bytes of a tile of keys or values
+    static constexpr int kSlots = D == 64 ? 8 : 5;
+    static constexpr int kSmem = 1024 + NQ * kQTile + kSlots * kSlot;
+    static constexpr int kSub = KT * 128;              // bytes of 64 dims of a tile
+    // columns of tensor memory: scores (two places), outputs
+    static constexpr int kO = 2 * KT;
+};
+constexpr uint32_t kTmemAll = 512;
+static_assert(ManyTraits<64>::kSmem > 114 * 1024 && ManyTraits<128>::kSmem > 114 * 1024 && ManyTraits<256>::kSmem > 114 * 1024,
+              "one CTA per SM: tensor memory is allocated whole (see ptx::tmem_alloc)");
+
+// Largest of three.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// Two fp32 FMAs and sums at once.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "add.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+
+// The part of an item that lies in this CTA's stretch: tiles [j0, j1), of which row tile t has [a[t], b[t]).
+template <int D>
+struct Segment {
+    PagedItem it;
+    uint32_t take;
+    int j0, j1;
+    int a[2], b[2], nq[2];
+};
+template <int D>
+__device__ __forceinline__ Segment<D> segment_of(const PagedParams& p, int r, int g, int b, uint32_t off, uint32_t x, uint32_t x1) {
+    using T = ManyTraits<D>;
+    Segment<D> s;
+    s.it = paged_item<T::KT>(p, r, g, b);
+    s.take = min(x1 - x, uint32_t(s.it.units) - off);
+    s.j0 = s.it.t0 + int(off);
+    s.j1 = s.it.t0 + min(int(off + s.take), s.it.nt);
+    const int qt = p.QB / T::NQ;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        s.nq[t] = t < T::NQ ? max(0, min(qt, s.it.nq - t * qt)) : 0;
+        s.a[t] = s.b[t] = 0;
+        if (s.nq[t] == 0) continue;
+        const int i0 = s.it.i0 + t * qt;
+        const KeyRange first = query_keys(p, s.it.q, i0), last = query_keys(p, s.it.q, i0 + s.nq[t] - 1);
+        if (last.hi <= first.lo) continue;
+        s.a[t] = max(s.j0, first.lo / T::KT);
+        s.b[t] = min(s.j1, (last.hi + T::KT - 1) / T::KT);
+        if (s.b[t] < s.a[t]) s.b[t] = s.a[t];
+    }
+    return s;
+}
+
+template <int D, bool CAP>
+__global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(const __grid_constant__ PagedParams p) {
+    using T = ManyTraits<D>;
+    constexpr int NQ = T::NQ, KT = T::KT, S = T::kSlots;
+    constexpr int kRows = 128 * NQ;
+    constexpr int64_t kPart = int64_t(kRows) * (D + 2);
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t kv_full[S], kv_empty[S], q_full, q_empty, s_full[2], p_ready[2], o_done[2], o_free[2], drain;
+    __shared__ uint32_t tmem_slot, odd_item;
+    __shared__ int abort_flag;
+    uint8_t* sq = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* ring = sq + NQ * T::kQTile;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned all = 0xffffffffu;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S; ++i) {
+            ptx::mbar_init(&kv_full[i], 1);
+            ptx::mbar_init(&kv_empty[i], 1);
+        }
+        ptx::mbar_init(&q_full, 1);
+        ptx::mbar_init(&q_empty, 1);
+        for (int t = 0; t < 2; ++t) {
+            ptx::mbar_init(&s_full[t], 1);
+            ptx::mbar_init(&p_ready[t], 4);
+            ptx::mbar_init(&o_done[t], 1);
+            ptx::mbar_init(&o_free[t], 4);
+        }
+        ptx::mbar_init(&drain, 1);
+        abort_flag = 0;
+        odd_item = 0;
+        ptx::fence_mbar_init();
+        ptx::prefetch_tmap(&p.q_map);
+        ptx::prefetch_tmap(&p.k_map);
+        ptx::prefetch_tmap(&p.v_map);
+    }
+    if (warp == T::kSoftWarps) {
+        ptx::tmem_alloc(&tmem_slot, kTmemAll);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = ptx::warp_uniform(tmem_slot);
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();  // lengths, queries and the new tokens' keys and values come from earlier launches
+    const PagedStretch st = paged_stretch<KT, T::kThreads>(p);
+
+    int r = st.r, g = st.g, b = st.b;
+    uint32_t x = st.x0, off = st.off;
+    auto wait = [&](uint64_t* bar, uint32_t phase) {
+        return __all_sync(all, ptx::mbar_wait(bar, phase & 1, &abort_flag, p.status, kWaitLimitNs)) != 0;
+    };
+    // the tiles of the stretch are numbered through; tile n has its keys in ring position 2 n, its values in 2 n + 1
+    auto slot_of = [](uint32_t pos) { return int(pos % uint32_t(S)); };
+    auto turn_of = [](uint32_t pos) { return pos / uint32_t(S); };
+
+    if (warp == T::kSoftWarps + 1) {
+        // ---------------------------------------------------------------------- producer
+        ptx::fence_proxy_async_global();  // (the cache and the queries were written by ordinary stores)
+        const int page_size = 1 << p.page_shift, box = min(page_size, KT), n_box = KT / box;
+        const int qt = p.QB / NQ;
+        uint32_t n = 0, loads = 0, items = 0;  // tiles; ring copies and items with queries issued
+        bool ok = true;
+        while (x < st.x1 && ok) {
+            const Segment<D> sg = segment_of<D>(p, r, g, b, off, x, st.x1);
+            const PagedItem& it = sg.it;
+            if (sg.j1 > sg.j0) {
+                if (items > 0) ok = wait(&q_empty, items - 1);
+                if (!ok) break;
+                const int tiles_q = sg.nq[1] > 0 ? 2 : 1;
+                if (ptx::elect_one()) {
+                    ptx::mbar_arrive_expect_tx(&q_full, uint32_t(tiles_q * (D / 64) * qt * p.G * 128));
+                    for (int t = 0; t < tiles_q; ++t)
+#pragma unroll
+                        for (int c = 0; c < D / 64; ++c)
+                            ptx::tma_load_3d(sq + t * T::kQTile + c * 16384, &p.q_map, &q_full, c * 64, g * p.G, it.q.q0 + it.i0 + t * qt);
+                }
+                __syncwarp();
+                ++items;
+            }
+            const int32_t* row = p.table + int64_t(r) * p.max_pages;
+            // lane i looks up the page of the tile's box i; boxes that no query sees, and pages that do not exist,
+            // are fetched from behind the cache: zeros
+            auto page_of = [&](int j) {
+                const int key = j * KT + lane * box;
+                int page = p.n_pages;
+                if (lane < n_box && j < sg.j1 && key < it.hi && key + box > it.lo) {
+                    page = row[key >> p.page_shift];
+                    if (page < 0 || page > p.n_pages) page = p.n_pages;
+                }
+                return page;
+            };
+            int page = page_of(sg.j0);
+            for (int j = sg.j0; j < sg.j1 && ok; ++j, ++n) {
+                const int next = page_of(j + 1);
+                const int place = (j * KT) & (page_size - 1);
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    const uint32_t pos = 2 * n + kv;
+                    const int s = slot_of(pos);
+                    if (turn_of(pos) > 0) ok = wait(&kv_empty[s], turn_of(pos) - 1);
+                    if (!ok) break;
+                    if (ptx::elect_one()) ptx::mbar_arrive_expect_tx(&kv_full[s], T::kSlot);
+                    __syncwarp();
+                    for (int i = 0; i < n_box; ++i) {
+                        const int pg = __shfl_sync(all, page, i);
+                        if (ptx::elect_one()) {
+#pragma unroll
+                            for (int c = 0; c < D / 64; ++c)
+                                ptx::tma_load_4d(ring + s * T::kSlot + c * T::kSub + i * box * 128, kv ? &p.v_map : &p.k_map,
+                                                 &kv_full[s], c * 64, g, place, pg);
+                        }
+                        __syncwarp();
+                    }
+                    loads = pos + 1;
+                }
+                page = next;
+            }
+            x += sg.take;
+            off = 0;
+            if (x < st.x1) next_item(p, r, g, b, it.q.n);
+        }
+        // every copy must land before this CTA's shared memory is released
+        for (uint32_t i = loads > uint32_t(S) ? loads - S : 0; i < loads; ++i)
+            ptx::mbar_wait(&kv_full[slot_of(i)], turn_of(i) & 1, nullptr, p.status, kWaitLimitNs);
+        if (items > 0) ptx::mbar_wait(&q_full, (items - 1) & 1, nullptr, p.status, kWaitLimitNs);
+    } else if (warp == T::kSoftWarps) {
+        // ------------------------------------------------------------------------- MMAs
+        const uint32_t idesc_qk = ptx::idesc_bf16_f32(128, KT), idesc_pv = ptx::idesc_bf16_f32(128, D) | ptx::kIdescMnMajorB;
+        const uint32_t sq_u = ptx::smem_u32(sq), ring_u = ptx::smem_u32(ring);
+        uint32_t n = 0, items = 0;
+        uint32_t scores[2] = {0, 0}, owned[2] = {0, 0};  // score tiles by place, items with outputs by row tile
+        bool ok = true;
+        auto qk = [&](int t, int place, uint32_t pos) {  // S[place] = Q[t] K^T
+            const uint32_t k = ring_u + uint32_t(slot_of(pos) * T::kSlot);
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks)
+                ptx::mma_bf16_ss(tmem + uint32_t(place * KT), ptx::smem_desc_sw128(sq_u + t * T::kQTile + (ks / 4) * 16384) + 2 * (ks & 3),
+                                 ptx::smem_desc_sw128(k + (ks / 4) * T::kSub) + 2 * (ks & 3), idesc_qk, ks != 0);
+            ptx::mma_commit(&s_full[place]);
+        };
+        auto pv = [&](int t, int place, uint32_t pos, bool first) {  // O[t] (+)= P[place] V
+            const uint32_t v = ring_u + uint32_t(slot_of(pos) * T::kSlot);
+            const uint64_t desc = ptx::smem_desc_mn_sw128(v, T::kSub);
+#pragma unroll
+            for (int kk = 0; kk < KT / 16; ++kk)
+                ptx::mma_bf16_ta(tmem + uint32_t(T::kO + t * D), tmem + uint32_t(place * KT + 8 * kk), desc + uint32_t(kk * 2048 / 16),
+                                 idesc_pv, !first || kk != 0);
+            ptx::mma_commit(&o_done[t]);
+        };
+        while (x < st.x1 && ok) {
+            const Segment<D> sg = segment_of<D>(p, r, g, b, off, x, st.x1);
+            if (sg.j1 > sg.j0) {
+                ok = wait(&q_full, items++);
+                for (int j = sg.j0; j <= sg.j1 && ok; ++j) {
+                    const uint32_t pos = 2 * n;  // of tile j's keys; the tile before has its values in pos - 1
+                    if (j < sg.j1) ok = wait(&kv_full[slot_of(pos)], turn_of(pos));
+                    if (!ok) break;
+                    ptx::tc_fence_after();
+                    auto finish = [&](int t, int place) {  // P V of tile j - 1
+                        const bool first = j - 1 == sg.a[t];
+                        ok = wait(&kv_full[slot_of(pos - 1)], turn_of(pos - 1)) && wait(&p_ready[place], scores[place] - 1);
+                        if (ok && first && owned[t] > 0) ok = wait(&o_free[t], owned[t] - 1);
+                        if (!ok) return;
+                        ptx::tc_fence_after();
+                        pv(t, place, pos - 1, first);
+                        if (first) ++owned[t];
+                    };
+                    if constexpr (NQ == 2) {
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            if (j > sg.a[t] && j <= sg.b[t]) finish(t, t);
+                            if (!ok) break;
+                            if (j >= sg.a[t] && j < sg.b[t]) {
+                                qk(t, t, pos);
+                                ++scores[t];
+                            }
+                        }
+                    } else {
+                        if (j < sg.j1) {
+                            qk(0, int(n & 1), pos);
+                            ++scores[n & 1];
+                        }
+                        if (j > sg.j0) finish(0, int((n - 1) & 1));
+                    }
+                    if (!ok) break;
+                    if (j > sg.j0) ptx::mma_commit(&kv_empty[slot_of(pos - 1)]);
+                    if (j < sg.j1) {
+                        ptx::mma_commit(&kv_empty[slot_of(pos)]);
+                        ++n;
+                        if (j == sg.j1 - 1) ptx::mma_commit(&q_empty);
+                    }
+                }
+            }
+            x += sg.take;
+            off = 0;
+            if (x < st.x1) next_item(p, r, g, b, sg.it.q.n);
+        }
+        // whatever was issued finishes before tensor memory is freed
+        ptx::mma_commit(&drain);
+        ptx::mbar_wait(&drain, 0, nullptr, p.status, kWaitLimitNs);
+    } else {
+        // ---------------------------------------------------------------------- softmax
+        zero_padding(p, D, threadIdx.x, 32 * T::kSoftWarps);
+        const int t = warp >> 2;  // row tile
+        const int row = 32 * (warp & 3) + lane, qt = p.QB / NQ, i = row / p.G;
+        const uint32_t lanes = uint32_t(32 * (warp & 3)) << 16;
+        const uint32_t o_col = tmem + lanes + uint32_t(T::kO + t * D);
+        uint32_t n = 0, seen[2] = {0, 0}, outs = 0, ordinal = 0;
+        PagedJoin join[2];
+        int joins = 0;
+        bool ok = true;
+        while (x < st.x1 && ok) {
+            const Segment<D> sg = segment_of<D>(p, r, g, b, off, x, st.x1);
+            const PagedItem& it = sg.it;
+            ++ordinal;
+            const bool live = i < sg.nq[t];
+            const KeyRange keys = live ? query_keys(p, it.q, it.i0 + t * qt + i) : KeyRange{0, 0};
+            float m = -INFINITY, mc = 0.0f;  // running maximum (of raw or capped scores) and what is subtracted
+            float2 l2[2] = {make_float2(0, 0), make_float2(0, 0)};
+            for (int j = sg.j0; j < sg.j1 && ok; ++j, ++n) {
+                if (j < sg.a[t] || j >= sg.b[t]) continue;
+                const int place = NQ == 2 ? t : int(n & 1);
+                ok = wait(&s_full[place], seen[place]++);
+                if (!ok) break;
+                ptx::tc_fence_after();
+                const uint32_t s_col = tmem + lanes + uint32_t(place * KT);
+                float s[KT];
+#pragma unroll
+                for (int c = 0; c < KT; c += 32) ptx::tmem_ld_32(s_col + c, s + c);
+                ptx::tmem_ld_wait();
+                if constexpr (CAP) {
+#pragma unroll
+                    for (int e = 0; e < KT; ++e) s[e] = capped(__fmul_rn(s[e], p.scale2), p.cap2);
+                }
+                const int key0 = j * KT;
+                const bool edge = key0 < it.lo_all || key0 + KT > it.hi_all;
+                if (edge) {
+                    const int lo = keys.lo - key0, hi = keys.hi - key0;
+#pragma unroll
+                    for (int e = 0; e < KT; ++e)
+                        if (e < lo || e >= hi) s[e] = -INFINITY;
+                }
+                float top[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+                for (int e = 4; e + 7 < KT; e += 8)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) top[k] = max3(top[k], s[e + k], s[e + 4 + k]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], s[KT - 4 + k]);
+                const float mt = fmaxf(max3(top[0], top[1], top[2]), top[3]);
+                const float unit = CAP ? 1.0f : p.scale2;  // base-2 units of a score
+                const bool grow = m == -INFINITY ? mt > m : (mt - m) * unit > 8.0f;
+                if (__any_sync(all, grow)) {
+                    const float m1 = grow ? mt : m;
+                    const float f = m1 == -INFINITY ? 1.0f : exp2_fast((m - m1) * unit);  // (-inf - x: 0)
+                    if (j > sg.a[t]) {
+                        ok = wait(&o_done[t], outs - 1);  // every product issued so far is in
+                        if (!ok) break;
+                        ptx::tc_fence_after();
+#pragma unroll
+                        for (int c = 0; c < D; c += 32) {
+                            float o[32];
+                            uint32_t w[32];
+                            ptx::tmem_ld_32(o_col + c, o);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(grow ? o[e] * f : o[e]);
+                            ptx::tmem_st_32(o_col + c, w);
+                        }
+                    }
+                    if (grow) {
+                        const float2 ff = make_float2(f, f), z = make_float2(0, 0);
+                        l2[0] = fma2(l2[0], ff, z);
+                        l2[1] = fma2(l2[1], ff, z);
+                        m = m1;
+                        mc = -m * unit;
+                    }
+                }
+                const float2 sc = make_float2(unit, unit), mm = make_float2(mc, mc);
+#pragma unroll
+                for (int c = 0; c < KT; c += 64) {
+                    uint32_t w[32];
+#pragma unroll
+                    for (int e = 0; e < 64; e += 2) {
+                        float2 v = fma2(make_float2(s[c + e], s[c + e + 1]), sc, mm);
+                        v.x = exp2_fast(v.x);
+                        v.y = exp2_fast(v.y);
+                        l2[(e >> 1) & 1] = add2(l2[(e >> 1) & 1], v);
+                        w[e / 2] = pack_bf16x2(v.x, v.y);
+                    }
+                    ptx::tmem_st_32(s_col + c / 2, w);
+                }
+                if (edge && t == (NQ == 2 && !(j >= sg.a[0] && j < sg.b[0]) ? 1 : 0)) {
+                    // values behind the request's last key are anything; those hidden from some rows may not be multiplied
+                    // by their weights of 0 if they are not finite: such values leave the tile here and are added
+                    // at the item's end for the rows that see them
+                    const uint32_t pos = 2 * n + 1;
+                    ok = wait(&kv_full[slot_of(pos)], turn_of(pos));
+                    if (!ok) break;
+                    uint8_t* v = ring + slot_of(pos) * T::kSlot;
+                    bool odd = false;
+                    for (int e = row; e < KT * (D / 8); e += 128) {  // 16 bytes of one key, whatever their dims
+                        const int key = (e / 8) % KT;
+                        uint4* at = reinterpret_cast<uint4*>(v) + e;
+                        if (key0 + key >= it.q.L) {
+                            *at = make_uint4(0, 0, 0, 0);
+                            continue;
+                        }
+                        uint4 u = *at;
+                        uint32_t* h = reinterpret_cast<uint32_t*>(&u);
+                        bool hit = false;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            if (not_finite(h[k])) {
+                                h[k] &= 0xFFFF0000u;
+                                hit = true;
+                            }
+                            if (not_finite(h[k] >> 16)) {
+                                h[k] &= 0x0000FFFFu;
+                                hit = true;
+                            }
+                        }
+                        if (hit) *at = u;
+                        odd |= hit;
+                    }
+                    if (odd) *reinterpret_cast<volatile uint32_t*>(&odd_item) = ordinal;
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                }
+                ptx::tmem_st_wait();
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&p_ready[place]);
+                ++outs;
+            }
+            if (!ok) break;
+            // the segment's result: outputs, or this CTA's part of them
+            const bool has = sg.b[t] > sg.a[t];
+            float l = (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
+            if (has) {
+                ok = wait(&o_done[t], outs - 1);
+                if (!ok) break;
+                ptx::tc_fence_after();
+            }
+            const bool whole = off == 0 && sg.take == uint32_t(it.units);
+            const uint32_t a = x - off;  // the item's first unit
+            PagedJoin J{r, g, b, int(a / st.chunk), 0};
+            J.count = int((a + uint32_t(it.units) - 1) / st.chunk) - J.first + 1;
+            float* part = p.part + part_slot(int(blockIdx.x), J.first) * kPart;
+            const int prow = t * qt * p.G + row;  // rows of both tiles in order
+            __nv_bfloat16* out = p.O + (int64_t(it.q.q0 + it.i0 + t * qt + i) * p.H + g * p.G + (row - i * p.G)) * D;
+            const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
+            const bool odd = has && *reinterpret_cast<volatile uint32_t*>(&odd_item) == ordinal;
+            if (!whole && live) {
+                part[prow] = CAP ? m : m * p.scale2;
+                part[kRows + prow] = l;
+            }
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+                float o[32];
+                __syncwarp();
+                if (has) {
+                    ptx::tmem_ld_32(o_col + c, o);
+                    ptx::tmem_ld_wait();
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0.0f;
+                }
+                if (odd) {
+                    for (int key = max(keys.lo, sg.j0 * KT); key < min(keys.hi, sg.j1 * KT); ++key) {
+                        const int key0 = key / KT * KT;
+                        if (!(key0 < it.lo_all || key0 + KT > it.hi_all)) continue;
+                        const int page = p.table[int64_t(r) * p.max_pages + (key >> p.page_shift)];
+                        if (page < 0 || page >= p.n_pages) continue;
+                        const int64_t slot = (int64_t(page) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
+                        const uint32_t* v = reinterpret_cast<const uint32_t*>(p.V + (slot * p.Hk + g) * D + c);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const uint32_t w = v[e];
+                            const float2 f = unpack_bf16x2(w);
+                            if (not_finite(w)) o[2 * e] += f.x;
+                            if (not_finite(w >> 16)) o[2 * e + 1] += f.y;
+                        }
+                    }
+                }
+                if (!live) continue;
+                if (whole) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        uint4 u;
+                        u.x = pack_bf16x2(__fmul_rn(o[e], inv), __fmul_rn(o[e + 1], inv));
+                        u.y = pack_bf16x2(__fmul_rn(o[e + 2], inv), __fmul_rn(o[e + 3], inv));
+                        u.z = pack_bf16x2(__fmul_rn(o[e + 4], inv), __fmul_rn(o[e + 5], inv));
+                        u.w = pack_bf16x2(__fmul_rn(o[e + 6], inv), __fmul_rn(o[e + 7], inv));
+                        *reinterpret_cast<uint4*>(out + c + e) = u;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<float4*>(part + 2 * kRows + prow * D + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                }
+            }
+            if (has) {
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&o_free[t]);
+            }
+            if (!whole) {
+                __threadfence();
+                __syncwarp();
+                if (lane == 0) atomicAdd(p.flags + J.first, 1u);
+                join[joins++ & 1] = J;
+            }
+            x += sg.take;
+            off = 0;
+            if (x < st.x1) next_item(p, r, g, b, it.q.n);
+        }
+        // Every CTA joins its share of the items that it has a part in, once all their parts are there. The CTAs of
+        // the grid are all resident, and each publishes its parts before it waits.
+        for (int k = 0; k < joins && ok; ++k) {
+            const PagedJoin J = k == 0 ? join[0] : join[1];
+            const uint32_t parts = uint32_t(T::kSoftWarps * J.count);
+            bool in = true;
+            if (lane == 0) in = join_wait(p.flags + J.first, parts, &abort_flag, p.status);
+            if (!__shfl_sync(all, in, 0)) break;
+            __syncwarp();
+            join_store<D, kRows>(p, J, paged_req(p, J.r), int(blockIdx.x) - J.first, threadIdx.x, 32 * T::kSoftWarps);
+            __syncwarp();
+            // the last warp to leave hands the flag back at zero
+            if (lane == 0 && atomicAdd(p.flags + J.first, 1u) == 2 * parts - 1) ptx::st_relaxed_gpu(p.flags + J.first, 0u);
+        }
+    }
+    __syncwarp();
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == T::kSoftWarps) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, kTmemAll);
+    }
+}
+
+template <int D, bool CAP>
+cudaError_t launch_many(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
+    using T = ManyTraits<D>;
+    // the opt-in shared-memory size is a per-device function attribute
+    static std::mutex mu;
+    static bool done[64] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (dev < 0 || dev >= 64 || !done[dev]) {
+            e = cudaFuncSetAttribute(paged_many_kernel<D, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::kSmem);
+            if (e != cudaSuccess) return e;
+            if (dev >= 0 && dev < 64) done[dev] = true;
+        }
+    }
+    const int tile = 128 / p.G;  // queries of a row tile
+    p.QB = T::NQ * tile;
+    p.min_units = 1;
+    const uint32_t box = uint32_t(std::min<int64_t>(a.page_size, T::KT));
+    if (!encode_cache(&p.k_map, a.k_cache, a, box) || !encode_cache(&p.v_map, a.v_cache, a, box) ||
+        !encode_queries(&p.q_map, a, uint32_t(p.G), uint32_t(tile)))
+        return cudaErrorInvalidValue;
+    const size_t part = size_t(128 * T::NQ) * (D + 2) * 4;
+    const int fit = int((EMB_PAGED_WORKSPACE - kPagedFlagBytes) / (2 * part));
+    const int ctas = std::max(1, std::min({device_sm_count(), fit, int(kPagedFlagBytes / 4)}));
+    void* args[] = {&p};
+    const unsigned grid = unsigned(std::min(double(ctas), unit_bound(a, p.QB, T::KT)));
+    return launch_serialised(reinterpret_cast<const void*>(paged_many_kernel<D, CAP>), grid, T::kThreads, T::kSmem, s, args);
+}
+
+}  // namespace
+
+cudaError_t launch_paged_many(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
+    const bool cap = a.cap > 0.0f;
+    if (a.head_dim == 64) return cap ? launch_many<64, true>(p, a, s) : launch_many<64, false>(p, a, s);
+    if (a.head_dim == 128) return cap ? launch_many<128, true>(p, a, s) : launch_many<128, false>(p, a, s);
+    return cap ? launch_many<256, true>(p, a, s) : launch_many<256, false>(p, a, s);
+}
+
+}  // namespace emb

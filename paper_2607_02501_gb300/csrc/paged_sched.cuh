@@ -231,4 +231,16 @@ __device__ __forceinline__ bool join_wait(const uint32_t* flag, uint32_t count, 
     }
 }
 
+// ------------------------------------------------------------------ host side
+constexpr size_t kPagedFlagBytes = 4096;  // of the workspace
+
+// A cache array as (head_dim, kv head, place in page, page), boxes of 64 dims x `box` places; Q as (head_dim, head,
+// token), boxes of 64 dims x heads x tokens. Rows of 128 bytes, swizzled.
+bool encode_cache(CUtensorMap* m, const void* base, const PagedAttnArgs& a, uint32_t box);
+bool encode_queries(CUtensorMap* m, const PagedAttnArgs& a, uint32_t heads, uint32_t tokens);
+// Units of work of a call, at most: every block of every request over a full block table.
+double unit_bound(const PagedAttnArgs& a, int qb, int kt);
+// The tcgen05 kernel (paged_many.cu).
+cudaError_t launch_paged_many(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s);
+
 }  // namespace emb
