@@ -22,7 +22,7 @@ struct ManyTraits {
     static constexpr int NQ = D == 256 ? 1 : 2;        // row tiles of an item
     static constexpr int KT = D == 256 ? 64 : 128;     // keys of a tile
     static constexpr int kSoftWarps = 4 * NQ;
-    static constexpr int kThreads = 32 * (kSoftWarps + 2);
+    static constexpr int kThreads = 32 * (kSoftWarps + 2);  // and the MMA and the producer warp
     static constexpr int kQTile = 128 * D * 2;         // bytes of a row tile's queries
     static constexpr int kSlot = KT * D * 2;           // bytes of a tile of keys or values
     static constexpr int kSlots = D == 64 ? 8 : 5;
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         // whatever was issued finishes before tensor memory is freed
         ptx::mma_commit(&drain);
         ptx::mbar_wait(&drain, 0, nullptr, p.status, kWaitLimitNs);
-    } else {
+    } else if (warp < T::kSoftWarps) {
         // ---------------------------------------------------------------------- softmax
         zero_padding(p, D, threadIdx.x, 32 * T::kSoftWarps);
         const int t = warp >> 2;  // row tile
@@ -308,58 +308,63 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
             const Segment<D> sg = segment_of<D>(p, r, g, b, off, x, st.x1);
             const PagedItem& it = sg.it;
             ++ordinal;
-            const bool live = i < sg.nq[t];
+            const bool live = i < (t ? sg.nq[1] : sg.nq[0]);
             const KeyRange keys = live ? query_keys(p, it.q, it.i0 + t * qt + i) : KeyRange{0, 0};
-            float m = -INFINITY, mc = 0.0f;  // running maximum (of raw or capped scores) and what is subtracted
+            // (selected, not indexed: t is a run-time value)
+            const int a_t = t ? sg.a[1] : sg.a[0], b_t = t ? sg.b[1] : sg.b[0];
+            float m = -INFINITY, mc = 0.0f;  // running maximum of the raw scores, and what is added in base 2
             float2 l2[2] = {make_float2(0, 0), make_float2(0, 0)};
             for (int j = sg.j0; j < sg.j1 && ok; ++j, ++n) {
-                if (j < sg.a[t] || j >= sg.b[t]) continue;
+                if (j < a_t || j >= b_t) continue;
                 const int place = NQ == 2 ? t : int(n & 1);
                 ok = wait(&s_full[place], seen[place]++);
                 if (!ok) break;
                 ptx::tc_fence_after();
                 const uint32_t s_col = tmem + lanes + uint32_t(place * KT);
-                float s[KT];
-#pragma unroll
-                for (int c = 0; c < KT; c += 32) ptx::tmem_ld_32(s_col + c, s + c);
-                ptx::tmem_ld_wait();
-                if constexpr (CAP) {
-#pragma unroll
-                    for (int e = 0; e < KT; ++e) s[e] = capped(__fmul_rn(s[e], p.scale2), p.cap2);
-                }
                 const int key0 = j * KT;
                 const bool edge = key0 < it.lo_all || key0 + KT > it.hi_all;
-                if (edge) {
-                    const int lo = keys.lo - key0, hi = keys.hi - key0;
+                const int lo = keys.lo - key0, hi = keys.hi - key0;
+                // 32 scores at a time, the next ones on their way; they are read twice, for the maximum and for the
+                // weights: a thread's 128 in registers would be spilled
+                float s[2][32];
+                auto masked = [&](float* v, int c) {
+                    if (edge) {
 #pragma unroll
-                    for (int e = 0; e < KT; ++e)
-                        if (e < lo || e >= hi) s[e] = -INFINITY;
+                        for (int e = 0; e < 32; ++e)
+                            if (c + e < lo || c + e >= hi) v[e] = -INFINITY;
+                    }
+                };
+                ptx::tmem_ld_32(s_col, s[0]);
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int c = 0; c < KT; c += 32) {
+                    float* v = s[(c / 32) & 1];
+                    ptx::tmem_ld_wait_32(v);
+                    ptx::tmem_ld_32(s_col + (c + 32 < KT ? c + 32 : 0), s[(c / 32 + 1) & 1]);
+                    masked(v, c);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) top[k] = max3(top[k], v[e + k], v[e + 4 + k]);
                 }
-                float top[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-                for (int e = 4; e + 7 < KT; e += 8)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) top[k] = max3(top[k], s[e + k], s[e + 4 + k]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], s[KT - 4 + k]);
+                // (the maximum is of raw scores: a cap keeps their order)
                 const float mt = fmaxf(max3(top[0], top[1], top[2]), top[3]);
-                const float unit = CAP ? 1.0f : p.scale2;  // base-2 units of a score
-                const bool grow = m == -INFINITY ? mt > m : (mt - m) * unit > 8.0f;
+                auto base2 = [&](float v) { return CAP ? capped(v * p.scale2, p.cap2) : v * p.scale2; };
+                const bool grow = m == -INFINITY ? mt > m : base2(mt) - base2(m) > 8.0f;
                 if (__any_sync(all, grow)) {
-                    const float m1 = grow ? mt : m;
-                    const float f = m1 == -INFINITY ? 1.0f : exp2_fast((m - m1) * unit);  // (-inf - x: 0)
-                    if (j > sg.a[t]) {
+                    const float f = !grow ? 1.0f : m == -INFINITY ? 0.0f : exp2_fast(base2(m) - base2(mt));
+                    if (j > a_t) {
                         ok = wait(&o_done[t], outs - 1);  // every product issued so far is in
                         if (!ok) break;
                         ptx::tc_fence_after();
-#pragma unroll
+#pragma unroll 1
                         for (int c = 0; c < D; c += 32) {
                             float o[32];
                             uint32_t w[32];
                             ptx::tmem_ld_32(o_col + c, o);
-                            ptx::tmem_ld_wait();
+                            ptx::tmem_ld_wait_32(o);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(grow ? o[e] * f : o[e]);
+                            for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(o[e] * f);
                             ptx::tmem_st_32(o_col + c, w);
                         }
                     }
@@ -367,23 +372,32 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                         const float2 ff = make_float2(f, f), z = make_float2(0, 0);
                         l2[0] = fma2(l2[0], ff, z);
                         l2[1] = fma2(l2[1], ff, z);
-                        m = m1;
-                        mc = -m * unit;
+                        m = mt;
+                        mc = -base2(m);
                     }
                 }
-                const float2 sc = make_float2(unit, unit), mm = make_float2(mc, mc);
+                const float2 sc = make_float2(CAP ? 1.0f : p.scale2, CAP ? 1.0f : p.scale2), mm = make_float2(mc, mc);
 #pragma unroll
-                for (int c = 0; c < KT; c += 64) {
-                    uint32_t w[32];
+                for (int c = 0; c < KT; c += 32) {
+                    float* v = s[(c / 32 + KT / 32) & 1];
+                    uint32_t w[16];
+                    ptx::tmem_ld_wait_32(v);
+                    if (c + 32 < KT) ptx::tmem_ld_32(s_col + c + 32, s[(c / 32 + KT / 32 + 1) & 1]);
+                    if constexpr (CAP) {
 #pragma unroll
-                    for (int e = 0; e < 64; e += 2) {
-                        float2 v = fma2(make_float2(s[c + e], s[c + e + 1]), sc, mm);
-                        v.x = exp2_fast(v.x);
-                        v.y = exp2_fast(v.y);
-                        l2[(e >> 1) & 1] = add2(l2[(e >> 1) & 1], v);
-                        w[e / 2] = pack_bf16x2(v.x, v.y);
+                        for (int e = 0; e < 32; ++e) v[e] = capped(__fmul_rn(v[e], p.scale2), p.cap2);
                     }
-                    ptx::tmem_st_32(s_col + c / 2, w);
+                    masked(v, c);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        float2 u = fma2(make_float2(v[e], v[e + 1]), sc, mm);
+                        u.x = exp2_fast(u.x);
+                        u.y = exp2_fast(u.y);
+                        l2[(e >> 1) & 1] = add2(l2[(e >> 1) & 1], u);
+                        w[e / 2] = pack_bf16x2(u.x, u.y);
+                    }
+                    // (columns whose scores this thread has read already)
+                    ptx::tmem_st_16(s_col + c / 2, w);
                 }
                 if (edge && t == (NQ == 2 && !(j >= sg.a[0] && j < sg.b[0]) ? 1 : 0)) {
                     // values behind the request's last key are anything; those hidden from some rows may not be multiplied
@@ -430,7 +444,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
             }
             if (!ok) break;
             // the segment's result: outputs, or this CTA's part of them
-            const bool has = sg.b[t] > sg.a[t];
+            const bool has = b_t > a_t;
             float l = (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
             if (has) {
                 ok = wait(&o_done[t], outs - 1);
@@ -447,7 +461,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
             const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
             const bool odd = has && *reinterpret_cast<volatile uint32_t*>(&odd_item) == ordinal;
             if (!whole && live) {
-                part[prow] = CAP ? m : m * p.scale2;
+                part[prow] = m == -INFINITY ? m : -mc;
                 part[kRows + prow] = l;
             }
 #pragma unroll 1
@@ -456,7 +470,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 __syncwarp();
                 if (has) {
                     ptx::tmem_ld_32(o_col + c, o);
-                    ptx::tmem_ld_wait();
+                    ptx::tmem_ld_wait_32(o);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = 0.0f;

@@ -346,6 +346,13 @@ __device__ __forceinline__ void tmem_ld_32(uint32_t taddr, float* v) {
         : "r"(taddr)
         : "memory");
 }
+// tcgen05.wait::ld, tied to the registers that a tmem_ld_32 fills: no use of them can move before it.
+__device__ __forceinline__ void tmem_ld_wait_32(float* v) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+                 :
+                 : "memory");
+}
 // 32 registers per thread into 32 consecutive 32-bit columns of the warp's 32 lanes.
 __device__ __forceinline__ void tmem_st_32(uint32_t taddr, const uint32_t* v) {
     asm volatile(
