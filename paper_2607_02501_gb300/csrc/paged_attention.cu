@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
     constexpr int KS = D / 16, NT = D / 8, NJ = kFewTile / 8 / WK, ROWS = kFewRows<WK>;
     constexpr bool QS = D == 256;  // queries stay in shared memory: their fragments would not fit the registers
     constexpr int kSub = kFewTile * 128;  // bytes of a 64-dim part of a tile
-    constexpr int64_t kSlot = int64_t(ROWS) * (D + 2);
+    using PL = PartLayout<D, ROWS>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full[T::kStages], empty[T::kStages];
     __shared__ int abort_flag;
@@ -73,9 +73,10 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
         ptx::prefetch_tmap(&p.k_map);
         ptx::prefetch_tmap(&p.v_map);
     }
+    __syncthreads();
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();  // lengths, queries and the new tokens' keys and values come from earlier launches
-    const PagedStretch st = paged_stretch<kFewTile, kFewThreads>(p);  // (its barriers also publish the mbarriers)
+    const PagedStretch st = paged_stretch<kFewTile, kFewThreads>(p);
 
     int r = st.r, g = st.g, b = st.b;
     uint32_t x = st.x0, off = st.off;
@@ -147,7 +148,7 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
     const int wrow = WK == 1 ? warp * 16 : 0, wkey = WK == 1 ? 0 : warp * 16;
     const uint32_t ring_u = ptx::smem_u32(ring);
     __nv_bfloat16* sq = reinterpret_cast<__nv_bfloat16*>(ring + T::kStages * T::kStage) + (QS ? wrow * T::kQPitch : 0);
-    PagedJoin join[2];
+    PagedJoin join0{}, join1{};
     int joins = 0;
 
     while (x < st.x1) {
@@ -371,96 +372,87 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
             }
         }
 
+        // WK = 4: the warps lay their results side by side where the last tile was (a lane's four values of n-tile n at
+        // [n][lane]: no two lanes meet in a bank), and each adds up a quarter of the n-tiles
+        constexpr int kMine = NT / WK;
+        const int n0 = WK == 1 ? 0 : warp * kMine;
         if constexpr (WK == 4) {
-            // warps 2 and 3 hand their results to 0 and 1, then 1 to 0, through the last tile's keys
             if (j1 > j0) {
                 const int s = (issued - 1) % T::kStages;
-                float* buf = reinterpret_cast<float*>(ring + s * T::kStage);  // [2][16][D]
+                float4* buf = reinterpret_cast<float4*>(ring + s * T::kStage);  // [warp][n-tile][lane]
+                bar();  // every warp is done with the keys and values
 #pragma unroll
-                for (int half = 2; half >= 1; half >>= 1) {
-                    bar();  // every warp is done with the keys, or with the buffer
-                    if (warp >= half && warp < 2 * half) {
-                        float* to = buf + (warp - half) * 16 * D;
+                for (int n = 0; n < NT; ++n) buf[(warp * NT + n) * 32 + lane] = make_float4(o[n][0], o[n][1], o[n][2], o[n][3]);
+                if (qc == 0) {
+                    warp_m[warp][quad] = mA;
+                    warp_l[warp][quad] = lA;
+                    warp_m[warp][quad + 8] = mB;
+                    warp_l[warp][quad + 8] = lB;
+                }
+                bar();
+                mA = mB = -INFINITY;
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            *reinterpret_cast<float2*>(to + quad * D + n * 8 + 2 * qc) = make_float2(o[n][0], o[n][1]);
-                            *reinterpret_cast<float2*>(to + (quad + 8) * D + n * 8 + 2 * qc) = make_float2(o[n][2], o[n][3]);
-                        }
-                        if (qc == 0) {
-                            warp_m[warp][quad] = mA;
-                            warp_l[warp][quad] = lA;
-                            warp_m[warp][quad + 8] = mB;
-                            warp_l[warp][quad + 8] = lB;
-                        }
-                    }
-                    bar();
-                    if (warp < half) {
-                        const float* from = buf + warp * 16 * D;
-                        const float yA = warp_m[warp + half][quad], yB = warp_m[warp + half][quad + 8];
-                        const float nA = fmaxf(mA, yA), nB = fmaxf(mB, yB);
-                        const float zA = nA == -INFINITY ? 0.0f : nA, zB = nB == -INFINITY ? 0.0f : nB;
-                        const float cA = exp2_fast(mA - zA), cB = exp2_fast(mB - zB);
-                        const float dA = exp2_fast(yA - zA), dB = exp2_fast(yB - zB);
-                        lA = fmaf(lA, cA, warp_l[warp + half][quad] * dA);
-                        lB = fmaf(lB, cB, warp_l[warp + half][quad + 8] * dB);
+                for (int w = 0; w < 4; ++w) {
+                    mA = fmaxf(mA, warp_m[w][quad]);
+                    mB = fmaxf(mB, warp_m[w][quad + 8]);
+                }
+                const float zA = mA == -INFINITY ? 0.0f : mA, zB = mB == -INFINITY ? 0.0f : mB;
+                lA = lB = 0.0f;
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            const float2 u = *reinterpret_cast<const float2*>(from + quad * D + n * 8 + 2 * qc);
-                            const float2 v = *reinterpret_cast<const float2*>(from + (quad + 8) * D + n * 8 + 2 * qc);
-                            o[n][0] = fmaf(o[n][0], cA, u.x * dA);
-                            o[n][1] = fmaf(o[n][1], cA, u.y * dA);
-                            o[n][2] = fmaf(o[n][2], cB, v.x * dB);
-                            o[n][3] = fmaf(o[n][3], cB, v.y * dB);
-                        }
-                        mA = nA;
-                        mB = nB;
+                for (int n = 0; n < kMine; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    // weight 0 of a warp without a finite score: its sums are 0, or NaN, which has to show
+                    const float wA = exp2_fast(warp_m[w][quad] - zA), wB = exp2_fast(warp_m[w][quad + 8] - zB);
+                    lA = fmaf(warp_l[w][quad], wA, lA);
+                    lB = fmaf(warp_l[w][quad + 8], wB, lB);
+#pragma unroll
+                    for (int n = 0; n < kMine; ++n) {
+                        const float4 u = buf[(w * NT + n0 + n) * 32 + lane];
+                        o[n][0] = fmaf(u.x, wA, o[n][0]);
+                        o[n][1] = fmaf(u.y, wA, o[n][1]);
+                        o[n][2] = fmaf(u.z, wB, o[n][2]);
+                        o[n][3] = fmaf(u.w, wB, o[n][3]);
                     }
                 }
                 ptx::fence_proxy_async_smem();  // before the next copy into this buffer
-                bar();
+                __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&empty[s]);
             }
         }
 
-        // every warp holds results (WK = 1), or warp 0 does
         const bool whole = off == 0 && take == uint32_t(it.units);
         if (whole) {
-            if (WK == 1 || warp == 0) {
-                const float iv = lA == 0.0f ? 0.0f : __fdiv_rn(1.0f, lA), iw = lB == 0.0f ? 0.0f : __fdiv_rn(1.0f, lB);
+            const float iv = lA == 0.0f ? 0.0f : __fdiv_rn(1.0f, lA), iw = lB == 0.0f ? 0.0f : __fdiv_rn(1.0f, lB);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const int c = n * 8 + 2 * qc;
-                    if (okA) *reinterpret_cast<uint32_t*>(p.O + offA + c) = pack_bf16x2(__fmul_rn(o[n][0], iv), __fmul_rn(o[n][1], iv));
-                    if (okB) *reinterpret_cast<uint32_t*>(p.O + offB + c) = pack_bf16x2(__fmul_rn(o[n][2], iw), __fmul_rn(o[n][3], iw));
-                }
+            for (int n = 0; n < kMine; ++n) {
+                const int c = (n0 + n) * 8 + 2 * qc;
+                if (okA) *reinterpret_cast<uint32_t*>(p.O + offA + c) = pack_bf16x2(__fmul_rn(o[n][0], iv), __fmul_rn(o[n][1], iv));
+                if (okB) *reinterpret_cast<uint32_t*>(p.O + offB + c) = pack_bf16x2(__fmul_rn(o[n][2], iw), __fmul_rn(o[n][3], iw));
             }
         } else {
             const uint32_t a = x - off;  // the item's first unit
             PagedJoin J{r, g, b, int(a / st.chunk), 0};
             J.count = int((a + uint32_t(it.units) - 1) / st.chunk) - J.first + 1;
-            if (WK == 1 || warp == 0) {
-                float* s = p.part + part_slot(int(blockIdx.x), J.first) * kSlot;
-                if (qc == 0) {
-                    if (okA) {
-                        s[rA] = mA;
-                        s[ROWS + rA] = lA;
-                    }
-                    if (okB) {
-                        s[rB] = mB;
-                        s[ROWS + rB] = lB;
-                    }
+            float* part = p.part + part_slot(int(blockIdx.x), J.first) * PL::kFloats;
+            if (qc == 0 && (WK == 1 || warp == 0)) {
+                if (okA) {
+                    part[rA] = mA;
+                    part[ROWS + rA] = lA;
                 }
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const int c = n * 8 + 2 * qc;
-                    if (okA) *reinterpret_cast<float2*>(s + 2 * ROWS + rA * D + c) = make_float2(o[n][0], o[n][1]);
-                    if (okB) *reinterpret_cast<float2*>(s + 2 * ROWS + rB * D + c) = make_float2(o[n][2], o[n][3]);
+                if (okB) {
+                    part[rB] = mB;
+                    part[ROWS + rB] = lB;
                 }
-                __threadfence();
-                __syncwarp();
-                if (lane == 0) atomicAdd(p.flags + J.first, 1u);
             }
-            join[joins++ & 1] = J;
+#pragma unroll
+            for (int n = 0; n < kMine; ++n) {
+                const int c = (n0 + n) * 8 + 2 * qc;
+                if (okA) *reinterpret_cast<float2*>(PL::value(part, rA, c)) = make_float2(o[n][0], o[n][1]);
+                if (okB) *reinterpret_cast<float2*>(PL::value(part, rB, c)) = make_float2(o[n][2], o[n][3]);
+            }
+            part_publish(p.flags + J.first, lane);
+            (joins++ == 0 ? join0 : join1) = J;
         }
         x += take;
         off = 0;
@@ -470,18 +462,17 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
     // Every CTA joins its share of the items that it has a part in, once all their parts are there. The CTAs of
     // the grid are all resident, and each publishes its parts before it waits.
     for (int k = 0; k < joins; ++k) {
-        const PagedJoin J = k == 0 ? join[0] : join[1];
-        constexpr uint32_t kHolders = WK == 1 ? kFewWarps : 1;
-        const uint32_t parts = kHolders * uint32_t(J.count);
+        const PagedJoin J = k == 0 ? join0 : join1;
+        const uint32_t parts = uint32_t(kFewWarps * J.count);
         bool ok = true;
         if (lane == 0) ok = join_wait(p.flags + J.first, parts, &abort_flag, p.status);
         ok = __shfl_sync(0xffffffffu, ok, 0);
         __syncwarp();
         if (ok) {
-            join_store<D, ROWS>(p, J, paged_req(p, J.r), int(blockIdx.x) - J.first, threadIdx.x, 32 * kFewWarps);
+            join_store<D, ROWS, 8, 1>(p, J, paged_req(p, J.r), int(blockIdx.x) - J.first, threadIdx.x, 32 * kFewWarps);
             __syncwarp();
             // the last warp to leave hands the flag back at zero
-            if (lane == 0 && atomicAdd(p.flags + J.first, 1u) == parts + uint32_t(kFewWarps * J.count) - 1)
+            if (lane == 0 && atomicAdd(p.flags + J.first, 1u) == 2 * parts - 1)
                 ptx::st_relaxed_gpu(p.flags + J.first, 0u);
         }
     }

@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
     using T = ManyTraits<D>;
     constexpr int NQ = T::NQ, KT = T::KT, S = T::kSlots;
     constexpr int kRows = 128 * NQ;
-    constexpr int64_t kPart = int64_t(kRows) * (D + 2);
+    using PL = PartLayout<D, kRows>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t kv_full[S], kv_empty[S], q_full, q_empty, s_full[2], p_ready[2], o_done[2], o_free[2], drain;
     __shared__ uint32_t tmem_slot, odd_item;
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         const uint32_t lanes = uint32_t(32 * (warp & 3)) << 16;
         const uint32_t o_col = tmem + lanes + uint32_t(T::kO + t * D);
         uint32_t n = 0, seen[2] = {0, 0}, outs = 0, ordinal = 0;
-        PagedJoin join[2];
+        PagedJoin join0{}, join1{};
         int joins = 0;
         bool ok = true;
         while (x < st.x1 && ok) {
@@ -455,7 +455,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
             const uint32_t a = x - off;  // the item's first unit
             PagedJoin J{r, g, b, int(a / st.chunk), 0};
             J.count = int((a + uint32_t(it.units) - 1) / st.chunk) - J.first + 1;
-            float* part = p.part + part_slot(int(blockIdx.x), J.first) * kPart;
+            float* part = p.part + part_slot(int(blockIdx.x), J.first) * PL::kFloats;
             const int prow = t * qt * p.G + row;  // rows of both tiles in order
             __nv_bfloat16* out = p.O + (int64_t(it.q.q0 + it.i0 + t * qt + i) * p.H + g * p.G + (row - i * p.G)) * D;
             const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
@@ -506,7 +506,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 } else {
 #pragma unroll
                     for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<float4*>(part + 2 * kRows + prow * D + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        *reinterpret_cast<float4*>(PL::value(part, prow, c + e)) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                 }
             }
             if (has) {
@@ -515,10 +515,8 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 if (lane == 0) ptx::mbar_arrive(&o_free[t]);
             }
             if (!whole) {
-                __threadfence();
-                __syncwarp();
-                if (lane == 0) atomicAdd(p.flags + J.first, 1u);
-                join[joins++ & 1] = J;
+                part_publish(p.flags + J.first, lane);
+                (joins++ == 0 ? join0 : join1) = J;
             }
             x += sg.take;
             off = 0;
@@ -527,13 +525,13 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         // Every CTA joins its share of the items that it has a part in, once all their parts are there. The CTAs of
         // the grid are all resident, and each publishes its parts before it waits.
         for (int k = 0; k < joins && ok; ++k) {
-            const PagedJoin J = k == 0 ? join[0] : join[1];
+            const PagedJoin J = k == 0 ? join0 : join1;
             const uint32_t parts = uint32_t(T::kSoftWarps * J.count);
             bool in = true;
             if (lane == 0) in = join_wait(p.flags + J.first, parts, &abort_flag, p.status);
             if (!__shfl_sync(all, in, 0)) break;
             __syncwarp();
-            join_store<D, kRows>(p, J, paged_req(p, J.r), int(blockIdx.x) - J.first, threadIdx.x, 32 * T::kSoftWarps);
+            join_store<D, kRows, 2, 4>(p, J, paged_req(p, J.r), int(blockIdx.x) - J.first, threadIdx.x, 32 * T::kSoftWarps);
             __syncwarp();
             // the last warp to leave hands the flag back at zero
             if (lane == 0 && atomicAdd(p.flags + J.first, 1u) == 2 * parts - 1) ptx::st_relaxed_gpu(p.flags + J.first, 0u);

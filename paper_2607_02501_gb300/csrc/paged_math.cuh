@@ -37,38 +37,95 @@ __device__ __forceinline__ void zero_padding(const PagedParams& p, int D, int ti
         o[i] = make_uint4(0, 0, 0, 0);
 }
 
-// Adds the partial results of an item that several CTAs shared and stores this CTA's part of its outputs.
-// A partial result is ROWS maxima, ROWS sums and [ROWS][D] values, in CTA order (deterministic).
+// A partial result of an item, ROWS x D values not yet divided by their row's sum: ROWS maxima, ROWS sums, then the
+// values as [D / 4][ROWS][4], so that neighbouring rows lie side by side.
 template <int D, int ROWS>
+struct PartLayout {
+    static constexpr int64_t kFloats = int64_t(ROWS) * (D + 2);
+    __device__ static float* value(float* part, int row, int c) { return part + 2 * ROWS + ((c >> 2) * ROWS + row) * 4 + (c & 3); }
+};
+
+// Publishes what the calling warp wrote of a partial result (to every thread of the device that acquires the flag).
+__device__ __forceinline__ void part_publish(uint32_t* flag, int lane) {
+    __syncwarp();
+    if (lane == 0) {
+        __threadfence();
+        atomicAdd(flag, 1u);
+    }
+}
+
+// Adds the partial results of an item that several CTAs shared, in CTA order (deterministic), and stores this CTA's
+// share of the rows. One round of loads covers PARTS partial results of VALS groups of four values: the loads, not the
+// arithmetic, take the time.
+template <int D, int ROWS, int PARTS, int VALS>
 __device__ __forceinline__ void join_store(const PagedParams& p, const PagedJoin& J, const PagedReq& q, int me, int tid, int nt) {
-    constexpr int64_t kSlot = int64_t(ROWS) * (D + 2);
+    using PL = PartLayout<D, ROWS>;
     const int i0 = J.b * p.QB, rows = min(p.QB, q.n - i0) * p.G;
-    for (int e = me * nt + tid; e < rows * (D / 4); e += J.count * nt) {
-        const int row = e / (D / 4), c = (e - row * (D / 4)) * 4;
-        float M = -INFINITY;
-#pragma unroll 8
-        for (int i = 0; i < J.count; ++i) M = fmaxf(M, __ldcg(p.part + part_slot(J.first + i, J.first) * kSlot + row));
-        const float m0 = M == -INFINITY ? 0.0f : M;
-        float L = 0.0f;
-        float4 o = make_float4(0, 0, 0, 0);
-#pragma unroll 8
-        for (int i = 0; i < J.count; ++i) {
-            const float* s = p.part + part_slot(J.first + i, J.first) * kSlot;
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(s + 2 * ROWS + row * D + c));
-            // weight 0 of a partial without a finite score: its sums are 0, or NaN, which has to show
-            const float w = exp2_fast(__ldcg(s + row) - m0);
-            L = fmaf(__ldcg(s + ROWS + row), w, L);
-            o.x = fmaf(v.x, w, o.x);
-            o.y = fmaf(v.y, w, o.y);
-            o.z = fmaf(v.z, w, o.z);
-            o.w = fmaf(v.w, w, o.w);
+    const int row0 = rows * me / J.count, mine = rows * (me + 1) / J.count - row0;
+    if (mine <= 0) return;
+    for (int e0 = tid; e0 < mine * (D / 4); e0 += nt * VALS) {
+        float M[VALS], L[VALS];
+        float4 o[VALS];
+#pragma unroll
+        for (int v = 0; v < VALS; ++v) {
+            M[v] = -INFINITY;
+            L[v] = 0.0f;
+            o[v] = make_float4(0, 0, 0, 0);
         }
-        const float inv = L == 0.0f ? 0.0f : __fdiv_rn(1.0f, L);
-        uint2 u;
-        u.x = pack_bf16x2(__fmul_rn(o.x, inv), __fmul_rn(o.y, inv));
-        u.y = pack_bf16x2(__fmul_rn(o.z, inv), __fmul_rn(o.w, inv));
-        const int64_t t = q.q0 + i0 + row / p.G;
-        *reinterpret_cast<uint2*>(p.O + (t * p.H + J.g * p.G + row % p.G) * D + c) = u;
+        for (int i0p = 0; i0p < J.count; i0p += PARTS) {
+            float m[VALS][PARTS], l[VALS][PARTS];
+            float4 x[VALS][PARTS];
+#pragma unroll
+            for (int v = 0; v < VALS; ++v) {
+                const int e = e0 + v * nt;
+                const int c4 = e / mine, row = row0 + e - c4 * mine;
+#pragma unroll
+                for (int k = 0; k < PARTS; ++k) {
+                    m[v][k] = -INFINITY;
+                    l[v][k] = 0.0f;
+                    x[v][k] = make_float4(0, 0, 0, 0);
+                    if (e < mine * (D / 4) && i0p + k < J.count) {
+                        float* part = p.part + part_slot(J.first + i0p + k, J.first) * PL::kFloats;
+                        m[v][k] = __ldcg(part + row);
+                        l[v][k] = __ldcg(part + ROWS + row);
+                        x[v][k] = __ldcg(reinterpret_cast<const float4*>(PL::value(part, row, c4 * 4)));
+                    }
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < VALS; ++v) {
+                float top = M[v];
+#pragma unroll
+                for (int k = 0; k < PARTS; ++k) top = fmaxf(top, m[v][k]);
+                const float z = top == -INFINITY ? 0.0f : top;
+                const float f = exp2_fast(M[v] - z);
+                M[v] = top;
+                L[v] *= f;
+                o[v] = make_float4(o[v].x * f, o[v].y * f, o[v].z * f, o[v].w * f);
+#pragma unroll
+                for (int k = 0; k < PARTS; ++k) {
+                    // weight 0 of a partial without a finite score: its sums are 0, or NaN, which has to show
+                    const float w = exp2_fast(m[v][k] - z);
+                    L[v] = fmaf(l[v][k], w, L[v]);
+                    o[v].x = fmaf(x[v][k].x, w, o[v].x);
+                    o[v].y = fmaf(x[v][k].y, w, o[v].y);
+                    o[v].z = fmaf(x[v][k].z, w, o[v].z);
+                    o[v].w = fmaf(x[v][k].w, w, o[v].w);
+                }
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < VALS; ++v) {
+            const int e = e0 + v * nt;
+            if (e >= mine * (D / 4)) continue;
+            const int c4 = e / mine, row = row0 + e - c4 * mine;
+            const float inv = L[v] == 0.0f ? 0.0f : __fdiv_rn(1.0f, L[v]);
+            uint2 u;
+            u.x = pack_bf16x2(__fmul_rn(o[v].x, inv), __fmul_rn(o[v].y, inv));
+            u.y = pack_bf16x2(__fmul_rn(o[v].z, inv), __fmul_rn(o[v].w, inv));
+            const int64_t t = q.q0 + i0 + row / p.G;
+            *reinterpret_cast<uint2*>(p.O + (t * p.H + J.g * p.G + row % p.G) * D + c4 * 4) = u;
+        }
     }
 }
 
