@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
     using PL = PartLayout<D, ROWS>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full[T::kStages], empty[T::kStages];
-    __shared__ int abort_flag;
+    __shared__ int abort_flag, joined;
     __shared__ float warp_m[kFewWarps][16], warp_l[kFewWarps][16];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -76,6 +76,11 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
     __syncthreads();
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();  // lengths, queries and the new tokens' keys and values come from earlier launches
+    if (p.n_req == 1 && warp == kFewWarps && lane * 32 < p.max_pages) {
+        // the only request's row of the table on its way to L1 while the stretch is found
+        uint32_t page;
+        asm volatile("ld.global.u32 %0, [%1];" : "=r"(page) : "l"(p.table + lane * 32));
+    }
     const PagedStretch st = paged_stretch<kFewTile, kFewThreads>(p);
 
     int r = st.r, g = st.g, b = st.b;
@@ -203,6 +208,8 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
             const uint32_t kb = ring_u + uint32_t(s * T::kStage), vb = kb + T::kStage / 2;
             const int key0 = (it.t0 + j) * kFewTile;
             const bool edge = key0 < it.lo_all || key0 + kFewTile > it.hi_all;
+            // whether it holds places behind the request's last key, and keys that some row does not see
+            const bool tail = key0 + kFewTile > it.q.L, hidden = key0 < it.lo_all || min(key0 + kFewTile, it.q.L) > it.hi_all;
 
             // S = Q K^T, the warp's keys in n-tiles of 8; one ldmatrix gives the fragments of two k-steps
             float sc[NJ][4];
@@ -300,6 +307,10 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
                     const float2 h = unpack_bf16x2(ah[i]);
                     al[i] = pack_bf16x2(__fsub_rn(src[i][0], h.x), __fsub_rn(src[i][1], h.y));
                 }
+                // (of the fragments' keys 2 qc, 2 qc + 1 and the same + 8, those that the request has)
+                const int left = it.q.L - (key0 + wkey + kk * 16 + 2 * qc);
+                const uint32_t in0 = (left > 0 ? 0x0000FFFFu : 0u) | (left > 1 ? 0xFFFF0000u : 0u);
+                const uint32_t in1 = (left > 8 ? 0x0000FFFFu : 0u) | (left > 9 ? 0xFFFF0000u : 0u);
                 const int kl = wkey + kk * 16 + (lane & 7) + ((lane >> 3) & 1) * 8;
                 const uint32_t vrow = vb + uint32_t(kl) * 128;
 #pragma unroll
@@ -308,28 +319,32 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
                         ldsm_x4_trans(vrow + (jj / 8) * kSub + ((((jj & 7) + 2 * i + (lane >> 4)) ^ (lane & 7)) << 4), bv[i]);
-                    if (edge) {
-                        // values behind the request's last key are anything; those hidden from some rows may not be
-                        // multiplied by their weights of 0 if they are not finite: such values are left
-                        // out here and added at the end for the rows that see them
+                    // values behind the request's last key are anything; those hidden from some rows may not be
+                    // multiplied by their weights of 0 if they are not finite: such values are left out here and
+                    // added at the end for the rows that see them
+                    if (tail) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int key = key0 + wkey + kk * 16 + (e & 1) * 8 + 2 * qc;
-                                uint32_t w = bv[i][e];
-                                if (key >= it.q.L) w &= 0xFFFF0000u;
-                                if (key + 1 >= it.q.L) w &= 0x0000FFFFu;
-                                if (not_finite(w)) {
-                                    w &= 0xFFFF0000u;
-                                    odd = true;
+                            for (int e = 0; e < 4; ++e) bv[i][e] &= e & 1 ? in1 : in0;
+                    }
+                    if (hidden) {
+                        uint32_t bad = 0;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) bad |= not_finite2(bv[i][e]);
+                        if (__any_sync(0xffffffffu, bad != 0)) {
+                            odd = true;
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const uint32_t w = not_finite2(bv[i][e]);
+                                    if (w & 0x8000u) bv[i][e] &= 0xFFFF0000u;
+                                    if (w & 0x80000000u) bv[i][e] &= 0x0000FFFFu;
                                 }
-                                if (not_finite(w >> 16)) {
-                                    w &= 0x0000FFFFu;
-                                    odd = true;
-                                }
-                                bv[i][e] = w;
-                            }
+                        }
                     }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) mma_16816(o[jj + i], ah, bv[i >> 1][2 * (i & 1)], bv[i >> 1][2 * (i & 1) + 1]);
@@ -349,7 +364,7 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
         if (__any_sync(0xffffffffu, odd)) {
             for (int key = (it.t0 + j0) * kFewTile; key < min((it.t0 + j1) * kFewTile, it.hi); ++key) {
                 const int in = key & (kFewTile - 1), key0 = key - in;
-                if (!(key0 < it.lo_all || key0 + kFewTile > it.hi_all)) continue;
+                if (!(key0 < it.lo_all || min(key0 + kFewTile, it.q.L) > it.hi_all)) continue;
                 if (WK > 1 && (in < wkey || in >= wkey + 16)) continue;
                 const int page = p.table[int64_t(r) * p.max_pages + (key >> p.page_shift)];
                 if (page < 0 || page >= p.n_pages) continue;
@@ -451,7 +466,8 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
                 if (okA) *reinterpret_cast<float2*>(PL::value(part, rA, c)) = make_float2(o[n][0], o[n][1]);
                 if (okB) *reinterpret_cast<float2*>(PL::value(part, rB, c)) = make_float2(o[n][2], o[n][3]);
             }
-            part_publish(p.flags + J.first, lane);
+            bar();
+            if (threadIdx.x == 0) part_publish(p.flags + J.first);
             (joins++ == 0 ? join0 : join1) = J;
         }
         x += take;
@@ -463,18 +479,11 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
     // the grid are all resident, and each publishes its parts before it waits.
     for (int k = 0; k < joins; ++k) {
         const PagedJoin J = k == 0 ? join0 : join1;
-        const uint32_t parts = uint32_t(kFewWarps * J.count);
-        bool ok = true;
-        if (lane == 0) ok = join_wait(p.flags + J.first, parts, &abort_flag, p.status);
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-        __syncwarp();
-        if (ok) {
-            join_store<D, ROWS, 8, 1>(p, J, paged_req(p, J.r), int(blockIdx.x) - J.first, threadIdx.x, 32 * kFewWarps);
-            __syncwarp();
-            // the last warp to leave hands the flag back at zero
-            if (lane == 0 && atomicAdd(p.flags + J.first, 1u) == 2 * parts - 1)
-                ptx::st_relaxed_gpu(p.flags + J.first, 0u);
-        }
+        if (threadIdx.x == 0) joined = part_wait(p.flags + J.first, J.count, &abort_flag, p.status);
+        bar();
+        const bool in = joined != 0;
+        if (in) join_store<D, ROWS, 16, 1>(p, J, paged_req(p, J.r), int(blockIdx.x) - J.first, threadIdx.x, 32 * kFewWarps);
+        bar();  // before the next item's answer
     }
 }
 
@@ -563,11 +572,11 @@ cudaError_t launch_few(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
     const cudaError_t e = few_resident<D, WK, CAP>(ctas);
     if (e != cudaSuccess) return e;
     p.QB = kFewRows<WK> / p.G;
-    p.min_units = 1;
     const uint32_t box = uint32_t(std::min<int64_t>(a.page_size, kFewTile));
     if (!encode_cache(&p.k_map, a.k_cache, a, box) || !encode_cache(&p.v_map, a.v_cache, a, box)) return cudaErrorInvalidValue;
     void* args[] = {&p};
-    const unsigned grid = unsigned(std::min(double(ctas), unit_bound(a, p.QB, kFewTile)));
+    const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, kFewTile))));
+    set_grid(p, grid, 1);
     return launch_serialised(reinterpret_cast<const void*>(paged_few_kernel<D, WK, CAP>), grid, kFewThreads, FewTraits<D>::kSmem, s, args);
 }
 

@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t kv_full[S], kv_empty[S], q_full, q_empty, s_full[2], p_ready[2], o_done[2], o_free[2], drain;
     __shared__ uint32_t tmem_slot, odd_item;
-    __shared__ int abort_flag;
+    __shared__ int abort_flag, joined;
     uint8_t* sq = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* ring = sq + NQ * T::kQTile;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -303,8 +303,10 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         uint32_t n = 0, seen[2] = {0, 0}, outs = 0, ordinal = 0;
         PagedJoin join0{}, join1{};
         int joins = 0;
-        bool ok = true;
-        while (x < st.x1 && ok) {
+        auto soft_bar = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * T::kSoftWarps) : "memory"); };
+        // A wait that gave up sets abort_flag; later waits then return at once, and the loops run to their end (the
+        // outputs are undefined then), so that every barrier still meets all its threads.
+        while (x < st.x1) {
             const Segment<D> sg = segment_of<D>(p, r, g, b, off, x, st.x1);
             const PagedItem& it = sg.it;
             ++ordinal;
@@ -314,11 +316,10 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
             const int a_t = t ? sg.a[1] : sg.a[0], b_t = t ? sg.b[1] : sg.b[0];
             float m = -INFINITY, mc = 0.0f;  // running maximum of the raw scores, and what is added in base 2
             float2 l2[2] = {make_float2(0, 0), make_float2(0, 0)};
-            for (int j = sg.j0; j < sg.j1 && ok; ++j, ++n) {
+            for (int j = sg.j0; j < sg.j1; ++j, ++n) {
                 if (j < a_t || j >= b_t) continue;
                 const int place = NQ == 2 ? t : int(n & 1);
-                ok = wait(&s_full[place], seen[place]++);
-                if (!ok) break;
+                wait(&s_full[place], seen[place]++);
                 ptx::tc_fence_after();
                 const uint32_t s_col = tmem + lanes + uint32_t(place * KT);
                 const int key0 = j * KT;
@@ -354,8 +355,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 if (__any_sync(all, grow)) {
                     const float f = !grow ? 1.0f : m == -INFINITY ? 0.0f : exp2_fast(base2(m) - base2(mt));
                     if (j > a_t) {
-                        ok = wait(&o_done[t], outs - 1);  // every product issued so far is in
-                        if (!ok) break;
+                        wait(&o_done[t], outs - 1);  // every product issued so far is in
                         ptx::tc_fence_after();
 #pragma unroll 1
                         for (int c = 0; c < D; c += 32) {
@@ -399,40 +399,44 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                     // (columns whose scores this thread has read already)
                     ptx::tmem_st_16(s_col + c / 2, w);
                 }
-                if (edge && t == (NQ == 2 && !(j >= sg.a[0] && j < sg.b[0]) ? 1 : 0)) {
+                const bool tail = key0 + KT > it.q.L, hidden = key0 < it.lo_all || min(key0 + KT, it.q.L) > it.hi_all;
+                if ((tail || hidden) && t == (NQ == 2 && !(j >= sg.a[0] && j < sg.b[0]) ? 1 : 0)) {
                     // values behind the request's last key are anything; those hidden from some rows may not be multiplied
                     // by their weights of 0 if they are not finite: such values leave the tile here and are added
                     // at the item's end for the rows that see them
                     const uint32_t pos = 2 * n + 1;
-                    ok = wait(&kv_full[slot_of(pos)], turn_of(pos));
-                    if (!ok) break;
-                    uint8_t* v = ring + slot_of(pos) * T::kSlot;
-                    bool odd = false;
-                    for (int e = row; e < KT * (D / 8); e += 128) {  // 16 bytes of one key, whatever their dims
-                        const int key = (e / 8) % KT;
-                        uint4* at = reinterpret_cast<uint4*>(v) + e;
-                        if (key0 + key >= it.q.L) {
-                            *at = make_uint4(0, 0, 0, 0);
-                            continue;
+                    wait(&kv_full[slot_of(pos)], turn_of(pos));
+                    uint4* v = reinterpret_cast<uint4*>(ring + slot_of(pos) * T::kSlot);
+                    uint32_t odd = 0;
+                    // 16 bytes of one key at a time, whatever their dims
+                    if (hidden) {
+#pragma unroll 4
+                        for (int e = row; e < KT * (D / 8); e += 128) {
+                            const uint4 u = v[e];
+                            odd |= not_finite2(u.x) | not_finite2(u.y) | not_finite2(u.z) | not_finite2(u.w);
                         }
-                        uint4 u = *at;
-                        uint32_t* h = reinterpret_cast<uint32_t*>(&u);
-                        bool hit = false;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            if (not_finite(h[k])) {
-                                h[k] &= 0xFFFF0000u;
-                                hit = true;
-                            }
-                            if (not_finite(h[k] >> 16)) {
-                                h[k] &= 0x0000FFFFu;
-                                hit = true;
-                            }
-                        }
-                        if (hit) *at = u;
-                        odd |= hit;
                     }
-                    if (odd) *reinterpret_cast<volatile uint32_t*>(&odd_item) = ordinal;
+                    if (tail)
+                        for (int e = row; e < KT * (D / 8); e += 128)
+                            if (key0 + (e / 8) % KT >= it.q.L) v[e] = make_uint4(0, 0, 0, 0);
+                    if (odd) {
+                        for (int e = row; e < KT * (D / 8); e += 128) {
+                            uint4 u = v[e];
+                            uint32_t* h = reinterpret_cast<uint32_t*>(&u);
+                            bool hit = false;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const uint32_t bad = not_finite2(h[k]);
+                                if (bad & 0x8000u) h[k] &= 0xFFFF0000u;
+                                if (bad & 0x80000000u) h[k] &= 0x0000FFFFu;
+                                hit |= bad != 0;
+                            }
+                            if (hit) {
+                                v[e] = u;
+                                *reinterpret_cast<volatile uint32_t*>(&odd_item) = ordinal;
+                            }
+                        }
+                    }
                     ptx::fence_proxy_async_smem();
                     __syncwarp();
                 }
@@ -442,13 +446,11 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 if (lane == 0) ptx::mbar_arrive(&p_ready[place]);
                 ++outs;
             }
-            if (!ok) break;
             // the segment's result: outputs, or this CTA's part of them
             const bool has = b_t > a_t;
             float l = (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
             if (has) {
-                ok = wait(&o_done[t], outs - 1);
-                if (!ok) break;
+                wait(&o_done[t], outs - 1);
                 ptx::tc_fence_after();
             }
             const bool whole = off == 0 && sg.take == uint32_t(it.units);
@@ -478,7 +480,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 if (odd) {
                     for (int key = max(keys.lo, sg.j0 * KT); key < min(keys.hi, sg.j1 * KT); ++key) {
                         const int key0 = key / KT * KT;
-                        if (!(key0 < it.lo_all || key0 + KT > it.hi_all)) continue;
+                        if (!(key0 < it.lo_all || min(key0 + KT, it.q.L) > it.hi_all)) continue;
                         const int page = p.table[int64_t(r) * p.max_pages + (key >> p.page_shift)];
                         if (page < 0 || page >= p.n_pages) continue;
                         const int64_t slot = (int64_t(page) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
@@ -515,7 +517,8 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 if (lane == 0) ptx::mbar_arrive(&o_free[t]);
             }
             if (!whole) {
-                part_publish(p.flags + J.first, lane);
+                soft_bar();
+                if (threadIdx.x == 0) part_publish(p.flags + J.first);
                 (joins++ == 0 ? join0 : join1) = J;
             }
             x += sg.take;
@@ -524,17 +527,13 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         }
         // Every CTA joins its share of the items that it has a part in, once all their parts are there. The CTAs of
         // the grid are all resident, and each publishes its parts before it waits.
-        for (int k = 0; k < joins && ok; ++k) {
+        for (int k = 0; k < joins; ++k) {
             const PagedJoin J = k == 0 ? join0 : join1;
-            const uint32_t parts = uint32_t(T::kSoftWarps * J.count);
-            bool in = true;
-            if (lane == 0) in = join_wait(p.flags + J.first, parts, &abort_flag, p.status);
-            if (!__shfl_sync(all, in, 0)) break;
-            __syncwarp();
-            join_store<D, kRows, 2, 4>(p, J, paged_req(p, J.r), int(blockIdx.x) - J.first, threadIdx.x, 32 * T::kSoftWarps);
-            __syncwarp();
-            // the last warp to leave hands the flag back at zero
-            if (lane == 0 && atomicAdd(p.flags + J.first, 1u) == 2 * parts - 1) ptx::st_relaxed_gpu(p.flags + J.first, 0u);
+            if (threadIdx.x == 0) joined = part_wait(p.flags + J.first, J.count, &abort_flag, p.status);
+            soft_bar();
+            const bool in = joined != 0;
+            if (in) join_store<D, kRows, 2, 4>(p, J, paged_req(p, J.r), int(blockIdx.x) - J.first, threadIdx.x, 32 * T::kSoftWarps);
+            soft_bar();  // before the next item's answer
         }
     }
     __syncwarp();
@@ -565,7 +564,6 @@ cudaError_t launch_many(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) 
     }
     const int tile = 128 / p.G;  // queries of a row tile
     p.QB = T::NQ * tile;
-    p.min_units = 1;
     const uint32_t box = uint32_t(std::min<int64_t>(a.page_size, T::KT));
     if (!encode_cache(&p.k_map, a.k_cache, a, box) || !encode_cache(&p.v_map, a.v_cache, a, box) ||
         !encode_queries(&p.q_map, a, uint32_t(p.G), uint32_t(tile)))
@@ -574,7 +572,8 @@ cudaError_t launch_many(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) 
     const int fit = int((EMB_PAGED_WORKSPACE - kPagedFlagBytes) / (2 * part));
     const int ctas = std::max(1, std::min({device_sm_count(), fit, int(kPagedFlagBytes / 4)}));
     void* args[] = {&p};
-    const unsigned grid = unsigned(std::min(double(ctas), unit_bound(a, p.QB, T::KT)));
+    const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, T::KT))));
+    set_grid(p, grid, 1);
     return launch_serialised(reinterpret_cast<const void*>(paged_many_kernel<D, CAP>), grid, T::kThreads, T::kSmem, s, args);
 }
 

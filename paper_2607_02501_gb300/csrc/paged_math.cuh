@@ -27,6 +27,8 @@ __device__ __forceinline__ float2 unpack_bf16x2(uint32_t w) {
     return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
 }
 __device__ __forceinline__ bool not_finite(uint32_t bf16_bits) { return (bf16_bits & 0x7F80u) == 0x7F80u; }
+// Bits 15 and 31: whether the low and the high bf16 of a word are not finite.
+__device__ __forceinline__ uint32_t not_finite2(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
 
 // Rows of O behind the last request's (padding of a recorded step): zeros.
 __device__ __forceinline__ void zero_padding(const PagedParams& p, int D, int tid, int nt) {
@@ -45,13 +47,16 @@ struct PartLayout {
     __device__ static float* value(float* part, int row, int c) { return part + 2 * ROWS + ((c >> 2) * ROWS + row) * 4 + (c & 3); }
 };
 
-// Publishes what the calling warp wrote of a partial result (to every thread of the device that acquires the flag).
-__device__ __forceinline__ void part_publish(uint32_t* flag, int lane) {
-    __syncwarp();
-    if (lane == 0) {
-        __threadfence();
-        atomicAdd(flag, 1u);
-    }
+// Counts this CTA's partial result in: one thread, after a barrier behind all that was written of it.
+__device__ __forceinline__ void part_publish(uint32_t* flag) {
+    __threadfence();
+    atomicAdd(flag, 1u);
+}
+// Waits for all partial results of an item: one thread. The last CTA to pass hands the flag back at zero.
+__device__ __forceinline__ bool part_wait(uint32_t* flag, int count, volatile int* abort, int* status) {
+    if (!join_wait(flag, uint32_t(count), abort, status)) return false;
+    if (atomicAdd(flag, 1u) == 2u * uint32_t(count) - 1u) ptx::st_relaxed_gpu(flag, 0u);
+    return true;
 }
 
 // Adds the partial results of an item that several CTAs shared, in CTA order (deterministic), and stores this CTA's

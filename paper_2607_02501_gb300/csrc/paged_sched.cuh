@@ -34,6 +34,7 @@ struct PagedParams {
     int64_t max_pages, n_tokens;
     int n_req, n_pages, page_shift, kv_limit, window;
     int H, Hk, G, QB, min_units;
+    uint32_t grid_inv;  // ceil(2^32 / grid)
     float scale2;  // scores are kept in base 2: scale * log2(e); capped, 2 log2(e) scale / cap
     float cap2;    // cap * log2(e)
 };
@@ -104,8 +105,10 @@ struct PagedStretch {
     uint32_t off;
 };
 
+// Units of a CTA's stretch: total / grid rounded up (or one more: any that is enough will do).
 __device__ __forceinline__ uint32_t stretch_chunk(const PagedParams& p, uint32_t total, uint32_t biggest) {
-    return max(max((total + gridDim.x - 1) / gridDim.x, (biggest + kMaxJoin - 2) / (kMaxJoin - 1)), uint32_t(p.min_units));
+    const uint32_t even = __umulhi(total + gridDim.x - 1, p.grid_inv);
+    return max(max(even, (biggest + kMaxJoin - 2) / (kMaxJoin - 1)), uint32_t(p.min_units));
 }
 
 // For up to 64 requests of up to four blocks: every warp by itself, two requests a lane, without a barrier (one
@@ -155,7 +158,7 @@ __device__ __forceinline__ bool paged_stretch_few(const PagedParams& p, PagedStr
         if (k) rem -= s[0] * uint32_t(p.Hk);
         const uint32_t per = k ? s[1] : s[0];
         st.r = 2 * lane + k;
-        st.g = int(rem / per);
+        st.g = p.Hk > 1 ? int(rem / per) : 0;
         rem -= uint32_t(st.g) * per;
         const PagedReq qk = k ? q[1] : q[0];
         for (;; ++st.b) {
@@ -316,6 +319,11 @@ bool encode_cache(CUtensorMap* m, const void* base, const PagedAttnArgs& a, uint
 bool encode_queries(CUtensorMap* m, const PagedAttnArgs& a, uint32_t heads, uint32_t tokens);
 // Units of work of a call, at most: every block of every request over a full block table.
 double unit_bound(const PagedAttnArgs& a, int qb, int kt);
+// What a launch of `grid` CTAs (two at least), with stretches of min_units at least, tells its kernel.
+inline void set_grid(PagedParams& p, unsigned grid, int min_units) {
+    p.min_units = min_units;
+    p.grid_inv = uint32_t(((uint64_t(1) << 32) + grid - 1) / grid);
+}
 // The tcgen05 kernel (paged_many.cu).
 cudaError_t launch_paged_many(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s);
 
