@@ -22,7 +22,10 @@ struct ManyTraits {
     static constexpr int NQ = D == 256 ? 1 : 2;        // row tiles of an item
     static constexpr int KT = D == 256 ? 64 : 128;     // keys of a tile
     static constexpr int kSoftWarps = 4 * NQ;
-    static constexpr int kThreads = 32 * (kSoftWarps + 2);  // and the MMA and the producer warp
+    // then the MMA and the producer warp; with two row tiles their warpgroup is filled up by two idle warps, so that
+    // it can hand registers to the softmax, a thread of which holds 128 scores: 384 threads x 168 at launch, then
+    // 2 x 128 x 208 + 128 x 88
+    static constexpr int kThreads = NQ == 2 ? 384 : 192;
     static constexpr int kQTile = 128 * D * 2;         // bytes of a row tile's queries
     static constexpr int kSlot = KT * D * 2;           // bytes of a tile of keys or values
     static constexpr int kSlots = D == 64 ? 8 : 5;
@@ -150,6 +153,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
 
     if (warp == T::kSoftWarps + 1) {
         // ---------------------------------------------------------------------- producer
+        if constexpr (NQ == 2) ptx::regs_down<88>();
         ptx::fence_proxy_async_global();  // (the cache and the queries were written by ordinary stores)
         const int page_size = 1 << p.page_shift, box = min(page_size, KT), n_box = KT / box;
         const int qt = p.QB / NQ;
@@ -220,6 +224,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         if (items > 0) ptx::mbar_wait(&q_full, (items - 1) & 1, nullptr, p.status, kWaitLimitNs);
     } else if (warp == T::kSoftWarps) {
         // ------------------------------------------------------------------------- MMAs
+        if constexpr (NQ == 2) ptx::regs_down<88>();
         const uint32_t idesc_qk = ptx::idesc_bf16_f32(128, KT), idesc_pv = ptx::idesc_bf16_f32(128, D) | ptx::kIdescMnMajorB;
         const uint32_t sq_u = ptx::smem_u32(sq), ring_u = ptx::smem_u32(ring);
         uint32_t n = 0, items = 0;
@@ -293,8 +298,11 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         // whatever was issued finishes before tensor memory is freed
         ptx::mma_commit(&drain);
         ptx::mbar_wait(&drain, 0, nullptr, p.status, kWaitLimitNs);
-    } else if (warp < T::kSoftWarps) {
+    } else if (warp >= T::kSoftWarps) {
+        if constexpr (NQ == 2) ptx::regs_down<88>();  // (idle)
+    } else {
         // ---------------------------------------------------------------------- softmax
+        if constexpr (NQ == 2) ptx::regs_up<208>();
         zero_padding(p, D, threadIdx.x, 32 * T::kSoftWarps);
         const int t = warp >> 2;  // row tile
         const int row = 32 * (warp & 3) + lane, qt = p.QB / NQ, i = row / p.G;
@@ -325,9 +333,9 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 const int key0 = j * KT;
                 const bool edge = key0 < it.lo_all || key0 + KT > it.hi_all;
                 const int lo = keys.lo - key0, hi = keys.hi - key0;
-                // 32 scores at a time, the next ones on their way; they are read twice, for the maximum and for the
-                // weights: a thread's 128 in registers would be spilled
-                float s[2][32];
+                float s[KT];
+#pragma unroll
+                for (int c = 0; c < KT; c += 32) ptx::tmem_ld_32(s_col + c, s + c);
                 auto masked = [&](float* v, int c) {
                     if (edge) {
 #pragma unroll
@@ -335,18 +343,15 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                             if (c + e < lo || c + e >= hi) v[e] = -INFINITY;
                     }
                 };
-                ptx::tmem_ld_32(s_col, s[0]);
                 float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int c = 0; c < KT; c += 32) {
-                    float* v = s[(c / 32) & 1];
-                    ptx::tmem_ld_wait_32(v);
-                    ptx::tmem_ld_32(s_col + (c + 32 < KT ? c + 32 : 0), s[(c / 32 + 1) & 1]);
-                    masked(v, c);
+                    ptx::tmem_ld_wait_32(s + c);
+                    masked(s + c, c);
 #pragma unroll
                     for (int e = 0; e < 32; e += 8)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) top[k] = max3(top[k], v[e + k], v[e + 4 + k]);
+                        for (int k = 0; k < 4; ++k) top[k] = max3(top[k], s[c + e + k], s[c + e + 4 + k]);
                 }
                 // (the maximum is of raw scores: a cap keeps their order)
                 const float mt = fmaxf(max3(top[0], top[1], top[2]), top[3]);
@@ -379,24 +384,18 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 const float2 sc = make_float2(CAP ? 1.0f : p.scale2, CAP ? 1.0f : p.scale2), mm = make_float2(mc, mc);
 #pragma unroll
                 for (int c = 0; c < KT; c += 32) {
-                    float* v = s[(c / 32 + KT / 32) & 1];
+                    const float* v = s + c;
                     uint32_t w[16];
-                    ptx::tmem_ld_wait_32(v);
-                    if (c + 32 < KT) ptx::tmem_ld_32(s_col + c + 32, s[(c / 32 + KT / 32 + 1) & 1]);
-                    if constexpr (CAP) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] = capped(__fmul_rn(v[e], p.scale2), p.cap2);
-                    }
-                    masked(v, c);
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
-                        float2 u = fma2(make_float2(v[e], v[e + 1]), sc, mm);
+                        float2 u = make_float2(v[e], v[e + 1]);
+                        if constexpr (CAP) u = add2(make_float2(base2(u.x), base2(u.y)), mm);
+                        else u = fma2(u, sc, mm);
                         u.x = exp2_fast(u.x);
                         u.y = exp2_fast(u.y);
                         l2[(e >> 1) & 1] = add2(l2[(e >> 1) & 1], u);
                         w[e / 2] = pack_bf16x2(u.x, u.y);
                     }
-                    // (columns whose scores this thread has read already)
                     ptx::tmem_st_16(s_col + c / 2, w);
                 }
                 const bool tail = key0 + KT > it.q.L, hidden = key0 < it.lo_all || min(key0 + KT, it.q.L) > it.hi_all;

@@ -232,6 +232,17 @@ __device__ __forceinline__ float4 ld_dsmem_f32x4(uint32_t caddr) {
     return v;
 }
 
+// Registers of every thread of the calling warpgroup from here on (all its warps call it). The block's warpgroups
+// together may not ask for more than the block was launched with.
+template <int N>
+__device__ __forceinline__ void regs_up() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_down() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
 // -------------------------------------------------------------------- tcgen05
 // tcgen05.alloc blocks until ncols columns are free on the SM; it is the one wait in the
 // library without a time limit. It cannot block here because no two CTAs that allocate
