@@ -59,6 +59,7 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full[T::kStages], empty[T::kStages];
     __shared__ int abort_flag, joined;
+    __shared__ PagedJoin cut[2];
     __shared__ float warp_m[kFewWarps][16], warp_l[kFewWarps][16];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -153,7 +154,6 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
     const int wrow = WK == 1 ? warp * 16 : 0, wkey = WK == 1 ? 0 : warp * 16;
     const uint32_t ring_u = ptx::smem_u32(ring);
     __nv_bfloat16* sq = reinterpret_cast<__nv_bfloat16*>(ring + T::kStages * T::kStage) + (QS ? wrow * T::kQPitch : 0);
-    PagedJoin join0{}, join1{};
     int joins = 0;
 
     while (x < st.x1) {
@@ -468,7 +468,8 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
             }
             bar();
             if (threadIdx.x == 0) part_publish(p.flags + J.first);
-            (joins++ == 0 ? join0 : join1) = J;
+            if (threadIdx.x == 0) cut[joins] = J;
+            ++joins;
         }
         x += take;
         off = 0;
@@ -477,8 +478,9 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
 
     // Every CTA joins its share of the items that it has a part in, once all their parts are there. The CTAs of
     // the grid are all resident, and each publishes its parts before it waits.
+    if (joins > 0) bar();
     for (int k = 0; k < joins; ++k) {
-        const PagedJoin J = k == 0 ? join0 : join1;
+        const PagedJoin J = cut[k];
         if (threadIdx.x == 0) joined = part_wait(p.flags + J.first, J.count, &abort_flag, p.status);
         bar();
         const bool in = joined != 0;
@@ -576,7 +578,7 @@ cudaError_t launch_few(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
     if (!encode_cache(&p.k_map, a.k_cache, a, box) || !encode_cache(&p.v_map, a.v_cache, a, box)) return cudaErrorInvalidValue;
     void* args[] = {&p};
     const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, kFewTile))));
-    set_grid(p, grid, 1);
+    set_grid(p, grid, 3);
     return launch_serialised(reinterpret_cast<const void*>(paged_few_kernel<D, WK, CAP>), grid, kFewThreads, FewTraits<D>::kSmem, s, args);
 }
 
@@ -606,7 +608,7 @@ cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s) {
     p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + kPagedFlagBytes);
     p.status = a.status;
     p.max_pages = a.max_pages;
-    p.n_tokens = a.n_tokens;
+    p.n_tokens = int(a.n_tokens);
     p.n_req = int(a.n_req);
     p.n_pages = int(a.n_pages);
     while ((int64_t(1) << p.page_shift) < a.page_size) ++p.page_shift;

@@ -24,7 +24,7 @@ struct ManyTraits {
     static constexpr int kSoftWarps = 4 * NQ;
     // then the MMA and the producer warp; with two row tiles their warpgroup is filled up by two idle warps, so that
     // it can hand registers to the softmax, a thread of which holds 128 scores: 384 threads x 168 at launch, then
-    // 2 x 128 x 208 + 128 x 88
+    // 2 x 128 x 216 + 128 x 72
     static constexpr int kThreads = NQ == 2 ? 384 : 192;
     static constexpr int kQTile = 128 * D * 2;         // bytes of a row tile's queries
     static constexpr int kSlot = KT * D * 2;           // bytes of a tile of keys or values
@@ -104,6 +104,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
     __shared__ uint64_t kv_full[S], kv_empty[S], q_full, q_empty, s_full[2], p_ready[2], o_done[2], o_free[2], drain;
     __shared__ uint32_t tmem_slot, odd_item;
     __shared__ int abort_flag, joined;
+    __shared__ PagedJoin cut[2];
     uint8_t* sq = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* ring = sq + NQ * T::kQTile;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -153,7 +154,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
 
     if (warp == T::kSoftWarps + 1) {
         // ---------------------------------------------------------------------- producer
-        if constexpr (NQ == 2) ptx::regs_down<88>();
+        if constexpr (NQ == 2) ptx::regs_down<72>();
         ptx::fence_proxy_async_global();  // (the cache and the queries were written by ordinary stores)
         const int page_size = 1 << p.page_shift, box = min(page_size, KT), n_box = KT / box;
         const int qt = p.QB / NQ;
@@ -224,27 +225,29 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         if (items > 0) ptx::mbar_wait(&q_full, (items - 1) & 1, nullptr, p.status, kWaitLimitNs);
     } else if (warp == T::kSoftWarps) {
         // ------------------------------------------------------------------------- MMAs
-        if constexpr (NQ == 2) ptx::regs_down<88>();
+        if constexpr (NQ == 2) ptx::regs_down<72>();
         const uint32_t idesc_qk = ptx::idesc_bf16_f32(128, KT), idesc_pv = ptx::idesc_bf16_f32(128, D) | ptx::kIdescMnMajorB;
         const uint32_t sq_u = ptx::smem_u32(sq), ring_u = ptx::smem_u32(ring);
         uint32_t n = 0, items = 0;
         uint32_t scores[2] = {0, 0}, owned[2] = {0, 0};  // score tiles by place, items with outputs by row tile
         bool ok = true;
+        // (operands in a form that the compiler knows to be uniform: see ptx::elect_one)
         auto qk = [&](int t, int place, uint32_t pos) {  // S[place] = Q[t] K^T
-            const uint32_t k = ring_u + uint32_t(slot_of(pos) * T::kSlot);
+            const uint32_t k = ptx::warp_uniform(ring_u + uint32_t(slot_of(pos) * T::kSlot));
+            const uint32_t d = ptx::warp_uniform(tmem + uint32_t(place * KT));
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks)
-                ptx::mma_bf16_ss(tmem + uint32_t(place * KT), ptx::smem_desc_sw128(sq_u + t * T::kQTile + (ks / 4) * 16384) + 2 * (ks & 3),
+                ptx::mma_bf16_ss(d, ptx::smem_desc_sw128(sq_u + t * T::kQTile + (ks / 4) * 16384) + 2 * (ks & 3),
                                  ptx::smem_desc_sw128(k + (ks / 4) * T::kSub) + 2 * (ks & 3), idesc_qk, ks != 0);
             ptx::mma_commit(&s_full[place]);
         };
         auto pv = [&](int t, int place, uint32_t pos, bool first) {  // O[t] (+)= P[place] V
-            const uint32_t v = ring_u + uint32_t(slot_of(pos) * T::kSlot);
-            const uint64_t desc = ptx::smem_desc_mn_sw128(v, T::kSub);
+            const uint64_t desc = ptx::smem_desc_mn_sw128(ptx::warp_uniform(ring_u + uint32_t(slot_of(pos) * T::kSlot)), T::kSub);
+            const uint32_t d = ptx::warp_uniform(tmem + uint32_t(T::kO + t * D)), a = ptx::warp_uniform(tmem + uint32_t(place * KT));
+            const uint32_t more = ptx::warp_uniform(first ? 0u : 1u);
 #pragma unroll
             for (int kk = 0; kk < KT / 16; ++kk)
-                ptx::mma_bf16_ta(tmem + uint32_t(T::kO + t * D), tmem + uint32_t(place * KT + 8 * kk), desc + uint32_t(kk * 2048 / 16),
-                                 idesc_pv, !first || kk != 0);
+                ptx::mma_bf16_ta(d, a + uint32_t(8 * kk), desc + uint32_t(kk * 2048 / 16), idesc_pv, kk == 0 ? more : 1u);
             ptx::mma_commit(&o_done[t]);
         };
         while (x < st.x1 && ok) {
@@ -299,17 +302,16 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         ptx::mma_commit(&drain);
         ptx::mbar_wait(&drain, 0, nullptr, p.status, kWaitLimitNs);
     } else if (warp >= T::kSoftWarps) {
-        if constexpr (NQ == 2) ptx::regs_down<88>();  // (idle)
+        if constexpr (NQ == 2) ptx::regs_down<72>();  // (idle)
     } else {
         // ---------------------------------------------------------------------- softmax
-        if constexpr (NQ == 2) ptx::regs_up<208>();
+        if constexpr (NQ == 2) ptx::regs_up<216>();
         zero_padding(p, D, threadIdx.x, 32 * T::kSoftWarps);
         const int t = warp >> 2;  // row tile
         const int row = 32 * (warp & 3) + lane, qt = p.QB / NQ, i = row / p.G;
         const uint32_t lanes = uint32_t(32 * (warp & 3)) << 16;
         const uint32_t o_col = tmem + lanes + uint32_t(T::kO + t * D);
         uint32_t n = 0, seen[2] = {0, 0}, outs = 0, ordinal = 0;
-        PagedJoin join0{}, join1{};
         int joins = 0;
         auto soft_bar = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * T::kSoftWarps) : "memory"); };
         // A wait that gave up sets abort_flag; later waits then return at once, and the loops run to their end (the
@@ -333,21 +335,27 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 const int key0 = j * KT;
                 const bool edge = key0 < it.lo_all || key0 + KT > it.hi_all;
                 const int lo = keys.lo - key0, hi = keys.hi - key0;
+                if (edge) {
+                    // scores that the row does not see, in tensor memory: rolled up and away from the path of most tiles
+#pragma unroll 1
+                    for (int c = 0; c < KT; c += 32) {
+                        float v[32];
+                        uint32_t w[32];
+                        ptx::tmem_ld_32(s_col + c, v);
+                        ptx::tmem_ld_wait_32(v);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(c + e < lo || c + e >= hi ? -INFINITY : v[e]);
+                        ptx::tmem_st_32(s_col + c, w);
+                    }
+                    ptx::tmem_st_wait();
+                }
                 float s[KT];
 #pragma unroll
                 for (int c = 0; c < KT; c += 32) ptx::tmem_ld_32(s_col + c, s + c);
-                auto masked = [&](float* v, int c) {
-                    if (edge) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (c + e < lo || c + e >= hi) v[e] = -INFINITY;
-                    }
-                };
                 float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int c = 0; c < KT; c += 32) {
                     ptx::tmem_ld_wait_32(s + c);
-                    masked(s + c, c);
 #pragma unroll
                     for (int e = 0; e < 32; e += 8)
 #pragma unroll
@@ -439,6 +447,9 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                     ptx::fence_proxy_async_smem();
                     __syncwarp();
                 }
+                // every phase of o_done is waited for, so that a wait cannot take the one before the last for the last:
+                // with two score places the last scores do not tell that the product before theirs is in
+                if (NQ == 1 && j > a_t) wait(&o_done[t], outs - 1);
                 ptx::tmem_st_wait();
                 ptx::tc_fence_before();
                 __syncwarp();
@@ -518,7 +529,8 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
             if (!whole) {
                 soft_bar();
                 if (threadIdx.x == 0) part_publish(p.flags + J.first);
-                (joins++ == 0 ? join0 : join1) = J;
+                if (threadIdx.x == 0) cut[joins] = J;
+                ++joins;
             }
             x += sg.take;
             off = 0;
@@ -526,12 +538,13 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         }
         // Every CTA joins its share of the items that it has a part in, once all their parts are there. The CTAs of
         // the grid are all resident, and each publishes its parts before it waits.
+        if (joins > 0) soft_bar();
         for (int k = 0; k < joins; ++k) {
-            const PagedJoin J = k == 0 ? join0 : join1;
+            const PagedJoin J = cut[k];
             if (threadIdx.x == 0) joined = part_wait(p.flags + J.first, J.count, &abort_flag, p.status);
             soft_bar();
             const bool in = joined != 0;
-            if (in) join_store<D, kRows, 2, 4>(p, J, paged_req(p, J.r), int(blockIdx.x) - J.first, threadIdx.x, 32 * T::kSoftWarps);
+            if (in) join_store<D, kRows, 4, 2>(p, J, paged_req(p, J.r), int(blockIdx.x) - J.first, threadIdx.x, 32 * T::kSoftWarps);
             soft_bar();  // before the next item's answer
         }
     }
@@ -572,7 +585,8 @@ cudaError_t launch_many(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) 
     const int ctas = std::max(1, std::min({device_sm_count(), fit, int(kPagedFlagBytes / 4)}));
     void* args[] = {&p};
     const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, T::KT))));
-    set_grid(p, grid, 1);
+    set_grid(p, grid, D == 256 ? 8 : 4);
+
     return launch_serialised(reinterpret_cast<const void*>(paged_many_kernel<D, CAP>), grid, T::kThreads, T::kSmem, s, args);
 }
 

@@ -32,10 +32,9 @@ __device__ __forceinline__ uint32_t not_finite2(uint32_t w) { return ((w & 0x7F8
 
 // Rows of O behind the last request's (padding of a recorded step): zeros.
 __device__ __forceinline__ void zero_padding(const PagedParams& p, int D, int tid, int nt) {
-    const int64_t used = min(max(int64_t(p.q_start[p.n_req]), int64_t(0)), p.n_tokens);
-    const int64_t row16 = int64_t(p.H) * D / 8;
+    const int64_t used = min(max(p.q_start[p.n_req], 0), p.n_tokens), row16 = int64_t(p.H) * D / 8;
     uint4* o = reinterpret_cast<uint4*>(p.O);
-    for (int64_t i = used * row16 + int64_t(blockIdx.x) * nt + tid; i < p.n_tokens * row16; i += int64_t(gridDim.x) * nt)
+    for (int64_t i = used * row16 + int64_t(blockIdx.x) * nt + tid; i < int64_t(p.n_tokens) * row16; i += int64_t(gridDim.x) * nt)
         o[i] = make_uint4(0, 0, 0, 0);
 }
 
