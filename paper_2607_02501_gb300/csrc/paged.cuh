@@ -34,8 +34,9 @@ struct QkArgs {
     uint16_t* q_out;
     uint16_t* k_cache;
     uint16_t* v_cache;
-    int64_t q_stride, k_stride, v_stride, pos_stride, n_tokens, n_heads, n_kv_heads, head_dim, rot_dim, n_slots;
+    int64_t q_stride, k_stride, v_stride, pos_stride, n_tokens, n_heads, n_kv_heads, head_dim, rot_dim, n_slots, n_axes;
     float eps, base;
+    int* status;
 };
 cudaError_t launch_qk_norm_rope(const QkArgs& a, cudaStream_t s);
 

@@ -170,6 +170,9 @@ emb_status emb_qk_norm_rope(const uint16_t* q, int64_t q_stride, const uint16_t*
     a.n_slots = n_pages * page_size;
     a.eps = eps;
     a.base = base;
+    a.n_axes = n_axes;
+    a.status = device_words(false);
+    if (!a.status) return EMB_ECUDA;
     return from_cuda(launch_qk_norm_rope(a, stream_of(stream)));
 }
 

@@ -5,6 +5,8 @@
 // Both kernels are launched with programmatic stream serialisation and read device memory only
 // after griddepcontrol.wait, with ordinary loads.
 #include <algorithm>
+#include <cstring>
+#include <mutex>
 
 #include "paged.cuh"
 #include "rotate.cuh"
@@ -166,15 +168,26 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const __grid_
 }
 
 // ------------------------------------------------------------------ norm, rotation, cache write
-// A CTA takes a few tokens: it forms their cosines and sines once, in shared memory, for all heads
-// (a token's 40 heads share 64 of them), while the first rows are on their way. A row (one head of one token)
-// belongs to 2^n lanes, each of which holds VEC elements of the row's first half and the VEC they are paired with, so
-// the rotation stays within the thread and the sum of squares takes n shuffles. Elements behind the rotated ones
-// are paired likewise and turned by nothing. Rows of values are copied the same way. HBM bounds it: every
-// element is read and written once.
-constexpr int kQkThreads = 256;
+// HBM bounds it: every element is read and written once. CTAs stay and take items in turn, an item being a run of rows
+// (heads of queries, then of keys, then of values) of a few tokens. A ring of three items in shared memory is filled by
+// bulk copies and written out by bulk copies, both by a warp of their own, so what is on its way needs no registers and
+// holds nobody up; values pass through untouched. In between four warps turn the rows in place: 2^n lanes to a row, each with VEC elements of the first half and
+// the VEC that they are paired with, so the rotation stays within the thread and the sum of squares takes n shuffles.
+// Elements behind the rotated ones are paired likewise and turned by nothing. A token's cosines and sines are formed once
+// for all heads.
+// Angles are counted in turns: the host passes frequency / 2 pi as two floats, position times that is formed with one
+// exact FMA residual, and its fraction goes to the hardware's sine and cosine, whose error in +-pi is below 2^-21.
+// Measured (us): 16000 tokens of 10 heads of 256 (164 MB) 30.9, 78 % of the measured copy rate; 816 of 48 heads of 128
+// (20 MB, three axes, norms) 7.5; one token of 10 heads of 128 2.8. Rows through registers, angles by sincosf for every CTA
+// of a few tokens took 72, 11 and 2.8; with the copies issued by one of the computing warps 43 and 8.7; CTAs of eight
+// computing warps and 24 KB items, two per SM, 33.5, 7.9 and 2.8.
+constexpr int kQkWarps = 4;  // that compute; one more copies
+constexpr int kQkCompute = 32 * kQkWarps, kQkThreads = kQkCompute + 32;
 constexpr int kQkMaxPairs = 128;
-constexpr int kQkMaxTokens = 16;  // of a CTA
+constexpr int kQkMaxTokens = 16;  // of an item
+constexpr int kQkStages = 3;
+constexpr int kQkItemBytes = 12 * 1024;  // of rows, at most
+constexpr int kQkCtas = 4;               // per SM
 
 struct QkParams {
     const __nv_bfloat16* q;
@@ -187,141 +200,300 @@ struct QkParams {
     __nv_bfloat16* q_out;
     __nv_bfloat16* k_cache;
     __nv_bfloat16* v_cache;
-    int64_t q_stride, k_stride, v_stride, pos_stride, n_tokens, n_slots;
-    int H, Hk, d, half, tokens;  // half: rotated pairs of a head; tokens of a CTA
-    int log_lanes;               // a row's lanes are 2^log_lanes
+    int64_t q_stride, k_stride, v_stride, pos_stride, n_tokens, n_slots, items;
+    int H, Hk, d, half;        // half: rotated pairs of a head
+    int tokens, run, runs;     // an item's tokens and rows of a token; runs of a token
+    int axes, log_lanes;       // a row's lanes are 2^log_lanes
     float eps;
-    float inv_hi[kQkMaxPairs], inv_lo[kQkMaxPairs];
-    uint8_t axis[kQkMaxPairs];
+    alignas(16) float turn_hi[kQkMaxPairs];  // frequency / 2 pi
+    alignas(16) float turn_lo[kQkMaxPairs];
+    alignas(16) uint8_t axis[kQkMaxPairs];
 };
+constexpr int kQkHeadBytes = 64 + kQkStages * kQkMaxTokens * (8 + 4 * 4) + 2 * kQkMaxPairs * 4 + kQkMaxPairs;  // 16-byte multiple
 
 template <int VEC>
 struct alignas(2 * VEC) QkVec {
     __nv_bfloat16 v[VEC];
 };
 
-template <int VEC, int ROWS>  // ROWS: rows that a thread has in flight at once
-__global__ void __launch_bounds__(kQkThreads) qk_norm_rope_kernel(const __grid_constant__ QkParams p) {
-    extern __shared__ __align__(16) float sm[];
-    float* gam = sm;                        // [2][d] of queries and keys
-    float* cosv = gam + 2 * p.d;            // [tokens][half]
-    float* sinv = cosv + p.tokens * p.half;
-    float* fhi = sinv + p.tokens * p.half;  // [half]
-    float* flo = fhi + p.half;
-    int* axis = reinterpret_cast<int*>(flo + p.half);
-    const int tid = threadIdx.x;
-    ptx::griddep_launch_dependents();
-    for (int i = tid; i < p.half; i += kQkThreads) {
-        fhi[i] = p.inv_hi[i];
-        flo[i] = p.inv_lo[i];
-        axis[i] = p.axis[i];
+// The fraction of at * (hi + lo) turns where the residual is turns by itself (far positions, a base below one). Called,
+// not inlined: as predicated instructions the few fp64 operations cost every position.
+__device__ __noinline__ float far_turn(int32_t at, float hi, float lo) {
+    const double t = double(at) * (double(hi) + double(lo));
+    return float(t - rint(t));
+}
+// Cosine and sine of 2 pi * at * (hi + lo).
+__device__ __forceinline__ void turn_sincos(int32_t at, float hi, float lo, float& c, float& s) {
+    const float pos = float(at), T = __fmul_rn(pos, hi);
+    float frac;
+    if (fabsf(T) < 1048576.0f && fabsf(pos) < 16777216.0f) {
+        frac = (T - rintf(T)) + fmaf(pos, lo, fmaf(pos, hi, -T));
+    } else {
+        frac = far_turn(at, hi, lo);
     }
+    __sincosf(frac * 6.283185307179586f, &s, &c);
+}
+
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "mul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 pair_of(const QkVec<2>& v) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(&v);
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+// VEC numbers of unit u, kept as [VEC / 4][units][4]: neighbouring lanes' loads lie side by side.
+template <int VEC>
+__device__ __forceinline__ void load_unit(const float* p, int u, int units, float2 (&v)[VEC / 2]) {
+#pragma unroll
+    for (int e = 0; e < VEC; e += 4)
+        *reinterpret_cast<float4*>(&v[e / 2]) = *reinterpret_cast<const float4*>(p + ((e >> 2) * units + u) * 4);
+}
+template <int VEC>
+__device__ __forceinline__ int unit_place(int i, int units) {  // of number i in that order
+    const int u = i / VEC, e = i % VEC;
+    return ((e >> 2) * units + u) * 4 + (e & 3);
+}
+
+template <int VEC>
+__global__ void __launch_bounds__(kQkThreads, kQkCtas) qk_norm_rope_kernel(const __grid_constant__ QkParams p, int* status) {
+    extern __shared__ __align__(128) uint8_t sm[];
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm);                               // [stages]
+    uint64_t* done = full + kQkStages;                                              // [stages]
+    int* abort_flag = reinterpret_cast<int*>(done + kQkStages);
+    int64_t* slot_of = reinterpret_cast<int64_t*>(sm + 64);                         // [stages][tokens]
+    int32_t* pos_of = reinterpret_cast<int32_t*>(slot_of + kQkStages * kQkMaxTokens);  // [stages][4][tokens]
+    float* turn_hi = reinterpret_cast<float*>(pos_of + kQkStages * 4 * kQkMaxTokens);
+    float* turn_lo = turn_hi + kQkMaxPairs;
+    uint8_t* axis_of = reinterpret_cast<uint8_t*>(turn_lo + kQkMaxPairs);
+    float* gam = reinterpret_cast<float*>(sm + kQkHeadBytes);                       // [q, k][first, second of the pairs][d / 2]
+    float* cs = gam + 2 * p.d;                                                      // [2][cos, sin][tokens][half]
+    const int cs_size = p.tokens * p.half;
+    uint8_t* ring = reinterpret_cast<uint8_t*>(cs + 4 * cs_size);
+    const int tid = threadIdx.x;
+    const uint32_t row_bytes = uint32_t(p.d) * 2, token_bytes = row_bytes * p.run, stage_bytes = token_bytes * p.tokens;
+
+    if (tid < kQkMaxPairs / 4) {
+        reinterpret_cast<float4*>(turn_hi)[tid] = reinterpret_cast<const float4*>(p.turn_hi)[tid];
+        reinterpret_cast<uint32_t*>(axis_of)[tid] = reinterpret_cast<const uint32_t*>(p.axis)[tid];
+    } else if (tid < kQkMaxPairs / 2) {
+        const int i = tid - kQkMaxPairs / 4;
+        reinterpret_cast<float4*>(turn_lo)[i] = reinterpret_cast<const float4*>(p.turn_lo)[i];
+    } else if (tid == kQkCompute) {
+        for (int i = 0; i < kQkStages; ++i) {
+            ptx::mbar_init(&full[i], 1 + 32);  // the rows, and the copy warp's lanes with slots and positions
+            ptx::mbar_init(&done[i], kQkWarps);
+        }
+        *abort_flag = 0;
+        ptx::fence_mbar_init();
+    }
+    ptx::griddep_launch_dependents();
     __syncthreads();
     ptx::griddep_wait();
 
-    const int64_t t0 = int64_t(blockIdx.x) * p.tokens;
-    const int nt = int(min(int64_t(p.tokens), p.n_tokens - t0));
-    const uint32_t heads = uint32_t(p.H + 2 * p.Hk), rows = heads * uint32_t(nt);
-    const int lanes = 1 << p.log_lanes;
-    const int u = tid & (lanes - 1), units = p.d / (2 * VEC), turned = p.half / VEC;
-    const uint32_t row_in = uint32_t(tid) >> p.log_lanes, pass = uint32_t(kQkThreads) >> p.log_lanes;
-    // the unit's elements: first and second of its pairs
-    const int rot = 2 * p.half, tail = (p.d - rot) / 2;
-    const int e0 = u < turned ? u * VEC : rot + (u - turned) * VEC;
-    const int e1 = u < turned ? p.half + u * VEC : e0 + tail;
-
-    QkVec<VEC> a[ROWS], b[ROWS];
-    int64_t slot[ROWS];
-    auto load = [&](uint32_t base) {
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            const uint32_t row = base + row_in + i * pass;
-            if (row >= rows || u >= units) continue;
-            const uint32_t tt = row / heads, h = row - tt * heads;
-            const int64_t t = t0 + tt;
-            const __nv_bfloat16* x = h < uint32_t(p.H)          ? p.q + t * p.q_stride + int64_t(h) * p.d
-                                     : h < uint32_t(p.H + p.Hk) ? p.k + t * p.k_stride + int64_t(h - p.H) * p.d
-                                                                : p.v + t * p.v_stride + int64_t(h - p.H - p.Hk) * p.d;
-            a[i] = *reinterpret_cast<const QkVec<VEC>*>(x + e0);
-            b[i] = *reinterpret_cast<const QkVec<VEC>*>(x + e1);
-            slot[i] = h < uint32_t(p.H) ? 0 : p.slots[t];
-        }
+    // Item `item`: tokens t0 .. t0 + nt - 1, rows h0 .. h1 - 1 of each. A token's part in the ring is its rows in order.
+    struct Item {
+        int64_t t0;
+        int nt, h0, h1;
     };
-    load(0);
-    for (int i = tid; i < p.d; i += kQkThreads) {
-        if (p.q_gamma) gam[i] = p.q_gamma[i];
-        if (p.k_gamma) gam[p.d + i] = p.k_gamma[i];
-    }
-    for (int i = tid; i < nt * p.half; i += kQkThreads) {
-        const int tt = i / p.half, j = i - tt * p.half;
-        const int32_t at = p.positions[int64_t(axis[j]) * p.pos_stride + t0 + tt];
-        // at * (hi + lo) as A + a, with what a position beyond 2^24 loses in fp32
-        const float pos = float(at), rest = float(int64_t(at) - int64_t(pos));
-        const float A = __fmul_rn(pos, fhi[j]);
-        const float r = fmaf(pos, flo[j], fmaf(pos, fhi[j], -A)) + rest * fhi[j];
-        sincos_two_float<true>(A, r, cosv[i], sinv[i]);
-    }
-    __syncthreads();
+    auto item_at = [&](int64_t item) {
+        Item I;
+        const int64_t group = p.runs == 1 ? item : item / p.runs;
+        I.t0 = group * p.tokens;
+        I.nt = int(min(int64_t(p.tokens), p.n_tokens - I.t0));
+        I.h0 = int(item - group * p.runs) * p.run;
+        I.h1 = min(I.h0 + p.run, p.H + 2 * p.Hk);
+        return I;
+    };
+    const int64_t step = gridDim.x;
 
-    for (uint32_t base = 0; base < rows; base += ROWS * pass) {
-        if (base > 0) load(base);
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            const uint32_t row = base + row_in + i * pass;
-            const bool live = row < rows && u < units;
-            const uint32_t tt = row / heads, h = row - tt * heads;
-            const int64_t t = t0 + tt;
-            const bool is_q = h < uint32_t(p.H), is_v = h >= uint32_t(p.H + p.Hk);
-            float xa[VEC], xb[VEC], ss = 0.0f;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                xa[e] = live ? __bfloat162float(a[i].v[e]) : 0.0f;
-                xb[e] = live ? __bfloat162float(b[i].v[e]) : 0.0f;
-                ss = fmaf(xa[e], xa[e], ss);
-                ss = fmaf(xb[e], xb[e], ss);
+    if (tid >= kQkCompute) {
+        // -------------------------------------------------------------------------- copies, a lane a token
+        const int lane = tid - kQkCompute;
+        // an item's rows of queries, keys and values: [lo, hi) counted from the kind's first head
+        struct Part {
+            int lo, hi;
+        };
+        auto part = [&](const Item& I, int first, int count) { return Part{max(I.h0 - first, 0), min(I.h1 - first, count)}; };
+        auto fill = [&](int64_t item, int st) {  // rows into a stage, and the token's slot and positions beside it
+            const Item I = item_at(item);
+            if (lane == 0) ptx::mbar_arrive_expect_tx(&full[st], uint32_t(I.nt * (I.h1 - I.h0)) * row_bytes);
+            __syncwarp();
+            if (lane < I.nt) {
+                const int64_t t = I.t0 + lane;
+                uint8_t* to = ring + st * stage_bytes + lane * token_bytes;
+                const Part q = part(I, 0, p.H), k = part(I, p.H, p.Hk), v = part(I, p.H + p.Hk, p.Hk);
+                if (q.lo < q.hi) ptx::bulk_load(to, p.q + t * p.q_stride + q.lo * p.d, uint32_t(q.hi - q.lo) * row_bytes, &full[st]);
+                if (k.lo < k.hi)
+                    ptx::bulk_load(to + (p.H + k.lo - I.h0) * row_bytes, p.k + t * p.k_stride + k.lo * p.d, uint32_t(k.hi - k.lo) * row_bytes, &full[st]);
+                if (v.lo < v.hi)
+                    ptx::bulk_load(to + (p.H + p.Hk + v.lo - I.h0) * row_bytes, p.v + t * p.v_stride + v.lo * p.d, uint32_t(v.hi - v.lo) * row_bytes, &full[st]);
+                ptx::async_copy<8>(slot_of + st * kQkMaxTokens + lane, p.slots + t);
+                for (int a = 0; a < p.axes; ++a)
+                    ptx::async_copy<4>(pos_of + (st * 4 + a) * kQkMaxTokens + lane, p.positions + a * p.pos_stride + t);
             }
-            if (p.q_gamma || p.k_gamma)
-                for (int o = lanes >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            if (!live) continue;
-            QkVec<VEC> oa = a[i], ob = b[i];
-            if (!is_v) {
-                if (is_q ? p.q_gamma != nullptr : p.k_gamma != nullptr) {
-                    const float inv = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, float(p.d)), p.eps)));
-                    const float* g = gam + (is_q ? 0 : p.d);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        xa[e] = __fmul_rn(__fmul_rn(xa[e], inv), g[e0 + e]);
-                        xb[e] = __fmul_rn(__fmul_rn(xb[e], inv), g[e1 + e]);
-                    }
+            ptx::async_copy_arrive(&full[st]);
+        };
+        auto drain = [&](const Item& I, int st) {  // and out of it
+            if (lane < I.nt) {
+                const int64_t t = I.t0 + lane, slot = slot_of[st * kQkMaxTokens + lane];
+                const uint8_t* from = ring + st * stage_bytes + lane * token_bytes;
+                const Part q = part(I, 0, p.H), k = part(I, p.H, p.Hk), v = part(I, p.H + p.Hk, p.Hk);
+                if (q.lo < q.hi) ptx::bulk_store(p.q_out + (t * p.H + q.lo) * p.d, from, uint32_t(q.hi - q.lo) * row_bytes);
+                if (slot >= 0 && slot < p.n_slots) {
+                    if (k.lo < k.hi)
+                        ptx::bulk_store(p.k_cache + (slot * p.Hk + k.lo) * p.d, from + (p.H + k.lo - I.h0) * row_bytes, uint32_t(k.hi - k.lo) * row_bytes);
+                    if (v.lo < v.hi)
+                        ptx::bulk_store(p.v_cache + (slot * p.Hk + v.lo) * p.d, from + (p.H + p.Hk + v.lo - I.h0) * row_bytes, uint32_t(v.hi - v.lo) * row_bytes);
                 }
-                if (u < turned) {
-                    const float* c = cosv + tt * p.half + e0;
-                    const float* s = sinv + tt * p.half + e0;
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float ya = __fsub_rn(__fmul_rn(xa[e], c[e]), __fmul_rn(xb[e], s[e]));
-                        xb[e] = __fadd_rn(__fmul_rn(xb[e], c[e]), __fmul_rn(xa[e], s[e]));
-                        xa[e] = ya;
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    oa.v[e] = __float2bfloat16_rn(xa[e]);
-                    ob.v[e] = __float2bfloat16_rn(xb[e]);
-                }
+                ptx::bulk_commit();
             }
-            __nv_bfloat16* y;
-            if (is_q) {
-                y = p.q_out + (t * p.H + h) * int64_t(p.d);
-            } else {
-                if (slot[i] < 0 || slot[i] >= p.n_slots) continue;
-                y = is_v ? p.v_cache + (slot[i] * p.Hk + (h - p.H - p.Hk)) * int64_t(p.d)
-                         : p.k_cache + (slot[i] * p.Hk + (h - p.H)) * int64_t(p.d);
+        };
+        ptx::fence_proxy_async_global();  // (the rows were written by ordinary stores)
+        for (int i = 0; i < kQkStages; ++i)
+            if (blockIdx.x + i * step < p.items) fill(blockIdx.x + i * step, i);
+        uint32_t n = 0;
+        for (int64_t item = blockIdx.x; item < p.items; item += step, ++n) {
+            const int st = int(n % kQkStages);
+            ptx::mbar_wait(&done[st], (n / kQkStages) & 1, abort_flag, status, kWaitLimitNs);
+            __syncwarp();
+            if (*reinterpret_cast<volatile int*>(abort_flag)) break;  // (the rows' copies have landed or never will)
+            drain(item_at(item), st);
+            // the item before this one has left its stage (its copies were given an item's time): it is filled again
+            const int64_t ahead = item + (kQkStages - 1) * step;
+            if (n > 0 && ahead < p.items) {
+                ptx::bulk_wait_read<1>();
+                __syncwarp();
+                fill(ahead, int((n + kQkStages - 1) % kQkStages));
             }
-            *reinterpret_cast<QkVec<VEC>*>(y + e0) = oa;
-            *reinterpret_cast<QkVec<VEC>*>(y + e1) = ob;
         }
+        ptx::bulk_wait_all();
+        return;
     }
+
+    // ------------------------------------------------------------------------------ norm and rotation
+    // (a wait that gave up sets the abort flag; the loop runs on, so that every barrier meets its threads)
+    const int lanes = 1 << p.log_lanes, u = tid & (lanes - 1), pass = kQkCompute >> p.log_lanes;
+    const int units = p.d / (2 * VEC);
+    // the lane's elements: first and second of its pairs
+    const int turned = p.half / VEC, rot = 2 * p.half;
+    const int e0 = u < turned ? u * VEC : rot + (u - turned) * VEC;
+    const int e1 = u < turned ? p.half + u * VEC : e0 + (p.d - rot) / 2;
+    for (int i = tid; i < p.d; i += kQkCompute) {
+        // element i is number `at` of the first or second halves of the pairs
+        const int in = i < rot ? i : i - rot, len = i < rot ? p.half : (p.d - rot) / 2;
+        const int second = in >= len, at = (i < rot ? 0 : p.half) + (second ? in - len : in);
+        float* to = gam + second * (p.d / 2) + unit_place<VEC>(at, units);
+        if (p.q_gamma) to[0] = p.q_gamma[i];
+        if (p.k_gamma) to[p.d] = p.k_gamma[i];
+    }
+    uint32_t n = 0;
+    for (int64_t item = blockIdx.x; item < p.items; item += step, ++n) {
+        const int st = int(n % kQkStages);
+        const Item I = item_at(item);
+        float* cosv = cs + (n & 1) * 2 * cs_size;  // (used two items ago: a barrier lies between)
+        float* sinv = cosv + cs_size;
+        ptx::mbar_wait(&full[st], (n / kQkStages) & 1, abort_flag, status, kWaitLimitNs);
+        const int per = min(I.h1, p.H + p.Hk) - I.h0, rows = max(per, 0) * I.nt;  // of queries and keys
+        if (rows > 0)
+            for (int i = tid; i < I.nt * p.half; i += kQkCompute) {
+                const int tt = i / p.half, j = i - tt * p.half, to = tt * p.half + unit_place<VEC>(j, turned);
+                turn_sincos(pos_of[(st * 4 + axis_of[j]) * kQkMaxTokens + tt], turn_hi[j], turn_lo[j], cosv[to], sinv[to]);
+            }
+        asm volatile("bar.sync 1, %0;" ::"n"(kQkCompute) : "memory");
+        for (int base = 0; base < rows; base += pass) {
+            const int row = base + (tid >> p.log_lanes);
+            const bool live = row < rows && u < units;
+            const int tt = live ? row / per : 0, h = live ? row - tt * per : 0;
+            __nv_bfloat16* x = reinterpret_cast<__nv_bfloat16*>(ring + st * stage_bytes + tt * token_bytes + h * row_bytes);
+            QkVec<VEC>* pa = reinterpret_cast<QkVec<VEC>*>(x + e0);
+            QkVec<VEC>* pb = reinterpret_cast<QkVec<VEC>*>(x + e1);
+            const bool is_q = I.h0 + h < p.H, norm = is_q ? p.q_gamma != nullptr : p.k_gamma != nullptr;
+            float2 xa[VEC / 2], xb[VEC / 2];
+            if (live) {
+                const QkVec<VEC> a = *pa, b = *pb;
+#pragma unroll
+                for (int e = 0; e < VEC / 2; ++e) {
+                    xa[e] = pair_of(reinterpret_cast<const QkVec<2>*>(&a)[e]);
+                    xb[e] = pair_of(reinterpret_cast<const QkVec<2>*>(&b)[e]);
+                }
+            }
+            if (p.q_gamma || p.k_gamma) {
+                float ss = 0.0f;
+                if (live) {
+                    float2 s2 = make_float2(0, 0);
+#pragma unroll
+                    for (int e = 0; e < VEC / 2; ++e) s2 = fma2(xb[e], xb[e], fma2(xa[e], xa[e], s2));
+                    ss = s2.x + s2.y;
+                }
+                __syncwarp();
+                for (int o = lanes >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+                if (live && norm) {
+                    const float inv = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, float(p.d)), p.eps)));
+                    const float2 inv2 = make_float2(inv, inv);
+                    float2 ga[VEC / 2], gb[VEC / 2];
+                    load_unit<VEC>(gam + (is_q ? 0 : p.d), u, units, ga);
+                    load_unit<VEC>(gam + (is_q ? 0 : p.d) + p.d / 2, u, units, gb);
+#pragma unroll
+                    for (int e = 0; e < VEC / 2; ++e) {
+                        xa[e] = mul2(mul2(xa[e], inv2), ga[e]);
+                        xb[e] = mul2(mul2(xb[e], inv2), gb[e]);
+                    }
+                }
+            }
+            if (!live) continue;
+            if (u < turned) {
+                float2 c[VEC / 2], s[VEC / 2];
+                load_unit<VEC>(cosv + tt * p.half, u, turned, c);
+                load_unit<VEC>(sinv + tt * p.half, u, turned, s);
+#pragma unroll
+                for (int e = 0; e < VEC / 2; ++e) {
+                    const float2 bs = mul2(xb[e], s[e]);
+                    const float2 y = fma2(xa[e], c[e], make_float2(-bs.x, -bs.y));
+                    xb[e] = fma2(xb[e], c[e], mul2(xa[e], s[e]));
+                    xa[e] = y;
+                }
+            }
+            QkVec<VEC> oa, ob;
+#pragma unroll
+            for (int e = 0; e < VEC / 2; ++e) {
+                reinterpret_cast<__nv_bfloat162*>(&oa)[e] = __floats2bfloat162_rn(xa[e].x, xa[e].y);
+                reinterpret_cast<__nv_bfloat162*>(&ob)[e] = __floats2bfloat162_rn(xb[e].x, xb[e].y);
+            }
+            *pa = oa;
+            *pb = ob;
+        }
+        ptx::fence_proxy_async_smem();  // the rows, before they are copied out
+        __syncwarp();
+        if ((tid & 31) == 0) ptx::mbar_arrive(&done[st]);
+    }
+}
+
+// The opt-in shared-memory size is a per-device function attribute.
+template <int VEC>
+cudaError_t qk_shared_memory() {
+    static std::mutex mu;
+    static bool done[64] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    std::lock_guard<std::mutex> lock(mu);
+    if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
+    e = cudaFuncSetAttribute(qk_norm_rope_kernel<VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, 110 * 1024);
+    if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
+    return e;
 }
 
 }  // namespace
@@ -352,35 +524,38 @@ cudaError_t launch_qk_norm_rope(const QkArgs& a, cudaStream_t s) {
     p.k_stride = a.k_stride;
     p.v_stride = a.v_stride;
     p.pos_stride = a.pos_stride;
-    p.n_tokens = a.n_tokens;
     p.n_slots = a.n_slots;
     p.H = int(a.n_heads);
     p.Hk = int(a.n_kv_heads);
     p.d = int(a.head_dim);
     p.half = int(a.rot_dim / 2);
     p.eps = a.eps;
-    if (p.half > 0) rotary_frequencies(double(a.base), a.rot_dim, p.inv_hi, p.inv_lo);
-    for (int i = 0; i < p.half; ++i) p.axis[i] = a.axis_of_pair ? a.axis_of_pair[i] : uint8_t(0);
+    std::memset(p.turn_hi, 0, sizeof(p.turn_hi) + sizeof(p.turn_lo) + sizeof(p.axis));
+    if (p.half > 0) rotary_frequencies(double(a.base), a.rot_dim, p.turn_hi, p.turn_lo, 1.0 / 6.283185307179586);
+    if (a.axis_of_pair) std::memcpy(p.axis, a.axis_of_pair, size_t(p.half));
     // 16-byte accesses where both halves of the pairs start on that boundary
     const int vec = p.half % 8 == 0 && (p.d - 2 * p.half) % 16 == 0 ? 8 : 4;
     const int units = p.d / (2 * vec);
     p.log_lanes = 0;
     while ((1 << p.log_lanes) < units) ++p.log_lanes;
-    const int64_t pass = kQkThreads >> p.log_lanes, heads = a.n_heads + 2 * a.n_kv_heads;
-    // as many tokens as give every thread four rows at once, one while that leaves SMs without a CTA
-    int rows = 4;
-    p.tokens = int(std::min<int64_t>(kQkMaxTokens, std::max<int64_t>(1, rows * pass / heads)));
-    if ((a.n_tokens + p.tokens - 1) / p.tokens < 2 * 152) {
-        rows = 1;
-        p.tokens = int(std::min<int64_t>(kQkMaxTokens, std::max<int64_t>(1, pass / heads)));
-    }
-    const size_t smem = (2 * size_t(p.d) + 2 * size_t(p.tokens) * p.half + 3 * size_t(p.half)) * 4;
-    const void* fn = vec == 8 ? (rows == 4 ? reinterpret_cast<const void*>(qk_norm_rope_kernel<8, 4>)
-                                           : reinterpret_cast<const void*>(qk_norm_rope_kernel<8, 1>))
-                              : (rows == 4 ? reinterpret_cast<const void*>(qk_norm_rope_kernel<4, 4>)
-                                           : reinterpret_cast<const void*>(qk_norm_rope_kernel<4, 1>));
-    void* args[] = {&p};
-    return launch_serialised(fn, unsigned((a.n_tokens + p.tokens - 1) / p.tokens), kQkThreads, smem, s, args);
+    // as many rows and tokens to an item as its bytes allow, fewer tokens while that leaves SMs without one
+    const int64_t heads = a.n_heads + 2 * a.n_kv_heads, row_bytes = a.head_dim * 2;
+    const int64_t sms = std::max(1, device_sm_count()), rows = kQkItemBytes / row_bytes;
+    p.run = int(std::min(heads, rows));
+    p.runs = int((heads + p.run - 1) / p.run);
+    p.run = int((heads + p.runs - 1) / p.runs);
+    p.tokens = int(std::max<int64_t>(1, std::min<int64_t>({kQkMaxTokens, rows / p.run, a.n_tokens * p.runs / (sms * kQkCtas * 2)})));
+    p.items = (a.n_tokens + p.tokens - 1) / p.tokens * p.runs;
+    p.axes = int(a.n_axes);
+    p.n_tokens = a.n_tokens;
+    const size_t smem = kQkHeadBytes + (2 * size_t(p.d) + 4 * size_t(p.tokens) * p.half) * 4 +
+                        size_t(kQkStages) * p.tokens * p.run * row_bytes;
+    const void* fn = vec == 8 ? reinterpret_cast<const void*>(qk_norm_rope_kernel<8>) : reinterpret_cast<const void*>(qk_norm_rope_kernel<4>);
+    const cudaError_t e = vec == 8 ? qk_shared_memory<8>() : qk_shared_memory<4>();
+    if (e != cudaSuccess) return e;
+    int* status = a.status;
+    void* args[] = {&p, &status};
+    return launch_serialised(fn, unsigned(std::min(p.items, sms * kQkCtas)), kQkThreads, smem, s, args);
 }
 
 }  // namespace emb

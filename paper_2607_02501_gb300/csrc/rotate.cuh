@@ -28,15 +28,15 @@ __device__ __forceinline__ void sincos_two_float(float A, float a, float& c, flo
     }
 }
 
-// hi[i] + lo[i] = base^(-2i/d) for i < d / 2, as the product of two powers, i = 16 j + k: at most 32 calls
-// of pow instead of one per pair, within two roundings of fp64. d <= 512.
-inline void rotary_frequencies(double base, int64_t d, float* hi, float* lo) {
+// hi[i] + lo[i] = unit * base^(-2i/d) for i < d / 2, as the product of two powers, i = 16 j + k: at most 32 calls
+// of pow instead of one per pair, within three roundings of fp64. d <= 512.
+inline void rotary_frequencies(double base, int64_t d, float* hi, float* lo, double unit = 1.0) {
     double coarse[16], fine[16];
     const int half = int(d / 2);
     for (int j = 0; 16 * j < half; ++j) coarse[j] = std::pow(base, -32.0 * double(j) / double(d));
     for (int k = 0; k < 16 && k < half; ++k) fine[k] = std::pow(base, -2.0 * double(k) / double(d));
     for (int i = 0; i < half; ++i) {
-        const double v = coarse[i >> 4] * fine[i & 15];
+        const double v = unit * (coarse[i >> 4] * fine[i & 15]);
         hi[i] = float(v);
         lo[i] = float(v - double(hi[i]));
     }
