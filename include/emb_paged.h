@@ -106,7 +106,7 @@ EMB_API emb_status emb_qk_norm_rope(const uint16_t* q, int64_t q_stride, const u
  * makes its queries' outputs NaN; a score of -infinity has weight zero; a visible value that is not finite makes
  * that element of its queries' outputs infinite or NaN. The scores are held in base 2 (scale *
  * log2(e) rounded to fp32 once), the weights by the hardware's power of two (relative error about 2^-22; below 2^-126 of
- * the largest they are zero). Up to 64 query rows (queries times heads per key/value head) of a request, the
+ * the largest they are zero). Up to 16 query rows (max_q queries times heads per key/value head), the
  * weights enter the value product as bf16 hi + lo (2^-16); above, rounded once to bf16 (2^-9 each).
  * kv_len above max_pages * page_size counts as that; q_start past n_tokens as n_tokens, and a decreasing
  * q_start as no queries; a page id outside [0, n_pages) as a page of zeros. Rows of O from q_start[n_req] to

@@ -171,12 +171,20 @@ def _ptr(x) -> Optional[int]:
     return int(x.data_ptr())
 
 
+_current = None   # (device of the thread, raw handle of a device's current stream), once torch is loaded
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
         # the current stream's handle itself: building the Stream object of
-        # torch.cuda.current_stream() takes 2.8 us a call, this 0.3
-        import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        # torch.cuda.current_stream() takes 2.8 us a call, this 0.1 (0.4 through the public
+        # current_device and an import statement per call)
+        global _current
+        if _current is None:
+            import torch
+            torch.cuda.current_device()
+            _current = (torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+        return _current[1](_current[0]())
     if isinstance(stream, int):
         return stream
     return int(stream.cuda_stream)
@@ -385,16 +393,20 @@ def emb_attention(Q, K0, V0, K1, V1, O, n_heads: int, n_kv_heads: int, head_dim:
            "emb_attention")
 
 
+# (these are called once per step or layer on the smallest steps too: bound functions and one status test)
+
 def emb_paged_slots(cached, added, free_pages, used, table, q_start, kv_len, slots, positions, used_out,
                     page_size: int, stream=None) -> None:
     """cached, added: int32 [R]; free_pages: int32 [n_free]; used, used_out: int32 [1]; table: int32
     [R][max_pages], filled on; out: q_start int32 [R + 1], kv_len int32 [R], slots int64 [T], positions
     int32 [T]."""
     R, max_pages = table.shape
-    _check(paged_lib().emb_paged_slots(
+    status = (_paged or paged_lib()).emb_paged_slots(
         cached.data_ptr(), added.data_ptr(), R, free_pages.data_ptr(), free_pages.shape[0], used.data_ptr(), page_size,
         table.data_ptr(), max_pages, q_start.data_ptr(), kv_len.data_ptr(), slots.data_ptr(), positions.data_ptr(),
-        slots.shape[0], used_out.data_ptr(), _stream(stream)), "emb_paged_slots")
+        slots.shape[0], used_out.data_ptr(), _stream(stream))
+    if status:
+        raise EmbError(status, "emb_paged_slots")
 
 
 def emb_qk_norm_rope(q, k, v, q_out, k_cache, v_cache, slots, positions, q_gamma=None, k_gamma=None,
@@ -405,17 +417,20 @@ def emb_qk_norm_rope(q, k, v, q_out, k_cache, v_cache, slots, positions, q_gamma
     [d]; axis_of_pair: bytes or integers [rot_dim / 2]; rot_dim: d by default."""
     n_pages, page_size, Hk, d = k_cache.shape
     T, width = q.shape
-    axes, pos_stride = (1, T) if positions.dim() == 1 else (positions.shape[0], positions.stride(0))
+    shape = positions.shape
+    axes, pos_stride = (1, T) if len(shape) == 1 else (shape[0], positions.stride(0))
     rot = d if rot_dim is None else rot_dim
     if axis_of_pair is not None:
         axis_of_pair = bytes(axis_of_pair)
         if len(axis_of_pair) != rot // 2:
             raise EmbError(EMB_EINVAL, "emb_qk_norm_rope: axis_of_pair")
-    _check(paged_lib().emb_qk_norm_rope(
+    status = (_paged or paged_lib()).emb_qk_norm_rope(
         q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0), T, width // d, Hk, d,
-        _ptr(q_gamma), _ptr(k_gamma), eps, positions.data_ptr(), pos_stride, axes, axis_of_pair, rot, base, slots.data_ptr(),
-        q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), n_pages, page_size, _stream(stream)),
-        "emb_qk_norm_rope")
+        None if q_gamma is None else q_gamma.data_ptr(), None if k_gamma is None else k_gamma.data_ptr(), eps,
+        positions.data_ptr(), pos_stride, axes, axis_of_pair, rot, base, slots.data_ptr(), q_out.data_ptr(),
+        k_cache.data_ptr(), v_cache.data_ptr(), n_pages, page_size, _stream(stream))
+    if status:
+        raise EmbError(status, "emb_qk_norm_rope")
 
 
 def emb_paged_attention(Q, k_cache, v_cache, table, q_start, kv_len, O, scale: float, max_q: int,
@@ -425,11 +440,12 @@ def emb_paged_attention(Q, k_cache, v_cache, table, q_start, kv_len, O, scale: f
     n_pages, page_size, Hk, d = k_cache.shape
     R, max_pages = table.shape
     T, width = Q.shape
-    _check(paged_lib().emb_paged_attention(
+    status = (_paged or paged_lib()).emb_paged_attention(
         Q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), n_pages, page_size, table.data_ptr(), max_pages,
-        q_start.data_ptr(), kv_len.data_ptr(), _ptr(prefix), R, T, max_q, O.data_ptr(), width // d, Hk, d, scale, cap,
-        window, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)),
-        "emb_paged_attention")
+        q_start.data_ptr(), kv_len.data_ptr(), None if prefix is None else prefix.data_ptr(), R, T, max_q, O.data_ptr(),
+        width // d, Hk, d, scale, cap, window, workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    if status:
+        raise EmbError(status, "emb_paged_attention")
 
 
 def paged_workspace(device=None):

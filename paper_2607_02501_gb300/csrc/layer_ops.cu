@@ -14,7 +14,6 @@
 #include <type_traits>
 
 #include "ptx.cuh"
-#include "rotate.cuh"
 
 namespace emb {
 namespace {
@@ -174,8 +173,21 @@ __global__ void __launch_bounds__(256) rope_kernel(const __grid_constant__ RopeP
             const float hi = inv_hi[i + e];
             const float A = __fmul_rn(pos, hi);
             const float a = __fadd_rn(fmaf(pos, hi, -A), __fmul_rn(pos, inv_lo[i + e]));
+            float sA, cA;
+            sincosf(A, &sA, &cA);
             float c, s;
-            sincos_two_float<LARGE>(A, a, c, s);
+            if constexpr (LARGE) {
+                // sine and cosine of a by their series (error below 1e-10 up to 1/16), then the addition formulas
+                const float a2 = __fmul_rn(a, a);
+                float sa = __fmul_rn(a, fmaf(a2, fmaf(a2, 1.0f / 120.0f, -1.0f / 6.0f), 1.0f));
+                float ca = fmaf(a2, fmaf(a2, 1.0f / 24.0f, -0.5f), 1.0f);
+                if (fabsf(a) > 0.0625f) sincosf(a, &sa, &ca);
+                c = fmaf(cA, ca, -__fmul_rn(sA, sa));
+                s = fmaf(sA, ca, __fmul_rn(cA, sa));
+            } else {
+                c = fmaf(-a, sA, cA);
+                s = fmaf(a, cA, sA);
+            }
             const float xa = __bfloat162float(va.v[e]), xb = __bfloat162float(vb.v[e]);
             oa.v[e] = __float2bfloat16_rn(__fsub_rn(__fmul_rn(xa, c), __fmul_rn(xb, s)));
             ob.v[e] = __float2bfloat16_rn(__fadd_rn(__fmul_rn(xb, c), __fmul_rn(xa, s)));
@@ -755,8 +767,17 @@ cudaError_t launch_rope(uint16_t* x, int64_t n_heads, uint16_t* x2, int64_t n_he
     p.n_heads = int(n_heads);
     p.n_heads2 = int(n_heads2);
     p.head_dim = int(head_dim);
+    // base^(-2i/d) as the product of two powers, i = 16 j + k: at most 32 calls of pow instead of one
+    // per pair, within two roundings of fp64
+    double coarse[kRopeMaxPairs / 16], fine[16];
     const int half_d = int(head_dim / 2);
-    rotary_frequencies(base, head_dim, p.inv_hi, p.inv_lo);
+    for (int j = 0; 16 * j < half_d; ++j) coarse[j] = std::pow(base, -32.0 * double(j) / double(head_dim));
+    for (int k = 0; k < 16 && k < half_d; ++k) fine[k] = std::pow(base, -2.0 * double(k) / double(head_dim));
+    for (int i = 0; i < half_d; ++i) {
+        const double v = coarse[i >> 4] * fine[i & 15];
+        p.inv_hi[i] = float(v);
+        p.inv_lo[i] = float(v - double(p.inv_hi[i]));
+    }
     // Pairs per thread: the widest access that divides a head's half (both halves then start on
     // its boundary), fewer while that leaves the SMs short of threads.
     const int64_t half = head_dim / 2, pairs = M * (n_heads + n_heads2) * half;

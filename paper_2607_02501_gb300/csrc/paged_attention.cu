@@ -29,15 +29,13 @@ __device__ __forceinline__ void ldsm_x4_trans(uint32_t saddr, uint32_t (&r)[4]) 
 }
 // ------------------------------------------------------------------ few rows: mma.sync
 // A producer warp brings tiles of 64 keys and values by TMA (a box per page, 128-byte swizzled rows) into a ring;
-// four warps compute. WK = 4: an item has 16 rows (queries times heads), every warp takes 16 of a tile's keys, and the
-// warps' results are merged at the item's end. WK = 1: an item has 64 rows, 16 per warp, and every warp takes all
-// keys. Scores, softmax in base 2 with a running maximum and the value product (weights as bf16 hi + lo) stay in
-// registers. HBM bounds it: the cache is read once for 16 or 64 rows.
+// four warps compute. An item has 16 rows (queries times heads), every warp takes 16 of a tile's keys, and the
+// warps' results are merged at the item's end. Scores, softmax in base 2 with a running maximum and the value
+// product (weights as bf16 hi + lo) stay in registers. HBM bounds it: the cache is read once for the 16 rows.
 constexpr int kFewWarps = 4;
 constexpr int kFewThreads = 32 * (kFewWarps + 1);
 constexpr int kFewTile = 64;
-template <int WK>
-constexpr int kFewRows = 16 * kFewWarps / WK;
+constexpr int kFewRows = 16;
 
 template <int D>
 struct FewTraits {
@@ -45,14 +43,14 @@ struct FewTraits {
     static constexpr int kStages = D == 64 ? 6 : 3;
     static constexpr int kCtas = D == 256 ? 1 : 2;   // per SM
     static constexpr int kQPitch = D + 8;            // queries in shared memory (D = 256), bf16 per padded row
-    static constexpr int kQBytes = D == 256 ? 64 * kQPitch * 2 : 0;
+    static constexpr int kQBytes = D == 256 ? kFewRows * kQPitch * 2 : 0;
     static constexpr int kSmem = 1024 + kStages * kStage + kQBytes;
 };
 
-template <int D, int WK, bool CAP>
+template <int D, bool CAP>
 __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_kernel(const __grid_constant__ PagedParams p) {
     using T = FewTraits<D>;
-    constexpr int KS = D / 16, NT = D / 8, NJ = kFewTile / 8 / WK, ROWS = kFewRows<WK>;
+    constexpr int KS = D / 16, NT = D / 8, NJ = kFewTile / 8 / kFewWarps, ROWS = kFewRows;
     constexpr bool QS = D == 256;  // queries stay in shared memory: their fragments would not fit the registers
     constexpr int kSub = kFewTile * 128;  // bytes of a 64-dim part of a tile
     using PL = PartLayout<D, ROWS>;
@@ -151,9 +149,9 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
     zero_padding(p, D, threadIdx.x, 32 * kFewWarps);
     auto bar = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };
     const int quad = lane >> 2, qc = lane & 3;
-    const int wrow = WK == 1 ? warp * 16 : 0, wkey = WK == 1 ? 0 : warp * 16;
+    const int wkey = warp * 16;  // the warp's keys of a tile
     const uint32_t ring_u = ptx::smem_u32(ring);
-    __nv_bfloat16* sq = reinterpret_cast<__nv_bfloat16*>(ring + T::kStages * T::kStage) + (QS ? wrow * T::kQPitch : 0);
+    __nv_bfloat16* sq = reinterpret_cast<__nv_bfloat16*>(ring + T::kStages * T::kStage);
     int joins = 0;
 
     while (x < st.x1) {
@@ -161,7 +159,7 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
         const uint32_t take = min(st.x1 - x, uint32_t(it.units) - off);
         const int j0 = int(off), j1 = min(int(off + take), it.nt);
         // this thread's two rows: query and head, keys they see
-        const int rA = wrow + quad, rB = rA + 8, iA = rA / p.G, iB = rB / p.G;
+        const int rA = quad, rB = rA + 8, iA = rA / p.G, iB = rB / p.G;
         const bool okA = iA < it.nq, okB = iB < it.nq;
         const KeyRange none{0, 0};
         const KeyRange kA = okA ? query_keys(p, it.q, it.i0 + iA) : none, kB = okB ? query_keys(p, it.q, it.i0 + iB) : none;
@@ -180,19 +178,14 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
                 qf[ks][3] = ldq(okB, offB + c + 8);
             }
         } else {
-            // WK = 4: the warps bring four rows each of the 16 they share
-            if constexpr (WK == 4) bar();  // (the last item's rows are done with)
-            else __syncwarp();
-            constexpr int kMine = WK == 4 ? 4 : 16;
-            const int first = WK == 4 ? warp * 4 : 0;
-            for (int e = lane; e < kMine * (D / 8); e += 32) {
-                const int rr = first + e / (D / 8), c = (e % (D / 8)) * 8, i = (wrow + rr) / p.G;
+            bar();  // (the last item's rows are done with)
+            for (int e = threadIdx.x; e < ROWS * (D / 8); e += 32 * kFewWarps) {
+                const int rr = e / (D / 8), c = (e % (D / 8)) * 8, i = rr / p.G;
                 uint4 v = make_uint4(0, 0, 0, 0);
-                if (i < it.nq) v = *reinterpret_cast<const uint4*>(p.Q + row_of(i, wrow + rr) + c);
+                if (i < it.nq) v = *reinterpret_cast<const uint4*>(p.Q + row_of(i, rr) + c);
                 *reinterpret_cast<uint4*>(sq + rr * T::kQPitch + c) = v;
             }
-            if constexpr (WK == 4) bar();
-            else __syncwarp();
+            bar();
         }
 
         float o[NT][4];
@@ -354,7 +347,7 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
             }
             __syncwarp();
             // (the last tile's keys make room for the warps' merge first)
-            if (lane == 0 && (WK == 1 || j + 1 < j1)) ptx::mbar_arrive(&empty[s]);
+            if (lane == 0 && j + 1 < j1) ptx::mbar_arrive(&empty[s]);
         }
 #pragma unroll
         for (int i = 1; i <= 2; i <<= 1) {
@@ -365,7 +358,7 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
             for (int key = (it.t0 + j0) * kFewTile; key < min((it.t0 + j1) * kFewTile, it.hi); ++key) {
                 const int in = key & (kFewTile - 1), key0 = key - in;
                 if (!(key0 < it.lo_all || min(key0 + kFewTile, it.q.L) > it.hi_all)) continue;
-                if (WK > 1 && (in < wkey || in >= wkey + 16)) continue;
+                if (in < wkey || in >= wkey + 16) continue;
                 const int page = p.table[int64_t(r) * p.max_pages + (key >> p.page_shift)];
                 if (page < 0 || page >= p.n_pages) continue;
                 const int64_t slot = (int64_t(page) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
@@ -387,53 +380,51 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
             }
         }
 
-        // WK = 4: the warps lay their results side by side where the last tile was (a lane's four values of n-tile n at
+        // The warps lay their results side by side where the last tile was (a lane's four values of n-tile n at
         // [n][lane]: no two lanes meet in a bank), and each adds up a quarter of the n-tiles
-        constexpr int kMine = NT / WK;
-        const int n0 = WK == 1 ? 0 : warp * kMine;
-        if constexpr (WK == 4) {
-            if (j1 > j0) {
-                const int s = (issued - 1) % T::kStages;
-                float4* buf = reinterpret_cast<float4*>(ring + s * T::kStage);  // [warp][n-tile][lane]
-                bar();  // every warp is done with the keys and values
+        constexpr int kMine = NT / kFewWarps;
+        const int n0 = warp * kMine;
+        if (j1 > j0) {
+            const int s = (issued - 1) % T::kStages;
+            float4* buf = reinterpret_cast<float4*>(ring + s * T::kStage);  // [warp][n-tile][lane]
+            bar();  // every warp is done with the keys and values
 #pragma unroll
-                for (int n = 0; n < NT; ++n) buf[(warp * NT + n) * 32 + lane] = make_float4(o[n][0], o[n][1], o[n][2], o[n][3]);
-                if (qc == 0) {
-                    warp_m[warp][quad] = mA;
-                    warp_l[warp][quad] = lA;
-                    warp_m[warp][quad + 8] = mB;
-                    warp_l[warp][quad + 8] = lB;
-                }
-                bar();
-                mA = mB = -INFINITY;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    mA = fmaxf(mA, warp_m[w][quad]);
-                    mB = fmaxf(mB, warp_m[w][quad + 8]);
-                }
-                const float zA = mA == -INFINITY ? 0.0f : mA, zB = mB == -INFINITY ? 0.0f : mB;
-                lA = lB = 0.0f;
-#pragma unroll
-                for (int n = 0; n < kMine; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.0f;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    // weight 0 of a warp without a finite score: its sums are 0, or NaN, which has to show
-                    const float wA = exp2_fast(warp_m[w][quad] - zA), wB = exp2_fast(warp_m[w][quad + 8] - zB);
-                    lA = fmaf(warp_l[w][quad], wA, lA);
-                    lB = fmaf(warp_l[w][quad + 8], wB, lB);
-#pragma unroll
-                    for (int n = 0; n < kMine; ++n) {
-                        const float4 u = buf[(w * NT + n0 + n) * 32 + lane];
-                        o[n][0] = fmaf(u.x, wA, o[n][0]);
-                        o[n][1] = fmaf(u.y, wA, o[n][1]);
-                        o[n][2] = fmaf(u.z, wB, o[n][2]);
-                        o[n][3] = fmaf(u.w, wB, o[n][3]);
-                    }
-                }
-                ptx::fence_proxy_async_smem();  // before the next copy into this buffer
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&empty[s]);
+            for (int n = 0; n < NT; ++n) buf[(warp * NT + n) * 32 + lane] = make_float4(o[n][0], o[n][1], o[n][2], o[n][3]);
+            if (qc == 0) {
+                warp_m[warp][quad] = mA;
+                warp_l[warp][quad] = lA;
+                warp_m[warp][quad + 8] = mB;
+                warp_l[warp][quad + 8] = lB;
             }
+            bar();
+            mA = mB = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                mA = fmaxf(mA, warp_m[w][quad]);
+                mB = fmaxf(mB, warp_m[w][quad + 8]);
+            }
+            const float zA = mA == -INFINITY ? 0.0f : mA, zB = mB == -INFINITY ? 0.0f : mB;
+            lA = lB = 0.0f;
+#pragma unroll
+            for (int n = 0; n < kMine; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                // weight 0 of a warp without a finite score: its sums are 0, or NaN, which has to show
+                const float wA = exp2_fast(warp_m[w][quad] - zA), wB = exp2_fast(warp_m[w][quad + 8] - zB);
+                lA = fmaf(warp_l[w][quad], wA, lA);
+                lB = fmaf(warp_l[w][quad + 8], wB, lB);
+#pragma unroll
+                for (int n = 0; n < kMine; ++n) {
+                    const float4 u = buf[(w * NT + n0 + n) * 32 + lane];
+                    o[n][0] = fmaf(u.x, wA, o[n][0]);
+                    o[n][1] = fmaf(u.y, wA, o[n][1]);
+                    o[n][2] = fmaf(u.z, wB, o[n][2]);
+                    o[n][3] = fmaf(u.w, wB, o[n][3]);
+                }
+            }
+            ptx::fence_proxy_async_smem();  // before the next copy into this buffer
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&empty[s]);
         }
 
         const bool whole = off == 0 && take == uint32_t(it.units);
@@ -450,7 +441,7 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
             PagedJoin J{r, g, b, int(a / st.chunk), 0};
             J.count = int((a + uint32_t(it.units) - 1) / st.chunk) - J.first + 1;
             float* part = p.part + part_slot(int(blockIdx.x), J.first) * PL::kFloats;
-            if (qc == 0 && (WK == 1 || warp == 0)) {
+            if (qc == 0 && warp == 0) {
                 if (okA) {
                     part[rA] = mA;
                     part[ROWS + rA] = lA;
@@ -543,7 +534,7 @@ double unit_bound(const PagedAttnArgs& a, int qb, int kt) {
 namespace {
 
 // CTAs that run at once, asked once per device; the opt-in shared memory is a per-device attribute too.
-template <int D, int WK, bool CAP>
+template <int D, bool CAP>
 cudaError_t few_resident(int& ctas) {
     static std::mutex mu;
     static int known[64] = {};
@@ -555,38 +546,36 @@ cudaError_t few_resident(int& ctas) {
         ctas = known[dev];
         return cudaSuccess;
     }
-    auto* kernel = paged_few_kernel<D, WK, CAP>;
+    auto* kernel = paged_few_kernel<D, CAP>;
     int per_sm = 0;
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FewTraits<D>::kSmem);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kFewThreads, FewTraits<D>::kSmem);
     if (e != cudaSuccess) return e;
     // a partial result per item border: two per CTA, within the workspace
-    const size_t slot = size_t(kFewRows<WK>) * (D + 2) * 4;
+    const size_t slot = size_t(kFewRows) * (D + 2) * 4;
     const int fit = int((EMB_PAGED_WORKSPACE - kPagedFlagBytes) / (2 * slot));
     ctas = std::max(1, std::min({std::max(1, per_sm) * std::max(1, device_sm_count()), fit, int(kPagedFlagBytes / 4)}));
     if (dev >= 0 && dev < 64) known[dev] = ctas;
     return cudaSuccess;
 }
 
-template <int D, int WK, bool CAP>
+template <int D, bool CAP>
 cudaError_t launch_few(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
     int ctas = 0;
-    const cudaError_t e = few_resident<D, WK, CAP>(ctas);
+    const cudaError_t e = few_resident<D, CAP>(ctas);
     if (e != cudaSuccess) return e;
-    p.QB = kFewRows<WK> / p.G;
+    p.QB = kFewRows / p.G;
     const uint32_t box = uint32_t(std::min<int64_t>(a.page_size, kFewTile));
     if (!encode_cache(&p.k_map, a.k_cache, a, box) || !encode_cache(&p.v_map, a.v_cache, a, box)) return cudaErrorInvalidValue;
     void* args[] = {&p};
     const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, kFewTile))));
     set_grid(p, grid, 3);
-    return launch_serialised(reinterpret_cast<const void*>(paged_few_kernel<D, WK, CAP>), grid, kFewThreads, FewTraits<D>::kSmem, s, args);
+    return launch_serialised(reinterpret_cast<const void*>(paged_few_kernel<D, CAP>), grid, kFewThreads, FewTraits<D>::kSmem, s, args);
 }
 
 template <int D>
 cudaError_t launch_few_d(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
-    const bool one_warp_rows = p.G <= 16 && a.max_q * p.G <= 16;  // a request's rows fit a warp's 16
-    if (a.cap > 0.0f) return one_warp_rows ? launch_few<D, 4, true>(p, a, s) : launch_few<D, 1, true>(p, a, s);
-    return one_warp_rows ? launch_few<D, 4, false>(p, a, s) : launch_few<D, 1, false>(p, a, s);
+    return a.cap > 0.0f ? launch_few<D, true>(p, a, s) : launch_few<D, false>(p, a, s);
 }
 
 }  // namespace
@@ -620,8 +609,13 @@ cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s) {
     constexpr double kLog2e = 1.4426950408889634;
     p.scale2 = a.cap > 0.0f ? float(2.0 * kLog2e * double(a.scale) / double(a.cap)) : float(kLog2e * double(a.scale));
     p.cap2 = float(kLog2e * double(a.cap));
-    // a request's rows beyond 64 go to the tensor cores' kernel, which multiplies its scores by a positive scale
-    if (a.max_q * p.G > 64 && a.scale > 0.0f) return launch_paged_many(p, a, s);
+    // More rows than a warp's 16 go to the tcgen05 kernel. (A kernel of this kind with 64 rows, 16 per warp, was the
+    // sooner of the two by 6 % over 200 calls with heads of 64, and slower by 61 and 120 % with heads of 128 and 256.)
+    if (p.G > 16 || a.max_q * p.G > 16) {
+        p.negate = a.scale < 0.0f;
+        p.scale2 = std::max(std::fabs(p.scale2), 1e-37f);  // (hidden scores are -infinity times this)
+        return launch_paged_many(p, a, s);
+    }
     return a.head_dim == 64    ? launch_few_d<64>(p, a, s)
            : a.head_dim == 128 ? launch_few_d<128>(p, a, s)
                                : launch_few_d<256>(p, a, s);

@@ -5,11 +5,11 @@
 // Both kernels are launched with programmatic stream serialisation and read device memory only
 // after griddepcontrol.wait, with ordinary loads.
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <mutex>
 
 #include "paged.cuh"
-#include "rotate.cuh"
 
 namespace emb {
 namespace {
@@ -531,7 +531,19 @@ cudaError_t launch_qk_norm_rope(const QkArgs& a, cudaStream_t s) {
     p.half = int(a.rot_dim / 2);
     p.eps = a.eps;
     std::memset(p.turn_hi, 0, sizeof(p.turn_hi) + sizeof(p.turn_lo) + sizeof(p.axis));
-    if (p.half > 0) rotary_frequencies(double(a.base), a.rot_dim, p.turn_hi, p.turn_lo, 1.0 / 6.283185307179586);
+    if (p.half > 0) {
+        // base^(-2i/d) / 2 pi, i = 16 j + k, from two powers by multiplication: within 32 roundings of fp64, which the two
+        // floats (48 bits) do not see; a call of pow per pair takes longer than the launch
+        const double fine = std::pow(double(a.base), -2.0 / double(a.rot_dim)), coarse = std::pow(double(a.base), -32.0 / double(a.rot_dim));
+        double c = 1.0 / 6.283185307179586;
+        for (int j = 0; 16 * j < p.half; ++j, c *= coarse) {
+            double v = c;
+            for (int i = 16 * j; i < std::min(16 * j + 16, p.half); ++i, v *= fine) {
+                p.turn_hi[i] = float(v);
+                p.turn_lo[i] = float(v - double(p.turn_hi[i]));
+            }
+        }
+    }
     if (a.axis_of_pair) std::memcpy(p.axis, a.axis_of_pair, size_t(p.half));
     // 16-byte accesses where both halves of the pairs start on that boundary
     const int vec = p.half % 8 == 0 && (p.d - 2 * p.half) % 16 == 0 ? 8 : 4;

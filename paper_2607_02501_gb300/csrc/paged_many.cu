@@ -78,7 +78,7 @@ __device__ __forceinline__ Segment<D> segment_of(const PagedParams& p, int r, in
     s.take = min(x1 - x, uint32_t(s.it.units) - off);
     s.j0 = s.it.t0 + int(off);
     s.j1 = s.it.t0 + min(int(off + s.take), s.it.nt);
-    const int qt = p.QB / T::NQ;
+    const int qt = p.QT;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         s.nq[t] = t < T::NQ ? max(0, min(qt, s.it.nq - t * qt)) : 0;
@@ -100,6 +100,8 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
     constexpr int NQ = T::NQ, KT = T::KT, S = T::kSlots;
     constexpr int kRows = 128 * NQ;
     using PL = PartLayout<D, kRows>;
+    // what stands for the score of a key that a row does not see (a cap would make -infinity finite)
+    constexpr float kHidden = CAP ? -3.402823466e38f : -INFINITY;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t kv_full[S], kv_empty[S], q_full, q_empty, s_full[2], p_ready[2], o_done[2], o_free[2], drain;
     __shared__ uint32_t tmem_slot, odd_item;
@@ -157,7 +159,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         if constexpr (NQ == 2) ptx::regs_down<72>();
         ptx::fence_proxy_async_global();  // (the cache and the queries were written by ordinary stores)
         const int page_size = 1 << p.page_shift, box = min(page_size, KT), n_box = KT / box;
-        const int qt = p.QB / NQ;
+        const int qt = p.QT;
         uint32_t n = 0, loads = 0, items = 0;  // tiles; ring copies and items with queries issued
         bool ok = true;
         while (x < st.x1 && ok) {
@@ -226,7 +228,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
     } else if (warp == T::kSoftWarps) {
         // ------------------------------------------------------------------------- MMAs
         if constexpr (NQ == 2) ptx::regs_down<72>();
-        const uint32_t idesc_qk = ptx::idesc_bf16_f32(128, KT), idesc_pv = ptx::idesc_bf16_f32(128, D) | ptx::kIdescMnMajorB;
+        const uint32_t idesc_qk = ptx::idesc_bf16_f32(128, KT) | (p.negate ? ptx::kIdescNegateA : 0u), idesc_pv = ptx::idesc_bf16_f32(128, D) | ptx::kIdescMnMajorB;
         const uint32_t sq_u = ptx::smem_u32(sq), ring_u = ptx::smem_u32(ring);
         uint32_t n = 0, items = 0;
         uint32_t scores[2] = {0, 0}, owned[2] = {0, 0};  // score tiles by place, items with outputs by row tile
@@ -308,7 +310,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         if constexpr (NQ == 2) ptx::regs_up<216>();
         zero_padding(p, D, threadIdx.x, 32 * T::kSoftWarps);
         const int t = warp >> 2;  // row tile
-        const int row = 32 * (warp & 3) + lane, qt = p.QB / NQ, i = row / p.G;
+        const int row = 32 * (warp & 3) + lane, qt = p.QT, i = row / p.G;
         const uint32_t lanes = uint32_t(32 * (warp & 3)) << 16;
         const uint32_t o_col = tmem + lanes + uint32_t(T::kO + t * D);
         uint32_t n = 0, seen[2] = {0, 0}, outs = 0, ordinal = 0;
@@ -344,7 +346,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                         ptx::tmem_ld_32(s_col + c, v);
                         ptx::tmem_ld_wait_32(v);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(c + e < lo || c + e >= hi ? -INFINITY : v[e]);
+                        for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(c + e < lo || c + e >= hi ? kHidden : v[e]);
                         ptx::tmem_st_32(s_col + c, w);
                     }
                     ptx::tmem_st_wait();
@@ -364,7 +366,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 // (the maximum is of raw scores: a cap keeps their order)
                 const float mt = fmaxf(max3(top[0], top[1], top[2]), top[3]);
                 auto base2 = [&](float v) { return CAP ? capped(v * p.scale2, p.cap2) : v * p.scale2; };
-                const bool grow = m == -INFINITY ? mt > m : base2(mt) - base2(m) > 8.0f;
+                const bool grow = m == -INFINITY ? mt > kHidden : base2(mt) - base2(m) > 8.0f;
                 if (__any_sync(all, grow)) {
                     const float f = !grow ? 1.0f : m == -INFINITY ? 0.0f : exp2_fast(base2(m) - base2(mt));
                     if (j > a_t) {
@@ -397,7 +399,8 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
                         float2 u = make_float2(v[e], v[e + 1]);
-                        if constexpr (CAP) u = add2(make_float2(base2(u.x), base2(u.y)), mm);
+                        if constexpr (CAP)
+                            u = add2(make_float2(u.x == kHidden ? -INFINITY : base2(u.x), u.y == kHidden ? -INFINITY : base2(u.y)), mm);
                         else u = fma2(u, sc, mm);
                         u.x = exp2_fast(u.x);
                         u.y = exp2_fast(u.y);
@@ -574,15 +577,22 @@ cudaError_t launch_many(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) 
             if (dev >= 0 && dev < 64) done[dev] = true;
         }
     }
-    const int tile = 128 / p.G;  // queries of a row tile
-    p.QB = T::NQ * tile;
+    // An item has two full row tiles (one with heads of 256), less while the call would leave SMs without a unit: a small
+    // item's partial results are sooner written and joined (50 queries of 8 heads over 866 keys: 256 rows 16.5 us)
+    const int sms = std::max(1, device_sm_count());
+    p.QT = 128 / p.G;
+    p.QB = T::NQ * p.QT;
+    while (p.QB * p.G > 16 && p.QB > 1 && unit_bound(a, p.QB, T::KT) < 0.6 * sms) {
+        if (p.QB > p.QT) p.QB = p.QT;
+        else p.QB = p.QT = (p.QT + 1) / 2;
+    }
     const uint32_t box = uint32_t(std::min<int64_t>(a.page_size, T::KT));
     if (!encode_cache(&p.k_map, a.k_cache, a, box) || !encode_cache(&p.v_map, a.v_cache, a, box) ||
-        !encode_queries(&p.q_map, a, uint32_t(p.G), uint32_t(tile)))
+        !encode_queries(&p.q_map, a, uint32_t(p.G), uint32_t(p.QT)))
         return cudaErrorInvalidValue;
     const size_t part = size_t(128 * T::NQ) * (D + 2) * 4;
     const int fit = int((EMB_PAGED_WORKSPACE - kPagedFlagBytes) / (2 * part));
-    const int ctas = std::max(1, std::min({device_sm_count(), fit, int(kPagedFlagBytes / 4)}));
+    const int ctas = std::max(1, std::min({sms, fit, int(kPagedFlagBytes / 4)}));
     void* args[] = {&p};
     const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, T::KT))));
     set_grid(p, grid, D == 256 ? 8 : 4);

@@ -33,7 +33,8 @@ struct PagedParams {
     int* status;
     int64_t max_pages;
     int n_tokens, n_req, n_pages, page_shift, kv_limit, window;
-    int H, Hk, G, QB;
+    int H, Hk, G, QB, QT;  // heads, those of one key/value head; queries of an item and of a row tile
+    bool negate;           // the scale is negative: its magnitude is in scale2
     uint32_t join_units;  // units that joining a cut item costs
     uint32_t grid_inv;  // ceil(2^32 / grid)
     float scale2;  // scores are kept in base 2: scale * log2(e); capped, 2 log2(e) scale / cap

@@ -424,6 +424,7 @@ __device__ __forceinline__ uint64_t smem_desc_mn_sw128(uint32_t saddr, uint32_t 
     return d;
 }
 constexpr uint32_t kIdescMnMajorB = 1u << 16;  // B is MN-major (add to idesc_bf16_f32)
+constexpr uint32_t kIdescNegateA = 1u << 13;   // D = -A x B
 
 // Instruction descriptor for kind::f16 with bf16 A/B, fp32 D, both K-major.
 __host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N) {

@@ -10,13 +10,13 @@ import paper_2607_02501_gb300 as emb
 from tests.paged_util import Paged, dev_bf16, dev_i32, host
 
 pytestmark = pytest.mark.gpu
-# rounding of the value product's weights: bf16 hi + lo, within the oracle's allowance, up to 64 rows of queries
+# rounding of the value product's weights: bf16 hi + lo, within the oracle's allowance, up to 16 rows of queries
 # times heads per key/value head; one bf16 (2^-9, taken as 2^-8) above
 ONE_BF16 = 2.0 ** -8
 
 
 def _werr(new, H, Hk):
-    return ONE_BF16 if max(new) * (H // Hk) > 64 else 0.0
+    return ONE_BF16 if max(new) * (H // Hk) > 16 else 0.0
 
 
 CASES = [
@@ -166,6 +166,17 @@ def test_lengths_and_starts_beyond_the_buffers(cuda_device):
     ref, bound = oracle.paged_attention_reference(s.q, s.k, s.v, s.table, [0, 5, 5], s.kv, 4, s.scale)
     out = host(s.run(max_q=5))
     assert (np.abs(out - ref) <= bound)[:2].all()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("new", [1, 9, 130])
+@pytest.mark.parametrize("scale,cap", [(-0.1, 0.0), (-0.1, 3.0), (0.0, 0.0), (0.0, 5.0), (0.5, 1.0)])
+def test_scales_of_any_sign_and_tight_caps(cuda_device, d, new, scale, cap):
+    """A negative or zero scale; a cap so tight that a hidden key taken as -cap would show."""
+    s = Paged([new], [new + 150], 4, 2, d, 16, seed=18)
+    s.spoil_unused()
+    s.scale = scale
+    s.check(_werr([new], 4, 2), cap=cap, window=40)
 
 
 def test_strong_scores_and_large_gains(cuda_device):
