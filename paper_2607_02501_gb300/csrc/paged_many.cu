@@ -44,7 +44,20 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// Two fp32 FMAs and sums at once.
+__device__ __forceinline__ float min3(float a, float b, float c) {
+    float d;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// Two fp32 products, FMAs and sums at once.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "mul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     float2 d;
     asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
@@ -101,6 +114,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
     constexpr int kRows = 128 * NQ;
     using PL = PartLayout<D, kRows>;
     // what stands for the score of a key that a row does not see (a cap would make -infinity finite)
+    constexpr float kNearCap = 2.0f * 1.4426950408889634f * 0.35f;  // |scale q.k / cap| < 0.35, in units of scale2
     constexpr float kHidden = CAP ? -3.402823466e38f : -INFINITY;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t kv_full[S], kv_empty[S], q_full, q_empty, s_full[2], p_ready[2], o_done[2], o_free[2], drain;
@@ -337,6 +351,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 const int key0 = j * KT;
                 const bool edge = key0 < it.lo_all || key0 + KT > it.hi_all;
                 const int lo = keys.lo - key0, hi = keys.hi - key0;
+                float low = INFINITY;  // the lowest score that the row sees (for a cap)
                 if (edge) {
                     // scores that the row does not see, in tensor memory: rolled up and away from the path of most tiles
 #pragma unroll 1
@@ -346,7 +361,11 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                         ptx::tmem_ld_32(s_col + c, v);
                         ptx::tmem_ld_wait_32(v);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(c + e < lo || c + e >= hi ? kHidden : v[e]);
+                        for (int e = 0; e < 32; ++e) {
+                            const bool sees = c + e >= lo && c + e < hi;
+                            if (CAP && sees) low = fminf(low, v[e]);
+                            w[e] = __float_as_uint(sees ? v[e] : kHidden);
+                        }
                         ptx::tmem_st_32(s_col + c, w);
                     }
                     ptx::tmem_st_wait();
@@ -362,6 +381,14 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                     for (int e = 0; e < 32; e += 8)
 #pragma unroll
                         for (int k = 0; k < 4; ++k) top[k] = max3(top[k], s[c + e + k], s[c + e + 4 + k]);
+                }
+                if (CAP && !edge) {
+                    float l4[4] = {INFINITY, INFINITY, INFINITY, INFINITY};
+#pragma unroll
+                    for (int e = 0; e < KT; e += 8)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) l4[k] = min3(l4[k], s[e + k], s[e + 4 + k]);
+                    low = fminf(min3(l4[0], l4[1], l4[2]), l4[3]);
                 }
                 // (the maximum is of raw scores: a cap keeps their order)
                 const float mt = fmaxf(max3(top[0], top[1], top[2]), top[3]);
@@ -391,23 +418,45 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                         mc = -base2(m);
                     }
                 }
-                const float2 sc = make_float2(CAP ? 1.0f : p.scale2, CAP ? 1.0f : p.scale2), mm = make_float2(mc, mc);
+                // The weights, 32 at a time, over the scores. `base` gives two scores in base 2 less the row's maximum.
+                auto weights = [&](auto base) {
 #pragma unroll
-                for (int c = 0; c < KT; c += 32) {
-                    const float* v = s + c;
-                    uint32_t w[16];
+                    for (int c = 0; c < KT; c += 32) {
+                        uint32_t w[16];
 #pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        float2 u = make_float2(v[e], v[e + 1]);
-                        if constexpr (CAP)
-                            u = add2(make_float2(u.x == kHidden ? -INFINITY : base2(u.x), u.y == kHidden ? -INFINITY : base2(u.y)), mm);
-                        else u = fma2(u, sc, mm);
-                        u.x = exp2_fast(u.x);
-                        u.y = exp2_fast(u.y);
-                        l2[(e >> 1) & 1] = add2(l2[(e >> 1) & 1], u);
-                        w[e / 2] = pack_bf16x2(u.x, u.y);
+                        for (int e = 0; e < 32; e += 2) {
+                            float2 u = base(make_float2(s[c + e], s[c + e + 1]));
+                            u.x = exp2_fast(u.x);
+                            u.y = exp2_fast(u.y);
+                            l2[(e >> 1) & 1] = add2(l2[(e >> 1) & 1], u);
+                            w[e / 2] = pack_bf16x2(u.x, u.y);
+                        }
+                        ptx::tmem_st_16(s_col + c / 2, w);
                     }
-                    ptx::tmem_st_16(s_col + c / 2, w);
+                };
+                const float2 mm = make_float2(mc, mc);
+                if constexpr (!CAP) {
+                    const float2 sc = make_float2(p.scale2, p.scale2);
+                    weights([&](float2 u) { return fma2(u, sc, mm); });
+                } else if (__all_sync(all, mt == kHidden || fmaxf(fabsf(mt), fabsf(low)) * p.scale2 < kNearCap)) {
+                    // far below the cap tanh is its series to x^9 (the next term is 2.4e-7 of it at 0.35): one power of two
+                    // per score, where exponential and reciprocal take two more turns of the same unit. (The series runs away to
+                    // -infinity at what stands for a hidden score.)
+                    const float x1 = p.scale2 * (0.5f / 1.4426950408889634f), u1 = x1 * p.cap2;
+                    const float2 sx = make_float2(x1, x1), su = make_float2(u1, u1);
+                    weights([&](float2 u) {
+                        const float2 x = mul2(u, sx), y = mul2(x, x);
+                        auto k = [](float v) { return make_float2(v, v); };
+                        float2 t = fma2(y, k(62.0f / 2835.0f), k(-17.0f / 315.0f));
+                        t = fma2(t, y, k(2.0f / 15.0f));
+                        t = fma2(t, y, k(-1.0f / 3.0f));
+                        t = fma2(t, y, k(1.0f));
+                        return fma2(mul2(u, su), t, mm);
+                    });
+                } else {
+                    weights([&](float2 u) {
+                        return add2(make_float2(u.x == kHidden ? -INFINITY : base2(u.x), u.y == kHidden ? -INFINITY : base2(u.y)), mm);
+                    });
                 }
                 const bool tail = key0 + KT > it.q.L, hidden = key0 < it.lo_all || min(key0 + KT, it.q.L) > it.hi_all;
                 if ((tail || hidden) && t == (NQ == 2 && !(j >= sg.a[0] && j < sg.b[0]) ? 1 : 0)) {
