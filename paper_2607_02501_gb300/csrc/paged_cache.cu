@@ -15,14 +15,12 @@ namespace emb {
 namespace {
 
 // ------------------------------------------------------------------ block table, slots, positions
-// One launch. A CTA takes 1024 tokens and a share of the requests. Its 256 threads scan all the
+// One launch. A CTA takes 1024 tokens and a share of the requests. Its threads scan all the
 // requests' new tokens and new pages (a thread a run of requests, then shuffles), so no CTA waits for
 // another; a request that overlaps the CTA's tokens leaves its numbers in shared memory at its first token
 // there, and a maximum scan over those marks gives every token its request. A new page's table entry is written by
 // the token at the page's start, which is always new. Latency bounds it: two dependent loads, two scans.
-constexpr int kSlotThreads = 256;
-constexpr int kSlotPer = 4;  // consecutive tokens of a thread
-constexpr int kSlotTokens = kSlotThreads * kSlotPer;
+constexpr int kSlotTokens = 1024;
 
 struct PageDiv {
     uint32_t size;
@@ -39,17 +37,19 @@ __device__ __forceinline__ uint32_t warp_scan(uint32_t v, int lane) {
     return v;
 }
 
-__global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const __grid_constant__ SlotArgs p, PageDiv pd) {
+template <int NT>  // threads
+__global__ void __launch_bounds__(NT) paged_slots_kernel(const __grid_constant__ SlotArgs p, PageDiv pd) {
+    constexpr int kPer = kSlotTokens / NT;  // consecutive tokens of a thread
     // of the request whose first token of this CTA is token i: (request, position - token, last token + 1,
     // pages it had, index of its page 0 in the free list)
     __shared__ int mark[kSlotTokens];
     __shared__ uint32_t s_req[kSlotTokens], s_base[kSlotTokens], s_end[kSlotTokens], s_have[kSlotTokens], s_first[kSlotTokens];
-    __shared__ uint32_t sum_a[kSlotThreads / 32], sum_n[kSlotThreads / 32];
-    __shared__ int top[kSlotThreads / 32];
+    __shared__ uint32_t sum_a[NT / 32], sum_n[NT / 32];
+    __shared__ int top[NT / 32];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     ptx::griddep_launch_dependents();
 #pragma unroll
-    for (int i = 0; i < kSlotPer; ++i) mark[tid * kSlotPer + i] = 0;
+    for (int i = 0; i < kPer; ++i) mark[tid * kPer + i] = 0;
     ptx::griddep_wait();
     const uint32_t used = uint32_t(*p.used);
 
@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const __grid_
         const uint32_t full = pd.div(n);
         return min(full + (full * pd.size != n), max_pages);
     };
-    const int per = (p.n_req + kSlotThreads - 1) / kSlotThreads;
+    const int per = (p.n_req + NT - 1) / NT;
     const int r0 = min(p.n_req, tid * per), r1 = min(p.n_req, r0 + per);
     uint32_t a_sum = 0, n_sum = 0;
     for (int r = r0; r < r1; ++r) {
@@ -74,12 +74,12 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const __grid_
     __syncthreads();
     uint32_t start = a_in - a_sum, first = used + n_in - n_sum;
 #pragma unroll
-    for (int w = 0; w < kSlotThreads / 32; ++w)
+    for (int w = 0; w < NT / 32; ++w)
         if (w < warp) {
             start += sum_a[w];
             first += sum_n[w];
         }
-    if (blockIdx.x == 0 && tid == kSlotThreads - 1) {
+    if (blockIdx.x == 0 && tid == NT - 1) {
         p.q_start[p.n_req] = int32_t(start + a_sum);
         *p.used_out = int32_t(first + n_sum);
     }
@@ -109,13 +109,13 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const __grid_
     }
     __syncthreads();
 
-    int m[kSlotPer];
+    int m[kPer];
 #pragma unroll
-    for (int i = 0; i < kSlotPer; ++i) {
-        m[i] = mark[tid * kSlotPer + i];
+    for (int i = 0; i < kPer; ++i) {
+        m[i] = mark[tid * kPer + i];
         if (i > 0) m[i] = max(m[i], m[i - 1]);
     }
-    int incl = m[kSlotPer - 1];
+    int incl = m[kPer - 1];
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int u = __shfl_up_sync(0xffffffffu, incl, o);
@@ -126,14 +126,14 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const __grid_
     if (lane == 0) before = 0;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kSlotThreads / 32; ++w)
+    for (int w = 0; w < NT / 32; ++w)
         if (w < warp) before = max(before, top[w]);
 
-    int64_t slot[kSlotPer];
-    int32_t pos[kSlotPer];
+    int64_t slot[kPer];
+    int32_t pos[kPer];
 #pragma unroll
-    for (int i = 0; i < kSlotPer; ++i) {
-        const int64_t t = t0 + tid * kSlotPer + i;
+    for (int i = 0; i < kPer; ++i) {
+        const int64_t t = t0 + tid * kPer + i;
         const int at = max(m[i], before) - 1;
         slot[i] = -1;
         pos[i] = 0;
@@ -152,19 +152,21 @@ __global__ void __launch_bounds__(kSlotThreads) paged_slots_kernel(const __grid_
         }
         if (page >= 0) slot[i] = int64_t(page) * pd.size + in;
     }
-    const int64_t t = t0 + tid * kSlotPer;
-    if (t + kSlotPer <= t1 && ((uintptr_t(p.slots) | uintptr_t(p.positions)) & 15) == 0) {
-        *reinterpret_cast<longlong2*>(p.slots + t) = make_longlong2(slot[0], slot[1]);
-        *reinterpret_cast<longlong2*>(p.slots + t + 2) = make_longlong2(slot[2], slot[3]);
-        *reinterpret_cast<int4*>(p.positions + t) = make_int4(pos[0], pos[1], pos[2], pos[3]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kSlotPer; ++i)
-            if (t + i < t1) {
-                p.slots[t + i] = slot[i];
-                p.positions[t + i] = pos[i];
-            }
+    const int64_t t = t0 + tid * kPer;
+    if constexpr (kPer == 4) {
+        if (t + kPer <= t1 && ((uintptr_t(p.slots) | uintptr_t(p.positions)) & 15) == 0) {
+            *reinterpret_cast<longlong2*>(p.slots + t) = make_longlong2(slot[0], slot[1]);
+            *reinterpret_cast<longlong2*>(p.slots + t + 2) = make_longlong2(slot[2], slot[3]);
+            *reinterpret_cast<int4*>(p.positions + t) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+            return;
+        }
     }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (t + i < t1) {
+            p.slots[t + i] = slot[i];
+            p.positions[t + i] = pos[i];
+        }
 }
 
 // ------------------------------------------------------------------ norm, rotation, cache write
@@ -505,7 +507,10 @@ cudaError_t launch_paged_slots(const SlotArgs& a, cudaStream_t s) {
         if (a.page_size == 1 << i) pd.shift = i;
     void* args[] = {&p, &pd};
     const int64_t blocks = std::max<int64_t>(1, (a.n_tokens + kSlotTokens - 1) / kSlotTokens);
-    return launch_serialised(reinterpret_cast<const void*>(paged_slots_kernel), unsigned(blocks), kSlotThreads, 0, s, args);
+    // a thread a token while one CTA does, four in many CTAs
+    if (blocks == 1 && (a.n_tokens > 256 || a.n_req > 256))
+        return launch_serialised(reinterpret_cast<const void*>(paged_slots_kernel<1024>), 1, 1024, 0, s, args);
+    return launch_serialised(reinterpret_cast<const void*>(paged_slots_kernel<256>), unsigned(blocks), 256, 0, s, args);
 }
 
 cudaError_t launch_qk_norm_rope(const QkArgs& a, cudaStream_t s) {

@@ -291,9 +291,23 @@ __device__ __noinline__ PagedStretch paged_stretch_block(const PagedParams& p) {
 }
 // Up to 64 requests need no barrier (one decoded token over 867 keys: 4350 cycles by the block, a fifth of the call,
 // 1900 by a warp).
+// For one request of one block (a decoded token) there is nothing to scan.
+template <int KT>
+__device__ __forceinline__ PagedStretch paged_stretch_one(const PagedParams& p, const PagedReq& q) {
+    PagedItem it;
+    item_span<KT>(p, q, 0, it);
+    const uint32_t units = uint32_t(it.units), Hk = uint32_t(p.Hk);
+    return cut_stretch(p, units * Hk, units, Hk, [&](uint32_t x) {
+        const uint32_t g = Hk > 1 ? x / units : 0u, off = x - g * units;
+        return PagedPlace{0, int(g), 0, off, units - off};
+    });
+}
 template <int KT, int NT>
 __device__ __forceinline__ PagedStretch paged_stretch(const PagedParams& p) {
-    PagedStretch st = p.n_req == 1    ? paged_stretch_by<KT, 32, true>(p)
+    PagedReq q{0, 0, 0, 0};
+    if (p.n_req == 1) q = paged_req(p, 0);
+    PagedStretch st = q.n > 0 && q.n <= p.QB ? paged_stretch_one<KT>(p, q)
+                      : p.n_req == 1    ? paged_stretch_by<KT, 32, true>(p)
                       : p.n_req <= 64 ? paged_stretch_by<KT, 32>(p)
                                       : paged_stretch_block<KT, NT>(p);
     // In a form that the compiler knows to be uniform (as an item's numbers are): else its branches are not, and every
