@@ -75,6 +75,19 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     return d;
 }
 
+// A place of the ring and the parity of the turn it is in, carried along (a division per wait costs more than the wait).
+template <int S>
+struct RingPlace {
+    int slot = 0;
+    uint32_t turn = 0;
+    __device__ __forceinline__ void next() {
+        if (++slot == S) {
+            slot = 0;
+            turn ^= 1u;
+        }
+    }
+};
+
 // The part of an item that lies in this CTA's stretch: tiles [j0, j1), of which row tile t has [a[t], b[t]).
 template <int D>
 struct Segment {
@@ -164,9 +177,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
     auto wait = [&](uint64_t* bar, uint32_t phase) {
         return __all_sync(all, ptx::mbar_wait(bar, phase & 1, &abort_flag, p.status, kWaitLimitNs)) != 0;
     };
-    // the tiles of the stretch are numbered through; tile n has its keys in ring position 2 n, its values in 2 n + 1
-    auto slot_of = [](uint32_t pos) { return int(pos % uint32_t(S)); };
-    auto turn_of = [](uint32_t pos) { return pos / uint32_t(S); };
+    // the tiles of the stretch are numbered through; each has its keys in one place of the ring, its values in the next
 
     if (warp == T::kSoftWarps + 1) {
         // ---------------------------------------------------------------------- producer
@@ -174,7 +185,8 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         ptx::fence_proxy_async_global();  // (the cache and the queries were written by ordinary stores)
         const int page_size = 1 << p.page_shift, box = min(page_size, KT), n_box = KT / box;
         const int qt = p.QT;
-        uint32_t n = 0, loads = 0, items = 0;  // tiles; ring copies and items with queries issued
+        uint32_t loads = 0, items = 0;  // ring copies and items with queries issued
+        RingPlace<S> at;
         bool ok = true;
         while (x < st.x1 && ok) {
             const Segment<D> sg = segment_of<D>(p, r, g, b, off, x, st.x1);
@@ -206,14 +218,13 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 return page;
             };
             int page = page_of(sg.j0);
-            for (int j = sg.j0; j < sg.j1 && ok; ++j, ++n) {
+            for (int j = sg.j0; j < sg.j1 && ok; ++j) {
                 const int next = page_of(j + 1);
                 const int place = (j * KT) & (page_size - 1);
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
-                    const uint32_t pos = 2 * n + kv;
-                    const int s = slot_of(pos);
-                    if (turn_of(pos) > 0) ok = wait(&kv_empty[s], turn_of(pos) - 1);
+                    const int s = at.slot;
+                    if (loads >= uint32_t(S)) ok = wait(&kv_empty[s], at.turn ^ 1u);
                     if (!ok) break;
                     if (ptx::elect_one()) ptx::mbar_arrive_expect_tx(&kv_full[s], T::kSlot);
                     __syncwarp();
@@ -227,7 +238,8 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                         }
                         __syncwarp();
                     }
-                    loads = pos + 1;
+                    ++loads;
+                    at.next();
                 }
                 page = next;
             }
@@ -237,7 +249,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         }
         // every copy must land before this CTA's shared memory is released
         for (uint32_t i = loads > uint32_t(S) ? loads - S : 0; i < loads; ++i)
-            ptx::mbar_wait(&kv_full[slot_of(i)], turn_of(i) & 1, nullptr, p.status, kWaitLimitNs);
+            ptx::mbar_wait(&kv_full[i % S], (i / S) & 1, nullptr, p.status, kWaitLimitNs);
         if (items > 0) ptx::mbar_wait(&q_full, (items - 1) & 1, nullptr, p.status, kWaitLimitNs);
     } else if (warp == T::kSoftWarps) {
         // ------------------------------------------------------------------------- MMAs
@@ -245,11 +257,12 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         const uint32_t idesc_qk = ptx::idesc_bf16_f32(128, KT) | (p.negate ? ptx::kIdescNegateA : 0u), idesc_pv = ptx::idesc_bf16_f32(128, D) | ptx::kIdescMnMajorB;
         const uint32_t sq_u = ptx::smem_u32(sq), ring_u = ptx::smem_u32(ring);
         uint32_t n = 0, items = 0;
+        RingPlace<S> keys, values;  // of tile j, and of the tile before it
         uint32_t scores[2] = {0, 0}, owned[2] = {0, 0};  // score tiles by place, items with outputs by row tile
         bool ok = true;
         // (operands in a form that the compiler knows to be uniform: see ptx::elect_one)
-        auto qk = [&](int t, int place, uint32_t pos) {  // S[place] = Q[t] K^T
-            const uint32_t k = ptx::warp_uniform(ring_u + uint32_t(slot_of(pos) * T::kSlot));
+        auto qk = [&](int t, int place, int slot) {  // S[place] = Q[t] K^T
+            const uint32_t k = ptx::warp_uniform(ring_u + uint32_t(slot * T::kSlot));
             const uint32_t d = ptx::warp_uniform(tmem + uint32_t(place * KT));
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks)
@@ -257,8 +270,8 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                                  ptx::smem_desc_sw128(k + (ks / 4) * T::kSub) + 2 * (ks & 3), idesc_qk, ks != 0);
             ptx::mma_commit(&s_full[place]);
         };
-        auto pv = [&](int t, int place, uint32_t pos, bool first) {  // O[t] (+)= P[place] V
-            const uint64_t desc = ptx::smem_desc_mn_sw128(ptx::warp_uniform(ring_u + uint32_t(slot_of(pos) * T::kSlot)), T::kSub);
+        auto pv = [&](int t, int place, int slot, bool first) {  // O[t] (+)= P[place] V
+            const uint64_t desc = ptx::smem_desc_mn_sw128(ptx::warp_uniform(ring_u + uint32_t(slot * T::kSlot)), T::kSub);
             const uint32_t d = ptx::warp_uniform(tmem + uint32_t(T::kO + t * D)), a = ptx::warp_uniform(tmem + uint32_t(place * KT));
             const uint32_t more = ptx::warp_uniform(first ? 0u : 1u);
 #pragma unroll
@@ -271,17 +284,16 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
             if (sg.j1 > sg.j0) {
                 ok = wait(&q_full, items++);
                 for (int j = sg.j0; j <= sg.j1 && ok; ++j) {
-                    const uint32_t pos = 2 * n;  // of tile j's keys; the tile before has its values in pos - 1
-                    if (j < sg.j1) ok = wait(&kv_full[slot_of(pos)], turn_of(pos));
+                    if (j < sg.j1) ok = wait(&kv_full[keys.slot], keys.turn);
                     if (!ok) break;
                     ptx::tc_fence_after();
                     auto finish = [&](int t, int place) {  // P V of tile j - 1
                         const bool first = j - 1 == sg.a[t];
-                        ok = wait(&kv_full[slot_of(pos - 1)], turn_of(pos - 1)) && wait(&p_ready[place], scores[place] - 1);
+                        ok = wait(&kv_full[values.slot], values.turn) && wait(&p_ready[place], scores[place] - 1);
                         if (ok && first && owned[t] > 0) ok = wait(&o_free[t], owned[t] - 1);
                         if (!ok) return;
                         ptx::tc_fence_after();
-                        pv(t, place, pos - 1, first);
+                        pv(t, place, values.slot, first);
                         if (first) ++owned[t];
                     };
                     if constexpr (NQ == 2) {
@@ -290,22 +302,25 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                             if (j > sg.a[t] && j <= sg.b[t]) finish(t, t);
                             if (!ok) break;
                             if (j >= sg.a[t] && j < sg.b[t]) {
-                                qk(t, t, pos);
+                                qk(t, t, keys.slot);
                                 ++scores[t];
                             }
                         }
                     } else {
                         if (j < sg.j1) {
-                            qk(0, int(n & 1), pos);
+                            qk(0, int(n & 1), keys.slot);
                             ++scores[n & 1];
                         }
                         if (j > sg.j0) finish(0, int((n - 1) & 1));
                     }
                     if (!ok) break;
-                    if (j > sg.j0) ptx::mma_commit(&kv_empty[slot_of(pos - 1)]);
+                    if (j > sg.j0) ptx::mma_commit(&kv_empty[values.slot]);
                     if (j < sg.j1) {
-                        ptx::mma_commit(&kv_empty[slot_of(pos)]);
+                        ptx::mma_commit(&kv_empty[keys.slot]);
                         ++n;
+                        keys.next();
+                        values = keys;
+                        keys.next();
                         if (j == sg.j1 - 1) ptx::mma_commit(&q_empty);
                     }
                 }
@@ -464,8 +479,8 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                     // by their weights of 0 if they are not finite: such values leave the tile here and are added
                     // at the item's end for the rows that see them
                     const uint32_t pos = 2 * n + 1;
-                    wait(&kv_full[slot_of(pos)], turn_of(pos));
-                    uint4* v = reinterpret_cast<uint4*>(ring + slot_of(pos) * T::kSlot);
+                    wait(&kv_full[pos % uint32_t(S)], pos / uint32_t(S));
+                    uint4* v = reinterpret_cast<uint4*>(ring + (pos % uint32_t(S)) * T::kSlot);
                     uint32_t odd = 0;
                     // 16 bytes of one key at a time, whatever their dims
                     if (hidden) {
