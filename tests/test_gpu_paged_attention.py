@@ -55,6 +55,27 @@ def test_parity(cuda_device, new, kv, H, Hk, d, page, mask):
     s.check(_werr(new, H, Hk), prefix=prefix, what=f"{mask} new={new} kv={kv} H={H} Hk={Hk} d={d} page={page}", **kw)
 
 
+@pytest.mark.parametrize("R", [64, 65, 130, 400])
+@pytest.mark.parametrize("q_hi", [1, 3, 40])
+def test_many_requests(cuda_device, R, q_hi):
+    """More requests than a warp shares out by itself, some idle, some without keys."""
+    rng = np.random.default_rng(R + q_hi)
+    new = rng.integers(0, q_hi + 1, R)
+    kv = new + rng.integers(0, 90, R) * (rng.random(R) < 0.8)
+    new[0] = kv[0] = q_hi
+    s = Paged(new.tolist(), kv.tolist(), 8, 2, 64, 16, seed=R)
+    s.spoil_unused()
+    s.check(_werr([q_hi], 8, 2), pad=5)
+
+
+@pytest.mark.parametrize("d,H,new,kv", [(128, 8, 1, 20000), (64, 4, 2, 50000), (256, 2, 1, 9000), (128, 4, 20, 20000), (256, 8, 30, 6000)])
+def test_long_histories(cuda_device, d, H, new, kv):
+    """One item shared by as many CTAs as may join one."""
+    s = Paged([new], [kv], H, 1, d, 64, seed=kv)
+    s.check(_werr([new], H, 1))
+    s.check(_werr([new], H, 1), window=kv // 2, cap=30.0)
+
+
 @pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("window", [1, 2, 16, 63, 64, 65, 500])
 @pytest.mark.parametrize("new", [1, 5, 150])
