@@ -58,19 +58,23 @@ struct PagedAttnArgs {
 double paged_attention_tiles(const PagedAttnArgs& a);
 cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s);
 
-// A launch with programmatic stream serialisation.
+// A launch with programmatic stream serialisation, in clusters if `cluster` is above one.
 inline cudaError_t launch_serialised(const void* fn, unsigned grid, unsigned block, size_t smem, cudaStream_t s,
-                                     void** args) {
+                                     void** args, unsigned cluster = 1) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(block);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelExC(&cfg, fn, args);
 }
 

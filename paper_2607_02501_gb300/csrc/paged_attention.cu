@@ -32,10 +32,13 @@ __device__ __forceinline__ void ldsm_x4_trans(uint32_t saddr, uint32_t (&r)[4]) 
 // four warps compute. An item has 16 rows (queries times heads), every warp takes 16 of a tile's keys, and the
 // warps' results are merged at the item's end. Scores, softmax in base 2 with a running maximum and the value
 // product (weights as bf16 hi + lo) stay in registers. HBM bounds it: the cache is read once for the 16 rows.
+// CL: for few and short requests a cluster of CTAs takes a request's key/value head and shares out its tiles, and
+// the results are joined through distributed shared memory: no search for the work, no workspace.
 constexpr int kFewWarps = 4;
 constexpr int kFewThreads = 32 * (kFewWarps + 1);
 constexpr int kFewTile = 64;
 constexpr int kFewRows = 16;
+constexpr int kFewCluster = 8;  // CTAs of a cluster, at most (the portable size)
 
 template <int D>
 struct FewTraits {
@@ -44,10 +47,12 @@ struct FewTraits {
     static constexpr int kCtas = D == 256 ? 1 : 2;   // per SM
     static constexpr int kQPitch = D + 8;            // queries in shared memory (D = 256), bf16 per padded row
     static constexpr int kQBytes = D == 256 ? kFewRows * kQPitch * 2 : 0;
+    static constexpr int kFinPitch = D + 4;          // a CTA's result for its cluster, fp32 per padded row
     static constexpr int kSmem = 1024 + kStages * kStage + kQBytes;
+    static constexpr int kSmemCluster = kSmem + kFewRows * (kFinPitch + 2) * 4;
 };
 
-template <int D, bool CAP>
+template <int D, bool CAP, bool CL>
 __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_kernel(const __grid_constant__ PagedParams p) {
     using T = FewTraits<D>;
     constexpr int KS = D / 16, NT = D / 8, NJ = kFewTile / 8 / kFewWarps, ROWS = kFewRows;
@@ -80,19 +85,29 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
         uint32_t page;
         asm volatile("ld.global.u32 %0, [%1];" : "=r"(page) : "l"(p.table + lane * 32));
     }
-    const PagedStretch st = paged_stretch<kFewTile, kFewThreads>(p);
-
-    int r = st.r, g = st.g, b = st.b;
+    PagedStretch st{};
+    int r, g, b = 0, blocks = 0;
+    const int S = CL ? p.cluster : 1, rank = CL ? int(blockIdx.x) % S : 0;
+    if constexpr (CL) {
+        r = int(blockIdx.x) / S / p.Hk;
+        g = int(blockIdx.x) / S % p.Hk;
+        blocks = (ptx::warp_uniform(paged_req(p, r).n) + p.QB - 1) / p.QB;
+    } else {
+        st = paged_stretch<kFewTile, kFewThreads>(p);
+        r = st.r;
+        g = st.g;
+        b = st.b;
+    }
     uint32_t x = st.x0, off = st.off;
     uint32_t issued = 0;  // tiles so far (ring position and phase)
     if (warp == kFewWarps) {
         // -------------------------------------------------------------------- producer
         ptx::fence_proxy_async_global();  // (the cache was written by ordinary stores)
         const int page_size = 1 << p.page_shift, box = min(page_size, kFewTile), n_box = kFewTile / box;
-        while (x < st.x1) {
+        while (CL ? b < blocks : x < st.x1) {
             const PagedItem it = paged_item<kFewTile>(p, r, g, b);
             const uint32_t take = min(st.x1 - x, uint32_t(it.units) - off);
-            const int j1 = min(int(off + take), it.nt);
+            const int j0 = CL ? rank * it.nt / S : int(off), j1 = CL ? (rank + 1) * it.nt / S : min(int(off + take), it.nt);
             const int32_t* row = p.table + int64_t(r) * p.max_pages;
             // lane i looks up the page of the tile's box i; boxes that no query sees, and pages that do not
             // exist, are fetched from behind the cache: zeros
@@ -105,8 +120,8 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
                 }
                 return page;
             };
-            int page = page_of(int(off));
-            for (int j = int(off); j < j1; ++j, ++issued) {
+            int page = page_of(j0);
+            for (int j = j0; j < j1; ++j, ++issued) {
                 const int next = page_of(j + 1);
                 const int s = issued % T::kStages;
                 if (issued >= uint32_t(T::kStages))
@@ -132,9 +147,15 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
                 }
                 page = next;
             }
-            x += take;
-            off = 0;
-            if (x < st.x1) next_item(p, r, g, b, it.q.n);
+            if constexpr (CL) {
+                ptx::cluster_sync();  // (the compute warps' two)
+                ptx::cluster_sync();
+                ++b;
+            } else {
+                x += take;
+                off = 0;
+                if (x < st.x1) next_item(p, r, g, b, it.q.n);
+            }
         }
         // every copy must land before this CTA's shared memory is released
         if (!abort_flag)
@@ -152,12 +173,14 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
     const int wkey = warp * 16;  // the warp's keys of a tile
     const uint32_t ring_u = ptx::smem_u32(ring);
     __nv_bfloat16* sq = reinterpret_cast<__nv_bfloat16*>(ring + T::kStages * T::kStage);
+    float* fin = reinterpret_cast<float*>(ring + T::kStages * T::kStage + T::kQBytes);  // [rows][pitch], CL only
+    float *fin_m = fin + ROWS * T::kFinPitch, *fin_l = fin_m + ROWS;
     int joins = 0;
 
-    while (x < st.x1) {
+    while (CL ? b < blocks : x < st.x1) {
         const PagedItem it = paged_item<kFewTile>(p, r, g, b);
         const uint32_t take = min(st.x1 - x, uint32_t(it.units) - off);
-        const int j0 = int(off), j1 = min(int(off + take), it.nt);
+        const int j0 = CL ? rank * it.nt / S : int(off), j1 = CL ? (rank + 1) * it.nt / S : min(int(off + take), it.nt);
         // this thread's two rows: query and head, keys they see
         const int rA = quad, rB = rA + 8, iA = rA / p.G, iB = rB / p.G;
         const bool okA = iA < it.nq, okB = iB < it.nq;
@@ -427,6 +450,62 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
             if (lane == 0) ptx::mbar_arrive(&empty[s]);
         }
 
+        if constexpr (CL) {
+            // every CTA of the cluster lays down its result, and each adds up its share of the outputs, in CTA order
+            if (qc == 0 && warp == 0) {
+                fin_m[quad] = mA;
+                fin_m[quad + 8] = mB;
+                fin_l[quad] = lA;
+                fin_l[quad + 8] = lB;
+            }
+#pragma unroll
+            for (int n = 0; n < kMine; ++n) {
+                const int c = (n0 + n) * 8 + 2 * qc;
+                *reinterpret_cast<float2*>(fin + quad * T::kFinPitch + c) = make_float2(o[n][0], o[n][1]);
+                *reinterpret_cast<float2*>(fin + (quad + 8) * T::kFinPitch + c) = make_float2(o[n][2], o[n][3]);
+            }
+            __syncwarp();
+            ptx::cluster_sync();
+            for (int e = rank * 32 * kFewWarps + int(threadIdx.x); e < it.nq * p.G * (D / 4); e += S * 32 * kFewWarps) {
+                const int row = e / (D / 4), c = e % (D / 4) * 4;
+                float m[kFewCluster], l[kFewCluster], M = -INFINITY, L = 0.0f;
+                float4 v[kFewCluster], a = make_float4(0, 0, 0, 0);
+                const uint32_t am = ptx::smem_u32(fin_m + row), al = ptx::smem_u32(fin_l + row);
+                const uint32_t av = ptx::smem_u32(fin + row * T::kFinPitch + c);
+#pragma unroll
+                for (int q = 0; q < kFewCluster; ++q) {
+                    m[q] = -INFINITY;
+                    l[q] = 0.0f;
+                    v[q] = make_float4(0, 0, 0, 0);
+                    if (q < S) {
+                        m[q] = ptx::ld_dsmem_f32(ptx::map_dsmem(am, q));
+                        l[q] = ptx::ld_dsmem_f32(ptx::map_dsmem(al, q));
+                        v[q] = ptx::ld_dsmem_f32x4(ptx::map_dsmem(av, q));
+                    }
+                    M = fmaxf(M, m[q]);
+                }
+                const float z = M == -INFINITY ? 0.0f : M;
+#pragma unroll
+                for (int q = 0; q < kFewCluster; ++q) {
+                    // weight 0 of a result without a finite score: its sums are 0, or NaN, which has to show
+                    const float w = exp2_fast(m[q] - z);
+                    L = fmaf(l[q], w, L);
+                    a.x = fmaf(v[q].x, w, a.x);
+                    a.y = fmaf(v[q].y, w, a.y);
+                    a.z = fmaf(v[q].z, w, a.z);
+                    a.w = fmaf(v[q].w, w, a.w);
+                }
+                const float inv = L == 0.0f ? 0.0f : __fdiv_rn(1.0f, L);
+                uint2 u;
+                u.x = pack_bf16x2(__fmul_rn(a.x, inv), __fmul_rn(a.y, inv));
+                u.y = pack_bf16x2(__fmul_rn(a.z, inv), __fmul_rn(a.w, inv));
+                *reinterpret_cast<uint2*>(p.O + row_of(row / p.G, row) + c) = u;
+            }
+            __syncwarp();
+            ptx::cluster_sync();  // remote shared memory must outlive its readers
+            ++b;
+            continue;
+        }
         const bool whole = off == 0 && take == uint32_t(it.units);
         if (whole) {
             const float iv = lA == 0.0f ? 0.0f : __fdiv_rn(1.0f, lA), iw = lB == 0.0f ? 0.0f : __fdiv_rn(1.0f, lB);
@@ -546,9 +625,11 @@ cudaError_t few_resident(int& ctas) {
         ctas = known[dev];
         return cudaSuccess;
     }
-    auto* kernel = paged_few_kernel<D, CAP>;
+    auto* kernel = paged_few_kernel<D, CAP, false>;
     int per_sm = 0;
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FewTraits<D>::kSmem);
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(paged_few_kernel<D, CAP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewTraits<D>::kSmemCluster);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kFewThreads, FewTraits<D>::kSmem);
     if (e != cudaSuccess) return e;
     // a partial result per item border: two per CTA, within the workspace
@@ -557,6 +638,18 @@ cudaError_t few_resident(int& ctas) {
     ctas = std::max(1, std::min({std::max(1, per_sm) * std::max(1, device_sm_count()), fit, int(kPagedFlagBytes / 4)}));
     if (dev >= 0 && dev < 64) known[dev] = ctas;
     return cudaSuccess;
+}
+
+// CTAs of a cluster for a request's key/value head, or 0 where equal stretches of all the work are sooner done: a cluster
+// keeps its CTAs for the longest request that the table has room for, stretches take their share of the total and a join
+// worth eight tiles. Measured (us, stretches and clusters): one token of 8 heads on one of 128 over 867 keys 7.6 and 5.9,
+// 3000 9.5 and 8.8, 6000 10.8 and 12.8; 32 heads on 8 over 4000 13.9 and 10.4; 8 requests of them over 900 16.7 and 8.9;
+// 32 requests on one over up to 1500 14.7 and 8.1.
+int few_cluster(const PagedAttnArgs& a, int ctas) {
+    const double items = double(a.n_req * a.n_kv_heads), tiles = std::ceil(double(a.max_pages * a.page_size) / kFewTile);
+    int S = kFewCluster;
+    while (S > 1 && items * S > ctas) S /= 2;
+    return S > 1 && tiles <= 16.0 * S && tiles / S <= items * tiles / ctas + 8.0 ? S : 0;
 }
 
 template <int D, bool CAP>
@@ -568,9 +661,13 @@ cudaError_t launch_few(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
     const uint32_t box = uint32_t(std::min<int64_t>(a.page_size, kFewTile));
     if (!encode_cache(&p.k_map, a.k_cache, a, box) || !encode_cache(&p.v_map, a.v_cache, a, box)) return cudaErrorInvalidValue;
     void* args[] = {&p};
+    p.cluster = few_cluster(a, ctas);
+    if (p.cluster > 0)
+        return launch_serialised(reinterpret_cast<const void*>(paged_few_kernel<D, CAP, true>), unsigned(a.n_req * a.n_kv_heads * p.cluster),
+                                 kFewThreads, FewTraits<D>::kSmemCluster, s, args, unsigned(p.cluster));
     const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, kFewTile))));
     set_grid(p, grid, 3);
-    return launch_serialised(reinterpret_cast<const void*>(paged_few_kernel<D, CAP>), grid, kFewThreads, FewTraits<D>::kSmem, s, args);
+    return launch_serialised(reinterpret_cast<const void*>(paged_few_kernel<D, CAP, false>), grid, kFewThreads, FewTraits<D>::kSmem, s, args);
 }
 
 template <int D>
