@@ -20,7 +20,8 @@
  *
  * Conventions are those of emb_qmm.h (device pointers owned by the caller, no allocation, no
  * host synchronisation, argument errors before anything is enqueued, programmatic dependent
- * launch; calls can be recorded with emb_chain_record_begin). Lengths, tables, slots and
+ * launch; calls can be recorded with emb_chain_record_begin). Like the norm, rotary and attention calls of
+ * emb_qmm.h, they let the next launch start while work ahead of them may still run (emb_qlayer_seq_chained). Lengths, tables, slots and
  * positions are read on the device, so a recorded call follows them from replay to replay.
  * What they hold cannot fault: each entry point says what an impossible value does.
  */
@@ -107,7 +108,7 @@ EMB_API emb_status emb_qk_norm_rope(const uint16_t* q, int64_t q_stride, const u
  * that element of its queries' outputs infinite or NaN. The scores are held in base 2 (scale *
  * log2(e) rounded to fp32 once), the weights by the hardware's power of two (relative error about 2^-22; below 2^-126 of
  * the largest they are zero). Up to 16 query rows (max_q queries times heads per key/value head), the
- * weights enter the value product as bf16 hi + lo (2^-16); above, rounded once to bf16 (2^-9 each).
+ * weights enter the value product as bf16 hi + lo (2^-16); above, they may be rounded once to bf16 (2^-9 each).
  * kv_len above max_pages * page_size counts as that; q_start past n_tokens as n_tokens, and a decreasing
  * q_start as no queries; a page id outside [0, n_pages) as a page of zeros. Rows of O from q_start[n_req] to
  * n_tokens (padding) are zeroed.

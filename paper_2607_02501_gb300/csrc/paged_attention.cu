@@ -39,6 +39,7 @@ constexpr int kFewThreads = 32 * (kFewWarps + 1);
 constexpr int kFewTile = 64;
 constexpr int kFewRows = 16;
 constexpr int kFewCluster = 8;  // CTAs of a cluster, at most (the portable size)
+constexpr double kFewLongest = 16.0;  // tiles of a CTA of a cluster
 
 template <int D>
 struct FewTraits {
@@ -89,8 +90,10 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
     int r, g, b = 0, blocks = 0;
     const int S = CL ? p.cluster : 1, rank = CL ? int(blockIdx.x) % S : 0;
     if constexpr (CL) {
-        r = int(blockIdx.x) / S / p.Hk;
-        g = int(blockIdx.x) / S % p.Hk;
+        const int id = int(blockIdx.x) / S;
+        b = id % p.side;
+        g = id / p.side % p.Hk;
+        r = id / p.side / p.Hk;
         blocks = (ptx::warp_uniform(paged_req(p, r).n) + p.QB - 1) / p.QB;
     } else {
         st = paged_stretch<kFewTile, kFewThreads>(p);
@@ -150,7 +153,7 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
             if constexpr (CL) {
                 ptx::cluster_sync();  // (the compute warps' two)
                 ptx::cluster_sync();
-                ++b;
+                b += p.side;
             } else {
                 x += take;
                 off = 0;
@@ -503,7 +506,7 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
             }
             __syncwarp();
             ptx::cluster_sync();  // remote shared memory must outlive its readers
-            ++b;
+            b += p.side;
             continue;
         }
         const bool whole = off == 0 && take == uint32_t(it.units);
@@ -640,16 +643,24 @@ cudaError_t few_resident(int& ctas) {
     return cudaSuccess;
 }
 
-// CTAs of a cluster for a request's key/value head, or 0 where equal stretches of all the work are sooner done: a cluster
-// keeps its CTAs for the longest request that the table has room for, stretches take their share of the total and a join
-// worth eight tiles. Measured (us, stretches and clusters): one token of 8 heads on one of 128 over 867 keys 7.6 and 5.9,
-// 3000 9.5 and 8.8, 6000 10.8 and 12.8; 32 heads on 8 over 4000 13.9 and 10.4; 8 requests of them over 900 16.7 and 8.9;
-// 32 requests on one over up to 1500 14.7 and 8.1.
-int few_cluster(const PagedAttnArgs& a, int ctas) {
-    const double items = double(a.n_req * a.n_kv_heads), tiles = std::ceil(double(a.max_pages * a.page_size) / kFewTile);
+// Blocks of a request's queries that its clusters take side by side.
+int few_blocks(const PagedAttnArgs& a) {
+    const int64_t qb = kFewRows / (a.n_heads / a.n_kv_heads);
+    return int((std::min(a.max_q, a.n_tokens) + qb - 1) / qb);
+}
+// CTAs of the cluster that takes a block, or 0 where equal stretches of all the work are sooner done: a cluster keeps its
+// CTAs for the longest request that the table has room for, stretches take their share of the total and a join worth eight
+// tiles. Measured (us, stretches and clusters): one token of 8 heads on one of 128 over 867 keys 7.6 and 5.9, 3000 9.5 and
+// 8.8, 6000 10.8 and 12.8; 32 heads on 8 over 4000 13.9 and 10.4; 8 requests of them over 900 16.7 and 8.9; 32 requests on
+// one over up to 1500 14.7 and 8.1.
+int few_cluster(const PagedAttnArgs& a) {
+    double keys = double(a.max_pages * a.page_size);
+    if (a.window > 0) keys = std::min(keys, double(a.window) + kFewRows + kFewTile);
+    const double items = double(a.n_req * a.n_kv_heads) * few_blocks(a), tiles = std::ceil(keys / kFewTile);
+    const double ctas = (a.head_dim == 256 ? 1.0 : 2.0) * std::max(1, device_sm_count());
     int S = kFewCluster;
-    while (S > 1 && items * S > ctas) S /= 2;
-    return S > 1 && tiles <= 16.0 * S && tiles / S <= items * tiles / ctas + 8.0 ? S : 0;
+    while (S > 0 && items * S > ctas) S /= 2;
+    return S > 0 && tiles <= kFewLongest * S && tiles / S <= items * tiles / ctas + 8.0 ? S : 0;
 }
 
 template <int D, bool CAP>
@@ -661,9 +672,10 @@ cudaError_t launch_few(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
     const uint32_t box = uint32_t(std::min<int64_t>(a.page_size, kFewTile));
     if (!encode_cache(&p.k_map, a.k_cache, a, box) || !encode_cache(&p.v_map, a.v_cache, a, box)) return cudaErrorInvalidValue;
     void* args[] = {&p};
-    p.cluster = few_cluster(a, ctas);
+    p.side = few_blocks(a);
+    p.cluster = few_cluster(a);
     if (p.cluster > 0)
-        return launch_serialised(reinterpret_cast<const void*>(paged_few_kernel<D, CAP, true>), unsigned(a.n_req * a.n_kv_heads * p.cluster),
+        return launch_serialised(reinterpret_cast<const void*>(paged_few_kernel<D, CAP, true>), unsigned(a.n_req * a.n_kv_heads * p.side * p.cluster),
                                  kFewThreads, FewTraits<D>::kSmemCluster, s, args, unsigned(p.cluster));
     const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, kFewTile))));
     set_grid(p, grid, 3);
@@ -706,9 +718,12 @@ cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s) {
     constexpr double kLog2e = 1.4426950408889634;
     p.scale2 = a.cap > 0.0f ? float(2.0 * kLog2e * double(a.scale) / double(a.cap)) : float(kLog2e * double(a.scale));
     p.cap2 = float(kLog2e * double(a.cap));
-    // More rows than a warp's 16 go to the tcgen05 kernel. (A kernel of this kind with 64 rows, 16 per warp, was the
-    // sooner of the two by 6 % over 200 calls with heads of 64, and slower by 61 and 120 % with heads of 128 and 256.)
-    if (p.G > 16 || a.max_q * p.G > 16) {
+    // Up to 16 rows of a request go to the mma.sync kernel, and more where all its blocks of 16 have a cluster at once: such
+    // calls are small, and it has them sooner done (us, tcgen05 and mma.sync: 50 queries of 8 heads over 866 keys 11.3
+    // and 8.5, 8 over 816 10.3 and 6.8, 24 requests of 3 queries of 14 heads on 2 of 64 12.1 and 7.6, 280 of 8 heads of 64 alone
+    // 10.0 and 6.7). The rest goes to the tcgen05 kernel.
+    const bool few = p.G <= 16 && (a.max_q * p.G <= 16 || few_cluster(a) > 0);
+    if (!few) {
         p.negate = a.scale < 0.0f;
         p.scale2 = std::max(std::fabs(p.scale2), 1e-37f);  // (hidden scores are -infinity times this)
         return launch_paged_many(p, a, s);

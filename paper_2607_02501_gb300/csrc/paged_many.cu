@@ -659,7 +659,7 @@ cudaError_t launch_many(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) 
     const int ctas = std::max(1, std::min({sms, fit, int(kPagedFlagBytes / 4)}));
     void* args[] = {&p};
     const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, T::KT))));
-    set_grid(p, grid, D == 256 ? 8 : 4);
+    set_grid(p, grid, D == 256 ? 8 : 2);
 
     return launch_serialised(reinterpret_cast<const void*>(paged_many_kernel<D, CAP>), grid, T::kThreads, T::kSmem, s, args);
 }

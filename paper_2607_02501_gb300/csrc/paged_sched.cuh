@@ -34,7 +34,7 @@ struct PagedParams {
     int64_t max_pages;
     int n_tokens, n_req, n_pages, page_shift, kv_limit, window;
     int H, Hk, G, QB, QT;  // heads, those of one key/value head; queries of an item and of a row tile
-    int cluster;           // CTAs that share a request's key/value head (few rows), or 0
+    int cluster, side;     // few rows: CTAs of a cluster, or 0; clusters of a request's key/value head, for its blocks
     bool negate;           // the scale is negative: its magnitude is in scale2
     uint32_t join_units;  // units that joining a cut item costs
     uint32_t grid_inv;  // ceil(2^32 / grid)

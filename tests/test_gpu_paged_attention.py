@@ -16,7 +16,15 @@ ONE_BF16 = 2.0 ** -8
 
 
 def _werr(new, H, Hk):
-    return ONE_BF16 if max(new) * (H // Hk) > 16 else 0.0
+    return ONE_BF16 if Paged.many or max(new) * (H // Hk) > 16 else 0.0
+
+
+@pytest.fixture(params=["small", "many"], autouse=True)
+def kernel(request):
+    """Every test by the kernel that its sizes take, and by the one for many rows."""
+    Paged.many = request.param == "many"
+    yield request.param
+    Paged.many = False
 
 
 CASES = [
@@ -177,6 +185,7 @@ def test_reproducible_padded_and_any_hint(cuda_device, new, kv, H, Hk, d):
 def test_lengths_and_starts_beyond_the_buffers(cuda_device):
     """kv_len past the table's row counts as the row's end, starts past n_tokens as n_tokens."""
     s = Paged([2, 3], [64, 64], 4, 2, 128, 16, seed=12)
+    s.many = False  # (no padding: the starts are to pass the tokens)
     s.kv = [64, 64 + 500]
     s.q_start = np.array([0, 2, 5 + 90])
     a = host(s.run())
@@ -220,25 +229,32 @@ def test_growing_scores(cuda_device):
         s.check(_werr([new], 2, 1), prefix=[1200])
 
 
+def _rows_and_hint(s, new):
+    """Queries on the device and the hint, padded as Paged.run pads them."""
+    pad = 6000 if Paged.many else 0
+    return dev_bf16(np.concatenate([s.q, np.zeros((pad, s.q.shape[1]), dtype=np.float32)])), pad or new
+
+
 @pytest.mark.parametrize("new", [1, 20, 130])
 def test_recorded_call_follows_its_lengths(cuda_device, new):
     """A recorded call reads lengths, table and queries at every replay."""
     s = Paged([new, new], [new + 600, new + 40], 4, 2, 128, 16, seed=15)
-    q, k, v, tab, qs = dev_bf16(s.q), dev_bf16(s.k), dev_bf16(s.v), dev_i32(s.table), dev_i32(s.q_start)
+    q, hint = _rows_and_hint(s, new)
+    k, v, tab, qs = dev_bf16(s.k), dev_bf16(s.v), dev_i32(s.table), dev_i32(s.q_start)
     kv = dev_i32(s.kv)
-    O = torch.empty(s.T, 4 * 128, dtype=torch.bfloat16, device="cuda")
+    O = torch.empty_like(q)
     ws = emb.paged_workspace()
     stream = torch.cuda.Stream()
     torch.cuda.synchronize()
     with emb.Recording(stream, keep=[q, k, v, tab, qs, kv, O, ws]) as rec:
-        emb.emb_paged_attention(q, k, v, tab, qs, kv, O, s.scale, new, ws, stream=stream)
+        emb.emb_paged_attention(q, k, v, tab, qs, kv, O, s.scale, hint, ws, stream=stream)
     for lens in ([new + 600, new + 40], [new, new + 39], [new + 300, new]):
         s.kv = lens
         with torch.cuda.stream(stream):
             kv.copy_(dev_i32(lens))
             rec.launch(stream)
         torch.cuda.synchronize()
-        assert torch.equal(O, s.run())
+        assert torch.equal(O[:s.T], s.run())
     rec.close()
 
 
@@ -259,10 +275,11 @@ def test_cache_beyond_32_bits(cuda_device, new):
     far = np.array([[n_pages - 1 - 3 * i for i in range(n)]])
     for i in range(n):
         kc[far[0, i]], vc[far[0, i]] = dev_bf16(s.k[s.table[0, i]]), dev_bf16(s.v[s.table[0, i]])
-    O = torch.empty(s.T, Hk * d, dtype=torch.bfloat16, device="cuda")
-    emb.emb_paged_attention(dev_bf16(s.q), kc, vc, dev_i32(far), dev_i32(s.q_start), dev_i32(s.kv), O, s.scale, new,
+    q, hint = _rows_and_hint(s, new)
+    O = torch.empty_like(q)
+    emb.emb_paged_attention(q, kc, vc, dev_i32(far), dev_i32(s.q_start), dev_i32(s.kv), O, s.scale, hint,
                             emb.paged_workspace())
-    assert torch.equal(O, s.run())
+    assert torch.equal(O[:s.T], s.run())
     # and the cache write reaches them
     slots = torch.tensor([(n_pages - 1) * page + 7], dtype=torch.int64, device="cuda")
     x = torch.randn(1, Hk * d, device="cuda").to(torch.bfloat16)

@@ -101,13 +101,19 @@ def test_every_step_against_the_oracle(cuda_device):
                                                           77, 2.0 ** -8), "attention")
 
 
-@pytest.mark.parametrize("heads,kv_heads,max_q,kernel", [(8, 1, 2, "paged_few_kernel"), (8, 1, 3, "paged_many_kernel"),
-                                                         (16, 1, 1, "paged_few_kernel"), (17, 1, 1, "paged_many_kernel")])
-def test_which_kernel_a_call_takes(cuda_device, heads, kv_heads, max_q, kernel):
-    T = 6
+@pytest.mark.parametrize("heads,kv_heads,tokens,requests,kernel,clusters", [
+    (8, 1, 2, 1, "paged_few_kernel", 1), (16, 1, 1, 1, "paged_few_kernel", 1),          # up to 16 rows of a request
+    (8, 1, 50, 1, "paged_few_kernel", 1), (14, 2, 7, 1, "paged_few_kernel", 1),         # more, where all blocks have a cluster
+    (8, 8, 1, 400, "paged_few_kernel", 0),                                              # one token of many requests: stretches
+    (17, 1, 1, 1, "paged_many_kernel", 0), (8, 1, 3000, 1, "paged_many_kernel", 0)])
+def test_which_kernel_a_call_takes(cuda_device, heads, kv_heads, tokens, requests, kernel, clusters):
+    T = tokens * requests
     q = torch.zeros(T, heads * 64, dtype=torch.bfloat16, device="cuda")
     cache = torch.zeros(4, 16, kv_heads, 64, dtype=torch.bfloat16, device="cuda")
-    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
-    args = (q, cache, cache, ints(0, 1)[None], ints(0, T), ints(20), torch.empty_like(q), 0.1, max_q, emb.paged_workspace())
+    i32 = dict(dtype=torch.int32, device="cuda")
+    table, start, kv = torch.zeros(requests, 60, **i32), torch.arange(requests + 1, **i32) * tokens, torch.full((requests,), 900, **i32)
+    args = (q, cache, cache, table, start, kv, torch.empty_like(q), 0.1, tokens, emb.paged_workspace())
     got = launches(lambda: emb.emb_paged_attention(*args))
     assert [g[0] for g in got] == [kernel]
+    if kernel == "paged_few_kernel":
+        assert got[0][1][-1] == clusters  # the last template argument
