@@ -154,6 +154,20 @@ def paged_lib():
     return L
 
 
+_marshal = None
+
+
+def _binding():
+    """The module that marshals the paged-cache calls, bound to the library's entry points."""
+    global _marshal
+    if _marshal is None:
+        L = paged_lib()
+        from . import _paged_binding as m
+        m.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.emb_paged_slots, L.emb_qk_norm_rope, L.emb_paged_attention)))
+        _marshal = m
+    return _marshal
+
+
 def declared_symbols() -> list:
     """Names of every entry point declared in include/emb_qmm.h."""
     with open(HEADER_PATH) as fh:
@@ -393,18 +407,13 @@ def emb_attention(Q, K0, V0, K1, V1, O, n_heads: int, n_kv_heads: int, head_dim:
            "emb_attention")
 
 
-# (these are called once per step or layer on the smallest steps too: bound functions and one status test)
-
 def emb_paged_slots(cached, added, free_pages, used, table, q_start, kv_len, slots, positions, used_out,
                     page_size: int, stream=None) -> None:
     """cached, added: int32 [R]; free_pages: int32 [n_free]; used, used_out: int32 [1]; table: int32
     [R][max_pages], filled on; out: q_start int32 [R + 1], kv_len int32 [R], slots int64 [T], positions
     int32 [T]."""
-    R, max_pages = table.shape
-    status = (_paged or paged_lib()).emb_paged_slots(
-        cached.data_ptr(), added.data_ptr(), R, free_pages.data_ptr(), free_pages.shape[0], used.data_ptr(), page_size,
-        table.data_ptr(), max_pages, q_start.data_ptr(), kv_len.data_ptr(), slots.data_ptr(), positions.data_ptr(),
-        slots.shape[0], used_out.data_ptr(), _stream(stream))
+    status = (_marshal or _binding()).slots(cached, added, free_pages, used, table, q_start, kv_len, slots, positions,
+                                            used_out, page_size, _stream(stream))
     if status:
         raise EmbError(status, "emb_paged_slots")
 
@@ -415,20 +424,9 @@ def emb_qk_norm_rope(q, k, v, q_out, k_cache, v_cache, slots, positions, q_gamma
     """q: bf16 [T][H * d], k, v: bf16 [T][Hk * d] (rows may be strided); q_out: bf16 [T][H * d]; caches:
     bf16 [n_pages][page_size][Hk][d]; slots: int64 [T]; positions: int32 [T] or [n_axes][T]; gammas: fp32
     [d]; axis_of_pair: bytes or integers [rot_dim / 2]; rot_dim: d by default."""
-    n_pages, page_size, Hk, d = k_cache.shape
-    T, width = q.shape
-    shape = positions.shape
-    axes, pos_stride = (1, T) if len(shape) == 1 else (shape[0], positions.stride(0))
-    rot = d if rot_dim is None else rot_dim
-    if axis_of_pair is not None:
-        axis_of_pair = bytes(axis_of_pair)
-        if len(axis_of_pair) != rot // 2:
-            raise EmbError(EMB_EINVAL, "emb_qk_norm_rope: axis_of_pair")
-    status = (_paged or paged_lib()).emb_qk_norm_rope(
-        q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0), T, width // d, Hk, d,
-        None if q_gamma is None else q_gamma.data_ptr(), None if k_gamma is None else k_gamma.data_ptr(), eps,
-        positions.data_ptr(), pos_stride, axes, axis_of_pair, rot, base, slots.data_ptr(), q_out.data_ptr(),
-        k_cache.data_ptr(), v_cache.data_ptr(), n_pages, page_size, _stream(stream))
+    status = (_marshal or _binding()).qk_norm_rope(
+        q, k, v, q_out, k_cache, v_cache, slots, positions, q_gamma, k_gamma, eps,
+        None if axis_of_pair is None else bytes(axis_of_pair), rot_dim, base, _stream(stream))
     if status:
         raise EmbError(status, "emb_qk_norm_rope")
 
@@ -437,13 +435,8 @@ def emb_paged_attention(Q, k_cache, v_cache, table, q_start, kv_len, O, scale: f
                         workspace, prefix=None, cap: float = 0.0, window: int = 0, stream=None) -> None:
     """Q, O: bf16 [T][H * d]; caches: bf16 [n_pages][page_size][Hk][d]; table: int32 [R][max_pages]; q_start:
     int32 [R + 1]; kv_len, prefix: int32 [R]; workspace: paged_workspace()."""
-    n_pages, page_size, Hk, d = k_cache.shape
-    R, max_pages = table.shape
-    T, width = Q.shape
-    status = (_paged or paged_lib()).emb_paged_attention(
-        Q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), n_pages, page_size, table.data_ptr(), max_pages,
-        q_start.data_ptr(), kv_len.data_ptr(), None if prefix is None else prefix.data_ptr(), R, T, max_q, O.data_ptr(),
-        width // d, Hk, d, scale, cap, window, workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    status = (_marshal or _binding()).attention(Q, k_cache, v_cache, table, q_start, kv_len, O, workspace, prefix, scale,
+                                                max_q, cap, window, workspace.nbytes, _stream(stream))
     if status:
         raise EmbError(status, "emb_paged_attention")
 

@@ -1,5 +1,5 @@
 """Build libembqmm.so and libembpaged.so in-tree with nvcc for sm_103a (no cmake, no torch
-extension).
+extension), and the Python module that marshals the latter's calls.
 
 Each .cu is compiled in parallel, then linked into its shared library with the CUDA
 runtime linked statically, so the libraries need only the driver at run time.
@@ -11,6 +11,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -19,6 +20,7 @@ LIB = os.path.join(HERE, "libembqmm.so")
 SOURCES = ["api.cu", "quant.cu", "gemv.cu", "gemm_tc.cu", "layer_ops.cu"]
 PAGED_LIB = os.path.join(HERE, "libembpaged.so")
 PAGED_SOURCES = ["paged_api.cu", "paged_cache.cu", "paged_attention.cu", "paged_many.cu"]
+BINDING = os.path.join(HERE, "_paged_binding.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -39,9 +41,10 @@ def _flags(verbose_ptxas: bool):
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(PAGED_LIB):
+    built = (LIB, PAGED_LIB, BINDING)
+    if not all(os.path.exists(f) for f in built):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(PAGED_LIB))
+    t = min(os.path.getmtime(f) for f in built)
     deps = [os.path.join(CSRC, n) for n in os.listdir(CSRC)]
     deps += [os.path.join(HERE, "..", "include", n) for n in ("emb_qmm.h", "emb_paged.h")]
     deps.append(os.path.abspath(__file__))
@@ -62,8 +65,21 @@ def build(force: bool = False, verbose_ptxas: bool = False) -> str:
         return src, obj, r
 
     sources = SOURCES + PAGED_SOURCES
-    with cf.ThreadPoolExecutor(max_workers=len(sources)) as ex:
+    def compile_binding():
+        tmp = BINDING + f".tmp{os.getpid()}"
+        cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
+               "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "paged_binding.cpp"), "-o", tmp]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode == 0:
+            os.replace(tmp, BINDING)
+        return r
+
+    with cf.ThreadPoolExecutor(max_workers=len(sources) + 1) as ex:
+        binding = ex.submit(compile_binding)
         results = list(ex.map(compile_one, sources))
+        r = binding.result()
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed:\n{r.stdout}{r.stderr}")
     failed = False
     for src, _, r in results:
         if r.stdout or r.stderr:

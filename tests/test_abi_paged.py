@@ -111,6 +111,22 @@ def test_axis_list_of_the_wrong_length_is_refused(L):
                              axis_of_pair=[0] * 63, stream=1)
 
 
+def test_binding_reads_its_arguments(L):
+    """A wrong number of dimensions is a Python error; what the library refuses raises EmbError."""
+    import torch
+    i32, cache = torch.zeros(2, dtype=torch.int32), torch.zeros(1, 16, 1, 64, dtype=torch.bfloat16)
+    q = torch.zeros(2, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        emb.emb_paged_attention(q, cache[0], cache, i32[None], i32, i32, q, 0.1, 1, torch.zeros(16, dtype=torch.uint8), stream=1)
+    with pytest.raises(AttributeError):
+        emb.emb_paged_slots(None, i32, i32, i32, None, i32, i32, i32, i32, i32, 16, stream=1)
+    with pytest.raises(emb.EmbError) as e:
+        emb.emb_paged_attention(q, cache, cache, i32[None], i32, i32[:1], torch.empty_like(q), 0.1, 1, torch.zeros(16, dtype=torch.uint8), stream=1)
+    assert e.value.status in (emb.EMB_ENOSPC, emb.EMB_EALIGN)
+    with pytest.raises(emb.EmbError):
+        emb.emb_paged_slots(i32, i32, i32, i32[:1], i32[:, None], i32, i32, i32.long(), i32, i32[:1], 0, stream=1)
+
+
 def test_declarations_cite_their_passage():
     with open(emb.PAGED_HEADER_PATH) as fh:
         text = fh.read()
