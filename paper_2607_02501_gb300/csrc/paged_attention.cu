@@ -39,7 +39,6 @@ constexpr int kFewThreads = 32 * (kFewWarps + 1);
 constexpr int kFewTile = 64;
 constexpr int kFewRows = 16;
 constexpr int kFewCluster = 8;  // CTAs of a cluster, at most (the portable size)
-constexpr double kFewLongest = 16.0;  // tiles of a CTA of a cluster
 
 template <int D>
 struct FewTraits {
@@ -658,9 +657,12 @@ int few_cluster(const PagedAttnArgs& a) {
     if (a.window > 0) keys = std::min(keys, double(a.window) + kFewRows + kFewTile);
     const double items = double(a.n_req * a.n_kv_heads) * few_blocks(a), tiles = std::ceil(keys / kFewTile);
     const double ctas = (a.head_dim == 256 ? 1.0 : 2.0) * std::max(1, device_sm_count());
+    // a CTA's tiles, at most; more where a cap makes the other kernels dearer (24 requests of up to 7 queries, heads of 64, window
+    // of 1024: capped 18.6 and, by clusters of one, 15.5, uncapped 13.6 and 17.0)
+    const double longest = a.cap > 0.0f ? 24.0 : 16.0;
     int S = kFewCluster;
     while (S > 0 && items * S > ctas) S /= 2;
-    return S > 0 && tiles <= kFewLongest * S && tiles / S <= items * tiles / ctas + 8.0 ? S : 0;
+    return S > 0 && tiles <= longest * S && tiles / S <= items * tiles / ctas + 8.0 ? S : 0;
 }
 
 template <int D, bool CAP>
