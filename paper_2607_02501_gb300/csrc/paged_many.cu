@@ -11,9 +11,9 @@
 // memory is seldom rescaled. The weights are rounded once to bf16: hi + lo would double the value product for outputs
 // that are rounded to bf16 anyway (error against 64 bits 0.0023 of the outputs' norm, of which 0.0017 is that rounding).
 // What bounds it, measured: heads of 128, 4096 new tokens of 32 heads over 16384 keys 582 us (1650 TFLOP/s, 86 % of the
-// measured matrix rate): the softmax's powers of two (16 a cycle and SM) take as long as the MMAs. Heads of 64: half the MMAs for
-// the same powers. Heads of 256: every key and value is fetched for 128 rows instead of 256, and L2 delivers no more (2048
-// over 4096, 16 heads 137 us, 129 with the softmax left out). Small calls: latency and the join.
+// measured matrix rate): by nominal rates the softmax's powers of two (16 a cycle and SM) take as long as the MMAs. Heads of 64: half the MMAs for
+// the same powers. Heads of 256: every key and value is fetched for 128 rows instead of 256, which is probably the bound (2048
+// over 4096, 16 heads 137 us, 129 with the softmax left out; L2's own limit was not measured). Small calls: latency and the join.
 #include <algorithm>
 #include <mutex>
 
