@@ -371,6 +371,9 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 const int key0 = j * KT;
                 const bool edge = key0 < it.lo_all || key0 + KT > it.hi_all;
                 const int lo = keys.lo - key0, hi = keys.hi - key0;
+                // Votes are taken among rows that see a key of the tile. A tile's other rows are not of this request, or not
+                // even filled (3 heads: 126 of 128 rows), and what they hold may not decide how a warp computes.
+                const bool sees = max(lo, 0) < min(hi, KT);
                 float low = INFINITY;  // the lowest score that the row sees (for a cap)
                 if (edge) {
                     // scores that the row does not see, in tensor memory: rolled up and away from the path of most tiles
@@ -413,7 +416,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 // (the maximum is of raw scores: a cap keeps their order)
                 const float mt = fmaxf(max3(top[0], top[1], top[2]), top[3]);
                 auto base2 = [&](float v) { return CAP ? capped(v * p.scale2, p.cap2) : v * p.scale2; };
-                const bool grow = m == -INFINITY ? mt > kHidden : base2(mt) - base2(m) > 8.0f;
+                const bool grow = sees && (m == -INFINITY ? mt > kHidden : base2(mt) - base2(m) > 8.0f);
                 if (__any_sync(all, grow)) {
                     const float f = !grow ? 1.0f : m == -INFINITY ? 0.0f : exp2_fast(base2(m) - base2(mt));
                     if (j > a_t) {
@@ -458,7 +461,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 if constexpr (!CAP) {
                     const float2 sc = make_float2(p.scale2, p.scale2);
                     weights([&](float2 u) { return fma2(u, sc, mm); });
-                } else if (__all_sync(all, mt == kHidden || fmaxf(fabsf(mt), fabsf(low)) * p.scale2 < kNearCap)) {
+                } else if (__all_sync(all, !sees || fmaxf(fabsf(mt), fabsf(low)) * p.scale2 < kNearCap)) {
                     // far below the cap tanh is its series to x^9 (the next term is 2.4e-7 of it at 0.35): one power of two
                     // per score, where exponential and reciprocal take two more turns of the same unit. (The series runs away to
                     // -infinity at what stands for a hidden score.)
