@@ -106,7 +106,7 @@ EMB_API emb_status emb_qk_norm_rope(const uint16_t* q, int64_t q_stride, const u
  * no part in its output, whatever they hold (NaN included). A visible key whose score is NaN or +infinity
  * makes its queries' outputs NaN; a score of -infinity has weight zero; a visible value that is not finite makes
  * that element of its queries' outputs infinite or NaN. The scores are held in base 2 (scale *
- * log2(e) rounded to fp32 once), the weights by the hardware's power of two (relative error about 2^-22; below 2^-126 of
+ * log2(e) rounded to fp32 once; capped ones within a relative 2^-20, with caps of up to 64 within 2^-22 of the cap), the weights by the hardware's power of two (relative error about 2^-22; below 2^-126 of
  * the largest they are zero). Up to 16 query rows (max_q queries times heads per key/value head), the
  * weights enter the value product as bf16 hi + lo (2^-16); above, they may be rounded once to bf16 (2^-9 each).
  * kv_len above max_pages * page_size counts as that; q_start past n_tokens as n_tokens, and a decreasing

@@ -1,6 +1,7 @@
 // Attention of new tokens over a paged key/value cache (definition in include/emb_paged.h). Both kernels take
 // their work from paged_sched.cuh: few query rows per request on mma.sync, many on tcgen05.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <mutex>
@@ -54,7 +55,7 @@ struct FewTraits {
     static constexpr int kSmemCluster = kSmem + kFewRows * (kFinPitch + 2) * 4;
 };
 
-template <int D, bool CAP, bool CL>
+template <int D, int CAP, bool CL>
 __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_kernel(const __grid_constant__ PagedParams p) {
     using T = FewTraits<D>;
     constexpr int KS = D / 16, NT = D / 8, NJ = kFewTile / 8 / kFewWarps, ROWS = kFewRows;
@@ -262,9 +263,12 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
 #pragma unroll
             for (int n = 0; n < NJ; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sc[n][e] = __fmul_rn(sc[n][e], p.scale2);
-                    if constexpr (CAP) sc[n][e] = capped(sc[n][e], p.cap2);
+                for (int e = 0; e < 4; e += 2) {
+                    float2 z = make_float2(sc[n][e], sc[n][e + 1]);
+                    if constexpr (CAP) z = capped2<CAP>(z, p);
+                    else z = make_float2(__fmul_rn(z.x, p.scale2), __fmul_rn(z.y, p.scale2));
+                    sc[n][e] = z.x;
+                    sc[n][e + 1] = z.y;
                 }
             if (edge) {
 #pragma unroll
@@ -617,7 +621,7 @@ double unit_bound(const PagedAttnArgs& a, int qb, int kt) {
 namespace {
 
 // CTAs that run at once, asked once per device; the opt-in shared memory is a per-device attribute too.
-template <int D, bool CAP>
+template <int D, int CAP>
 cudaError_t few_resident(int& ctas) {
     static std::mutex mu;
     static int known[64] = {};
@@ -667,7 +671,7 @@ int few_cluster(const PagedAttnArgs& a) {
     return S > 0 && tiles <= longest * S && tiles / S <= items * tiles / ctas + 8.0 ? S : 0;
 }
 
-template <int D, bool CAP>
+template <int D, int CAP>
 cudaError_t launch_few(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
     int ctas = 0;
     const cudaError_t e = few_resident<D, CAP>(ctas);
@@ -688,7 +692,7 @@ cudaError_t launch_few(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
 
 template <int D>
 cudaError_t launch_few_d(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
-    return a.cap > 0.0f ? launch_few<D, true>(p, a, s) : launch_few<D, false>(p, a, s);
+    return a.cap > kMostLowCap ? launch_few<D, kAnyCap>(p, a, s) : a.cap > 0.0f ? launch_few<D, kLowCap>(p, a, s) : launch_few<D, kUncapped>(p, a, s);
 }
 
 }  // namespace
@@ -720,8 +724,12 @@ cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s) {
     p.Hk = int(a.n_kv_heads);
     p.G = p.H / p.Hk;
     constexpr double kLog2e = 1.4426950408889634;
-    p.scale2 = a.cap > 0.0f ? float(2.0 * kLog2e * double(a.scale) / double(a.cap)) : float(kLog2e * double(a.scale));
-    p.cap2 = float(kLog2e * double(a.cap));
+    p.lin2 = float(kLog2e * double(a.scale));
+    p.scale2 = p.lin2;
+    if (a.cap > 0.0f) {  // (held within fp32's range for the least and the largest caps)
+        p.scale2 = float(std::max(-double(FLT_MAX), std::min(2.0 * kLog2e * double(a.scale) / double(a.cap), double(FLT_MAX))));
+        p.cap2 = float(std::min(kLog2e * double(a.cap), double(FLT_MAX)));
+    }
     // Up to 16 rows of a request go to the mma.sync kernel, and more where all its blocks of 16 have a cluster at once: such
     // calls are small, and it has them sooner done (us, tcgen05 and mma.sync: 50 queries of 8 heads over 866 keys 11.3
     // and 8.5, 8 over 816 10.3 and 6.8, 24 requests of 3 queries of 14 heads on 2 of 64 12.1 and 7.6, 280 of 8 heads of 64 alone
@@ -729,7 +737,8 @@ cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s) {
     const bool few = p.G <= 16 && (a.max_q * p.G <= 16 || few_cluster(a) > 0);
     if (!few) {
         p.negate = a.scale < 0.0f;
-        p.scale2 = std::max(std::fabs(p.scale2), 1e-37f);  // (hidden scores are -infinity times this)
+        p.scale2 = std::max(std::fabs(p.scale2), 1e-37f);  // (hidden scores are the lowest there are times this)
+        p.lin2 = std::max(std::fabs(p.lin2), 1e-37f);
         return launch_paged_many(p, a, s);
     }
     return a.head_dim == 64    ? launch_few_d<64>(p, a, s)

@@ -54,32 +54,6 @@ __device__ __forceinline__ float min3(float a, float b, float c) {
     asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// Two fp32 products, FMAs and sums at once.
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 d;
-    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
-        "mul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
-        : "=f"(d.x), "=f"(d.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 d;
-    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
-        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
-        : "=f"(d.x), "=f"(d.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    float2 d;
-    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
-        "add.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
-        : "=f"(d.x), "=f"(d.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
-
 // A place of the ring and the parity of the turn it is in, carried along (a division per wait costs more than the wait).
 template <int S>
 struct RingPlace {
@@ -125,14 +99,13 @@ __device__ __forceinline__ Segment<D> segment_of(const PagedParams& p, int r, in
     return s;
 }
 
-template <int D, bool CAP>
+template <int D, int CAP>
 __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(const __grid_constant__ PagedParams p) {
     using T = ManyTraits<D>;
     constexpr int NQ = T::NQ, KT = T::KT, S = T::kSlots;
     constexpr int kRows = 128 * NQ;
     using PL = PartLayout<D, kRows>;
     // what stands for the score of a key that a row does not see (a cap would make -infinity finite)
-    constexpr float kNearCap = 2.0f * 1.4426950408889634f * 0.35f;  // |scale q.k / cap| < 0.35, in units of scale2
     constexpr float kHidden = CAP ? -3.402823466e38f : -INFINITY;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t kv_full[S], kv_empty[S], q_full, q_empty, s_full[2], p_ready[2], o_done[2], o_free[2], drain;
@@ -415,10 +388,14 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                 }
                 // (the maximum is of raw scores: a cap keeps their order)
                 const float mt = fmaxf(max3(top[0], top[1], top[2]), top[3]);
-                auto base2 = [&](float v) { return CAP ? capped(v * p.scale2, p.cap2) : v * p.scale2; };
-                const bool grow = sees && (m == -INFINITY ? mt > kHidden : base2(mt) - base2(m) > 8.0f);
+                auto base2 = [&](float v) {
+                    if constexpr (CAP) return capped2<CAP>(make_float2(v, v), p).x;
+                    else return v * p.scale2;
+                };
+                const float zt = base2(mt);
+                const bool grow = sees && (m == -INFINITY ? mt > kHidden : zt + mc > 8.0f);
                 if (__any_sync(all, grow)) {
-                    const float f = !grow ? 1.0f : m == -INFINITY ? 0.0f : exp2_fast(base2(m) - base2(mt));
+                    const float f = !grow ? 1.0f : m == -INFINITY ? 0.0f : exp2_fast(-mc - zt);
                     if (j > a_t) {
                         wait(&o_done[t], outs - 1);  // every product issued so far is in
                         ptx::tc_fence_after();
@@ -438,7 +415,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                         l2[0] = fma2(l2[0], ff, z);
                         l2[1] = fma2(l2[1], ff, z);
                         m = mt;
-                        mc = -base2(m);
+                        mc = -zt;
                     }
                 }
                 // The weights, 32 at a time, over the scores. `base` gives two scores in base 2 less the row's maximum.
@@ -462,23 +439,13 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                     const float2 sc = make_float2(p.scale2, p.scale2);
                     weights([&](float2 u) { return fma2(u, sc, mm); });
                 } else if (__all_sync(all, !sees || fmaxf(fabsf(mt), fabsf(low)) * p.scale2 < kNearCap)) {
-                    // far below the cap tanh is its series to x^9 (the next term is 2.4e-7 of it at 0.35): one power of two
-                    // per score, where exponential and reciprocal take two more turns of the same unit. (The series runs away to
-                    // -infinity at what stands for a hidden score.)
-                    const float x1 = p.scale2 * (0.5f / 1.4426950408889634f), u1 = x1 * p.cap2;
-                    const float2 sx = make_float2(x1, x1), su = make_float2(u1, u1);
-                    weights([&](float2 u) {
-                        const float2 x = mul2(u, sx), y = mul2(x, x);
-                        auto k = [](float v) { return make_float2(v, v); };
-                        float2 t = fma2(y, k(62.0f / 2835.0f), k(-17.0f / 315.0f));
-                        t = fma2(t, y, k(2.0f / 15.0f));
-                        t = fma2(t, y, k(-1.0f / 3.0f));
-                        t = fma2(t, y, k(1.0f));
-                        return fma2(mul2(u, su), t, mm);
-                    });
+                    // far below the cap one power of two per score, where exponential and reciprocal take two more turns of
+                    // the same unit. (The series runs away to -infinity at what stands for a hidden score.)
+                    weights([&](float2 u) { return capped_near2(u, p, mm); });
                 } else {
                     weights([&](float2 u) {
-                        return add2(make_float2(u.x == kHidden ? -INFINITY : base2(u.x), u.y == kHidden ? -INFINITY : base2(u.y)), mm);
+                        const float2 z = capped2<CAP>(u, p);
+                        return add2(make_float2(u.x == kHidden ? -INFINITY : z.x, u.y == kHidden ? -INFINITY : z.y), mm);
                     });
                 }
                 const bool tail = key0 + KT > it.q.L, hidden = key0 < it.lo_all || min(key0 + KT, it.q.L) > it.hi_all;
@@ -632,7 +599,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
     }
 }
 
-template <int D, bool CAP>
+template <int D, int CAP>
 cudaError_t launch_many(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
     using T = ManyTraits<D>;
     // the opt-in shared-memory size is a per-device function attribute
@@ -672,13 +639,15 @@ cudaError_t launch_many(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) 
     return launch_serialised(reinterpret_cast<const void*>(paged_many_kernel<D, CAP>), grid, T::kThreads, T::kSmem, s, args);
 }
 
+template <int D>
+cudaError_t launch_many_d(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
+    return a.cap > kMostLowCap ? launch_many<D, kAnyCap>(p, a, s) : a.cap > 0.0f ? launch_many<D, kLowCap>(p, a, s) : launch_many<D, kUncapped>(p, a, s);
+}
+
 }  // namespace
 
 cudaError_t launch_paged_many(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
-    const bool cap = a.cap > 0.0f;
-    if (a.head_dim == 64) return cap ? launch_many<64, true>(p, a, s) : launch_many<64, false>(p, a, s);
-    if (a.head_dim == 128) return cap ? launch_many<128, true>(p, a, s) : launch_many<128, false>(p, a, s);
-    return cap ? launch_many<256, true>(p, a, s) : launch_many<256, false>(p, a, s);
+    return a.head_dim == 64 ? launch_many_d<64>(p, a, s) : a.head_dim == 128 ? launch_many_d<128>(p, a, s) : launch_many_d<256>(p, a, s);
 }
 
 }  // namespace emb

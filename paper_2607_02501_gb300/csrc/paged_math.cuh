@@ -16,8 +16,36 @@ __device__ __forceinline__ float rcp_fast(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// cap log2(e) tanh(y / 2), y = 2 scale q.k / cap with its base 2: tanh as 1 - 2 / (1 + e^y), within 2^-22 of 1
-__device__ __forceinline__ float capped(float y, float cap2) { return fmaf(-2.0f * cap2, rcp_fast(1.0f + exp2_fast(y)), cap2); }
+// Capped scores cap log2(e) tanh(x), x = scale q.k / cap, from q.k.
+// capped_far: as 1 - 2 / (1 + e^2x), within 2^-22 of the cap: 2^-20 of the value from |x| = 0.35 on, and for caps up to 64 within
+// the 2^-16 that the weights are held to. capped_near, below 0.35: the series x (1 - x^2 / 3 + 2 x^4 / 15 - 17 x^6 / 315 +
+// 62 x^8 / 2835), whose next term is 2.4e-7 of it; the factor cap log2(e) x = q.k lin2 is formed without the cap, so it is right
+// however far the cap lies above the scores.
+// Kernels for caps of up to 64 have the first form for all scores, those for any cap have for each score its own. (us, the two:
+// 2048 tokens of 32 heads of 128 over 8192 keys, a cap of 50 and scores up to it 434 and 988; 24 requests of up to 7 queries,
+// heads of 64, 15.2 and 16.3.)
+constexpr float kNearCap = 2.0f * 1.4426950408889634f * 0.35f;  // |x| = 0.35 in units of |q.k scale2|
+enum : int { kUncapped, kLowCap, kAnyCap };                     // a kernel's scores
+constexpr float kMostLowCap = 64.0f;
+__device__ __forceinline__ float2 capped_near2(float2 qk, const PagedParams& p, float2 plus) {
+    auto k = [](float v) { return make_float2(v, v); };
+    const float2 x = mul2(qk, k(p.scale2 * (0.5f / 1.4426950408889634f))), y = mul2(x, x);
+    float2 t = fma2(y, k(62.0f / 2835.0f), k(-17.0f / 315.0f));
+    t = fma2(t, y, k(2.0f / 15.0f));
+    t = fma2(t, y, k(-1.0f / 3.0f));
+    t = fma2(t, y, k(1.0f));
+    return fma2(mul2(qk, k(p.lin2)), t, plus);
+}
+__device__ __forceinline__ float capped_far(float qk, const PagedParams& p) {
+    return fmaf(p.cap2, -2.0f * rcp_fast(1.0f + exp2_fast(qk * p.scale2)), p.cap2);
+}
+template <int CAP>
+__device__ __forceinline__ float2 capped2(float2 qk, const PagedParams& p) {
+    const float2 far = make_float2(capped_far(qk.x, p), capped_far(qk.y, p));
+    if constexpr (CAP == kLowCap) return far;
+    const float2 near = capped_near2(qk, p, make_float2(0, 0));
+    return make_float2(fabsf(qk.x * p.scale2) < kNearCap ? near.x : far.x, fabsf(qk.y * p.scale2) < kNearCap ? near.y : far.y);
+}
 
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);

@@ -40,6 +40,7 @@ struct PagedParams {
     uint32_t grid_inv;  // ceil(2^32 / grid)
     float scale2;  // scores are kept in base 2: scale * log2(e); capped, 2 log2(e) scale / cap
     float cap2;    // cap * log2(e)
+    float lin2;    // scale * log2(e)
 };
 
 struct PagedReq {
