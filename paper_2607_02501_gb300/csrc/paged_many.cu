@@ -333,7 +333,10 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
             const KeyRange keys = live ? query_keys(p, it.q, it.i0 + t * qt + i) : KeyRange{0, 0};
             // (selected, not indexed: t is a run-time value)
             const int a_t = t ? sg.a[1] : sg.a[0], b_t = t ? sg.b[1] : sg.b[0];
-            float m = -INFINITY, mc = 0.0f;  // running maximum of the raw scores, and what is added in base 2
+            // whether the row has seen a score, its running maximum in base 2 (negated, so that it is added), sums of weights. A
+            // cap makes a score of -infinity one of -cap, which counts.
+            bool any = false;
+            float mc = 0.0f;
             float2 l2[2] = {make_float2(0, 0), make_float2(0, 0)};
             for (int j = sg.j0; j < sg.j1; ++j, ++n) {
                 if (j < a_t || j >= b_t) continue;
@@ -393,9 +396,9 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                     else return v * p.scale2;
                 };
                 const float zt = base2(mt);
-                const bool grow = sees && (m == -INFINITY ? mt > kHidden : zt + mc > 8.0f);
+                const bool grow = sees && (any ? zt + mc > 8.0f : CAP || mt > -INFINITY);
                 if (__any_sync(all, grow)) {
-                    const float f = !grow ? 1.0f : m == -INFINITY ? 0.0f : exp2_fast(-mc - zt);
+                    const float f = !grow ? 1.0f : any ? exp2_fast(-mc - zt) : 0.0f;
                     if (j > a_t) {
                         wait(&o_done[t], outs - 1);  // every product issued so far is in
                         ptx::tc_fence_after();
@@ -414,7 +417,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                         const float2 ff = make_float2(f, f), z = make_float2(0, 0);
                         l2[0] = fma2(l2[0], ff, z);
                         l2[1] = fma2(l2[1], ff, z);
-                        m = mt;
+                        any = true;
                         mc = -zt;
                     }
                 }
@@ -515,7 +518,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
             const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
             const bool odd = has && *reinterpret_cast<volatile uint32_t*>(&odd_item) == ordinal;
             if (!whole && live) {
-                part[prow] = m == -INFINITY ? m : -mc;
+                part[prow] = any ? -mc : -INFINITY;
                 part[kRows + prow] = l;
             }
 #pragma unroll 1

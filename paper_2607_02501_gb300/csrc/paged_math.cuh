@@ -22,8 +22,7 @@ __device__ __forceinline__ float rcp_fast(float x) {
 // 62 x^8 / 2835), whose next term is 2.4e-7 of it; the factor cap log2(e) x = q.k lin2 is formed without the cap, so it is right
 // however far the cap lies above the scores.
 // Kernels for caps of up to 64 have the first form for all scores, those for any cap have for each score its own. (us, the two:
-// 2048 tokens of 32 heads of 128 over 8192 keys, a cap of 50 and scores up to it 434 and 988; 24 requests of up to 7 queries,
-// heads of 64, 15.2 and 16.3.)
+// 2048 tokens of 32 heads of 128 over 8192 keys, a cap of 65 and scores up to it 435 and 528.)
 constexpr float kNearCap = 2.0f * 1.4426950408889634f * 0.35f;  // |x| = 0.35 in units of |q.k scale2|
 enum : int { kUncapped, kLowCap, kAnyCap };                     // a kernel's scores
 constexpr float kMostLowCap = 64.0f;
