@@ -109,8 +109,8 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
     constexpr float kHidden = CAP ? -3.402823466e38f : -INFINITY;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t kv_full[S], kv_empty[S], q_full, q_empty, s_full[2], p_ready[2], o_done[2], o_free[2], drain;
-    __shared__ uint32_t tmem_slot, odd_item;
-    __shared__ int abort_flag, joined;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag, joined, odd_seen;
     __shared__ PagedJoin cut[2];
     uint8_t* sq = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* ring = sq + NQ * T::kQTile;
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         }
         ptx::mbar_init(&drain, 1);
         abort_flag = 0;
-        odd_item = 0;
+        odd_seen = 0;
         ptx::fence_mbar_init();
         ptx::prefetch_tmap(&p.q_map);
         ptx::prefetch_tmap(&p.k_map);
@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         const int row = 32 * (warp & 3) + lane, qt = p.QT, i = row / p.G;
         const uint32_t lanes = uint32_t(32 * (warp & 3)) << 16;
         const uint32_t o_col = tmem + lanes + uint32_t(T::kO + t * D);
-        uint32_t n = 0, seen[2] = {0, 0}, outs = 0, ordinal = 0;
+        uint32_t n = 0, seen[2] = {0, 0}, outs = 0;
         int joins = 0;
         auto soft_bar = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * T::kSoftWarps) : "memory"); };
         // A wait that gave up sets abort_flag; later waits then return at once, and the loops run to their end (the
@@ -328,7 +328,6 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
         while (x < st.x1) {
             const Segment<D> sg = segment_of<D>(p, r, g, b, off, x, st.x1);
             const PagedItem& it = sg.it;
-            ++ordinal;
             const bool live = i < (t ? sg.nq[1] : sg.nq[0]);
             const KeyRange keys = live ? query_keys(p, it.q, it.i0 + t * qt + i) : KeyRange{0, 0};
             // (selected, not indexed: t is a run-time value)
@@ -485,7 +484,9 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                             }
                             if (hit) {
                                 v[e] = u;
-                                *reinterpret_cast<volatile uint32_t*>(&odd_item) = ordinal;
+                                // (never taken back: the other row tile may be some items behind. Items without such values are
+                                // then searched for nothing)
+                                *reinterpret_cast<volatile int*>(&odd_seen) = 1;
                             }
                         }
                     }
@@ -516,7 +517,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
             const int prow = t * qt * p.G + row;  // rows of both tiles in order
             __nv_bfloat16* out = p.O + (int64_t(it.q.q0 + it.i0 + t * qt + i) * p.H + g * p.G + (row - i * p.G)) * D;
             const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
-            const bool odd = has && *reinterpret_cast<volatile uint32_t*>(&odd_item) == ordinal;
+            const bool odd = has && *reinterpret_cast<volatile int*>(&odd_seen) != 0;
             if (!whole && live) {
                 part[prow] = any ? -mc : -INFINITY;
                 part[kRows + prow] = l;
@@ -533,19 +534,21 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
                     for (int e = 0; e < 32; ++e) o[e] = 0.0f;
                 }
                 if (odd) {
-                    for (int key = max(keys.lo, sg.j0 * KT); key < min(keys.hi, sg.j1 * KT); ++key) {
-                        const int key0 = key / KT * KT;
+                    for (int j = sg.j0; j < sg.j1; ++j) {  // the tiles that such values left
+                        const int key0 = j * KT;
                         if (!(key0 < it.lo_all || min(key0 + KT, it.q.L) > it.hi_all)) continue;
-                        const int page = p.table[int64_t(r) * p.max_pages + (key >> p.page_shift)];
-                        if (page < 0 || page >= p.n_pages) continue;
-                        const int64_t slot = (int64_t(page) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
-                        const uint32_t* v = reinterpret_cast<const uint32_t*>(p.V + (slot * p.Hk + g) * D + c);
+                        for (int key = max(keys.lo, key0); key < min(keys.hi, key0 + KT); ++key) {
+                            const int page = p.table[int64_t(r) * p.max_pages + (key >> p.page_shift)];
+                            if (page < 0 || page >= p.n_pages) continue;
+                            const int64_t slot = (int64_t(page) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
+                            const uint32_t* v = reinterpret_cast<const uint32_t*>(p.V + (slot * p.Hk + g) * D + c);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const uint32_t w = v[e];
-                            const float2 f = unpack_bf16x2(w);
-                            if (not_finite(w)) o[2 * e] += f.x;
-                            if (not_finite(w >> 16)) o[2 * e + 1] += f.y;
+                            for (int e = 0; e < 16; ++e) {
+                                const uint32_t w = v[e];
+                                const float2 f = unpack_bf16x2(w);
+                                if (not_finite(w)) o[2 * e] += f.x;
+                                if (not_finite(w >> 16)) o[2 * e + 1] += f.y;
+                            }
                         }
                     }
                 }
