@@ -120,7 +120,8 @@ EMB_API emb_status emb_qk_norm_rope(const uint16_t* q, int64_t q_stride, const u
  * max_pages * page_size < 2^31. A call whose key tiles could number 2^31 is EMB_EUNSUPPORTED.
  * workspace: EMB_PAGED_WORKSPACE bytes (EMB_ENOSPC if ws_bytes says less), 256-byte aligned, zero-filled before its
  * first use; a call leaves it ready for the next one unless emb_paged_status reports EMB_ETIMEOUT: then zero
- * its first 4 KB again. One workspace serves one stream at a time. Results are bitwise reproducible for
+ * its first 4 KB again. One workspace serves one stream at a time; calls on other streams with a workspace of their own may
+ * run beside it (calls whose CTAs wait for one another are cooperative launches). Results are bitwise reproducible for
  * the same lengths. No output may overlap another buffer.
  * Errors: EMB_EINVAL, EMB_EALIGN, EMB_ENOSPC, EMB_EUNSUPPORTED, EMB_ECUDA. */
 EMB_API emb_status emb_paged_attention(const uint16_t* Q, const uint16_t* k_cache, const uint16_t* v_cache,

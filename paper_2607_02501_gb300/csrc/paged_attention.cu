@@ -555,7 +555,7 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
     }
 
     // Every CTA joins its share of the items that it has a part in, once all their parts are there. The CTAs of
-    // the grid are all resident, and each publishes its parts before it waits.
+    // the grid all run at once (a cooperative launch), and each publishes its parts before it waits.
     if (joins > 0) bar();
     for (int k = 0; k < joins; ++k) {
         const PagedJoin J = cut[k];
@@ -687,7 +687,7 @@ cudaError_t launch_few(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) {
                                  kFewThreads, FewTraits<D>::kSmemCluster, s, args, unsigned(p.cluster));
     const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, kFewTile))));
     set_grid(p, grid, 3);
-    return launch_serialised(reinterpret_cast<const void*>(paged_few_kernel<D, CAP, false>), grid, kFewThreads, FewTraits<D>::kSmem, s, args);
+    return launch_serialised(reinterpret_cast<const void*>(paged_few_kernel<D, CAP, false>), grid, kFewThreads, FewTraits<D>::kSmem, s, args, 1, true);
 }
 
 template <int D>

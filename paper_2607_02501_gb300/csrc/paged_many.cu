@@ -585,7 +585,7 @@ __global__ void __launch_bounds__(ManyTraits<D>::kThreads, 1) paged_many_kernel(
             if (x < st.x1) next_item(p, r, g, b, it.q.n);
         }
         // Every CTA joins its share of the items that it has a part in, once all their parts are there. The CTAs of
-        // the grid are all resident, and each publishes its parts before it waits.
+        // the grid all run at once (a cooperative launch), and each publishes its parts before it waits.
         if (joins > 0) soft_bar();
         for (int k = 0; k < joins; ++k) {
             const PagedJoin J = cut[k];
@@ -642,7 +642,7 @@ cudaError_t launch_many(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) 
     const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, T::KT))));
     set_grid(p, grid, D == 256 ? 8 : 2);
 
-    return launch_serialised(reinterpret_cast<const void*>(paged_many_kernel<D, CAP>), grid, T::kThreads, T::kSmem, s, args);
+    return launch_serialised(reinterpret_cast<const void*>(paged_many_kernel<D, CAP>), grid, T::kThreads, T::kSmem, s, args, 1, true);
 }
 
 template <int D>
