@@ -168,6 +168,13 @@ def _binding():
     return _marshal
 
 
+def _refused(status, where: str):
+    """Raises for a status, or for what the binding says of a tensor that is not what the call would take it for."""
+    if isinstance(status, str):
+        raise EmbError(EMB_EINVAL, f"{where}: {status}")
+    raise EmbError(status, where)
+
+
 def declared_symbols() -> list:
     """Names of every entry point declared in include/emb_qmm.h."""
     with open(HEADER_PATH) as fh:
@@ -411,11 +418,11 @@ def emb_paged_slots(cached, added, free_pages, used, table, q_start, kv_len, slo
                     page_size: int, stream=None) -> None:
     """cached, added: int32 [R]; free_pages: int32 [n_free]; used, used_out: int32 [1]; table: int32
     [R][max_pages], filled on; out: q_start int32 [R + 1], kv_len int32 [R], slots int64 [T], positions
-    int32 [T]."""
+    int32 [T]. A tensor that is shorter, strided or of another element size is refused (EMB_EINVAL), here and below."""
     status = (_marshal or _binding()).slots(cached, added, free_pages, used, table, q_start, kv_len, slots, positions,
                                             used_out, page_size, _stream(stream))
     if status:
-        raise EmbError(status, "emb_paged_slots")
+        _refused(status, "emb_paged_slots")
 
 
 def emb_qk_norm_rope(q, k, v, q_out, k_cache, v_cache, slots, positions, q_gamma=None, k_gamma=None,
@@ -428,7 +435,7 @@ def emb_qk_norm_rope(q, k, v, q_out, k_cache, v_cache, slots, positions, q_gamma
         q, k, v, q_out, k_cache, v_cache, slots, positions, q_gamma, k_gamma, eps,
         None if axis_of_pair is None else bytes(axis_of_pair), rot_dim, base, _stream(stream))
     if status:
-        raise EmbError(status, "emb_qk_norm_rope")
+        _refused(status, "emb_qk_norm_rope")
 
 
 def emb_paged_attention(Q, k_cache, v_cache, table, q_start, kv_len, O, scale: float, max_q: int,
@@ -438,7 +445,7 @@ def emb_paged_attention(Q, k_cache, v_cache, table, q_start, kv_len, O, scale: f
     status = (_marshal or _binding()).attention(Q, k_cache, v_cache, table, q_start, kv_len, O, workspace, prefix, scale,
                                                 max_q, cap, window, workspace.nbytes, _stream(stream))
     if status:
-        raise EmbError(status, "emb_paged_attention")
+        _refused(status, "emb_paged_attention")
 
 
 def paged_workspace(device=None):
