@@ -162,6 +162,9 @@ def _binding():
     global _marshal
     if _marshal is None:
         L = paged_lib()
+        from .buildlib import BINDING
+        if not os.path.exists(BINDING):  # (another interpreter's must not be taken for it)
+            raise RuntimeError(f"{BINDING} is missing: run paper_2607_02501_gb300.build() with this interpreter first")
         from . import _paged_binding as m
         m.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.emb_paged_slots, L.emb_qk_norm_rope, L.emb_paged_attention)))
         _marshal = m

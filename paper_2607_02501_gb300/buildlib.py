@@ -20,7 +20,8 @@ LIB = os.path.join(HERE, "libembqmm.so")
 SOURCES = ["api.cu", "quant.cu", "gemv.cu", "gemm_tc.cu", "layer_ops.cu"]
 PAGED_LIB = os.path.join(HERE, "libembpaged.so")
 PAGED_SOURCES = ["paged_api.cu", "paged_cache.cu", "paged_attention.cu", "paged_many.cu"]
-BINDING = os.path.join(HERE, "_paged_binding.so")
+# named for the interpreter and machine that it is compiled for, as the importer looks for it
+BINDING = os.path.join(HERE, "_paged_binding" + sysconfig.get_config_var("EXT_SUFFIX"))
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
