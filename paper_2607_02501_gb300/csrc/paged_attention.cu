@@ -109,6 +109,7 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
         // -------------------------------------------------------------------- producer
         ptx::fence_proxy_async_global();  // (the cache was written by ordinary stores)
         const int page_size = 1 << p.page_shift, box = min(page_size, kFewTile), n_box = kFewTile / box;
+        uint32_t loads = 0;  // tiles issued: all that were walked through, unless a wait gave up
         while (CL ? b < blocks : x < st.x1) {
             const PagedItem it = paged_item<kFewTile>(p, r, g, b);
             const uint32_t take = min(st.x1 - x, uint32_t(it.units) - off);
@@ -149,6 +150,7 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
                         }
                         __syncwarp();
                     }
+                    ++loads;
                 }
                 page = next;
             }
@@ -162,10 +164,9 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
                 if (x < st.x1) next_item(p, r, g, b, it.q.n);
             }
         }
-        // every copy must land before this CTA's shared memory is released
-        if (!abort_flag)
-            for (uint32_t i = issued > uint32_t(T::kStages) ? issued - T::kStages : 0; i < issued; ++i)
-                ptx::mbar_wait(&full[i % T::kStages], (i / T::kStages) & 1, &abort_flag, p.status, kWaitLimitNs);
+        // every copy must land before this CTA's shared memory is released, also where a wait gave up
+        for (uint32_t i = loads > uint32_t(T::kStages) ? loads - T::kStages : 0; i < loads; ++i)
+            ptx::mbar_wait(&full[i % T::kStages], (i / T::kStages) & 1, nullptr, p.status, kWaitLimitNs);
         return;
     }
 

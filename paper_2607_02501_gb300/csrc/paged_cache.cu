@@ -349,21 +349,26 @@ __global__ void __launch_bounds__(kQkThreads, kQkCtas) qk_norm_rope_kernel(const
             }
         };
         ptx::fence_proxy_async_global();  // (the rows were written by ordinary stores)
-        for (int i = 0; i < kQkStages; ++i)
-            if (blockIdx.x + i * step < p.items) fill(blockIdx.x + i * step, i);
+        uint32_t fills = 0;
+        for (; fills < kQkStages && blockIdx.x + fills * step < p.items; ++fills) fill(blockIdx.x + fills * step, int(fills));
         uint32_t n = 0;
         for (int64_t item = blockIdx.x; item < p.items; item += step, ++n) {
             const int st = int(n % kQkStages);
             ptx::mbar_wait(&done[st], (n / kQkStages) & 1, abort_flag, status, kWaitLimitNs);
             __syncwarp();
-            if (*reinterpret_cast<volatile int*>(abort_flag)) break;  // (the rows' copies have landed or never will)
+            if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(abort_flag) != 0)) {
+                // a wait gave up: what is still on its way into shared memory lands before the CTA leaves
+                for (uint32_t i = n; i < fills; ++i)
+                    ptx::mbar_wait(&full[i % kQkStages], (i / kQkStages) & 1, nullptr, status, kWaitLimitNs);
+                break;
+            }
             drain(item_at(item), st);
             // the item before this one has left its stage (its copies were given an item's time): it is filled again
             const int64_t ahead = item + (kQkStages - 1) * step;
             if (n > 0 && ahead < p.items) {
                 ptx::bulk_wait_read<1>();
                 __syncwarp();
-                fill(ahead, int((n + kQkStages - 1) % kQkStages));
+                fill(ahead, int(fills++ % kQkStages));
             }
         }
         ptx::bulk_wait_all();
