@@ -138,6 +138,12 @@ EMB_API emb_status emb_paged_attention(const uint16_t* Q, const uint16_t* k_cach
  * (the outputs of the calls since then are undefined). */
 EMB_API emb_status emb_paged_status(emb_stream_t stream);
 
+/* Section 3.2 (deployment boundary; test support for the failure path above).
+ * One CTA publishes its part of a shared item in a ready workspace of emb_paged_attention and waits for another's, which
+ * never comes, giving up after timeout_ns nanoseconds (1e3 .. 1e9): emb_paged_status then returns EMB_ETIMEOUT, and the
+ * workspace's first 4 KB are to be zeroed. Errors: EMB_EINVAL, EMB_EALIGN, EMB_ENOSPC, EMB_ECUDA. */
+EMB_API emb_status emb_paged_selftest_wait_timeout(void* workspace, size_t ws_bytes, int64_t timeout_ns, emb_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

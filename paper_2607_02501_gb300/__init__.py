@@ -148,7 +148,9 @@ def paged_lib():
     L.emb_paged_attention.argtypes = [vp, vp, vp, i64, i64, vp, i64, vp, vp, vp, i64, i64, i64, vp, i64, i64,
                                       i64, f32, f32, i64, vp, ctypes.c_size_t, vp]
     L.emb_paged_status.argtypes = [vp]
-    for name in ("emb_paged_slots", "emb_qk_norm_rope", "emb_paged_attention", "emb_paged_status"):
+    L.emb_paged_selftest_wait_timeout.argtypes = [vp, ctypes.c_size_t, i64, vp]
+    for name in ("emb_paged_slots", "emb_qk_norm_rope", "emb_paged_attention", "emb_paged_status",
+                 "emb_paged_selftest_wait_timeout"):
         getattr(L, name).restype = ctypes.c_int
     _paged = L
     return L
@@ -460,6 +462,12 @@ def paged_workspace(device=None):
 def emb_paged_status(stream=None) -> int:
     """Synchronise the stream; return (and clear) the paged-cache library's status code."""
     return int(paged_lib().emb_paged_status(_stream(stream)))
+
+
+def emb_paged_selftest_wait_timeout(workspace, timeout_ns: int, stream=None) -> None:
+    """Test support: a wait of the attention's joins that runs out; leaves the first 4 KB of `workspace` to be zeroed."""
+    _check(paged_lib().emb_paged_selftest_wait_timeout(_ptr(workspace), workspace.nbytes, timeout_ns, _stream(stream)),
+           "emb_paged_selftest_wait_timeout")
 
 
 def emb_dequantize_f32(fmt: int, W_blocks, N: int, K: int, out, stream=None) -> None:

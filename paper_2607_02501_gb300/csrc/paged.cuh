@@ -57,6 +57,7 @@ struct PagedAttnArgs {
 // Key tiles of a call, at most (an upper bound from the host's sizes).
 double paged_attention_tiles(const PagedAttnArgs& a);
 cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s);
+cudaError_t launch_paged_selftest(void* workspace, uint64_t limit_ns, int* status, cudaStream_t s);
 
 // Two fp32 products, FMAs and sums at once.
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) {

@@ -250,4 +250,13 @@ emb_status emb_paged_status(emb_stream_t stream) {
     return (host & kStatusTimeout) ? EMB_ETIMEOUT : EMB_OK;
 }
 
+emb_status emb_paged_selftest_wait_timeout(void* workspace, size_t ws_bytes, int64_t timeout_ns, emb_stream_t stream) {
+    if (!workspace || timeout_ns < 1000 || timeout_ns > 1000000000) return EMB_EINVAL;
+    if (!aligned(workspace, 256)) return EMB_EALIGN;
+    if (ws_bytes < EMB_PAGED_WORKSPACE) return EMB_ENOSPC;
+    int* st = device_words(false);
+    if (!st) return EMB_ECUDA;
+    return from_cuda(launch_paged_selftest(workspace, uint64_t(timeout_ns), st, stream_of(stream)));
+}
+
 }  // extern "C"

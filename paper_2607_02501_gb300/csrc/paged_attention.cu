@@ -568,6 +568,14 @@ __global__ void __launch_bounds__(kFewThreads, FewTraits<D>::kCtas) paged_few_ke
     }
 }
 
+// A CTA's part of an item whose other part never comes: published and waited for as in the kernels.
+__global__ void paged_selftest_kernel(uint32_t* flags, uint64_t limit_ns, int* status) {
+    __shared__ int abort_flag;
+    abort_flag = 0;
+    part_publish(flags);
+    part_wait(flags, 2, &abort_flag, status, limit_ns);
+}
+
 // ------------------------------------------------------------------ host side
 
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
@@ -699,6 +707,11 @@ cudaError_t launch_few_d(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s)
 }  // namespace
 
 double paged_attention_tiles(const PagedAttnArgs& a) { return unit_bound(a, std::max<int>(1, int(16 / (a.n_heads / a.n_kv_heads))), kFewTile); }
+
+cudaError_t launch_paged_selftest(void* workspace, uint64_t limit_ns, int* status, cudaStream_t s) {
+    paged_selftest_kernel<<<1, 1, 0, s>>>(static_cast<uint32_t*>(workspace), limit_ns, status);
+    return cudaGetLastError();
+}
 
 cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s) {
     PagedParams p;

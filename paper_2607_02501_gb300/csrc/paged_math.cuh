@@ -79,8 +79,8 @@ __device__ __forceinline__ void part_publish(uint32_t* flag) {
     atomicAdd(flag, 1u);
 }
 // Waits for all partial results of an item: one thread. The last CTA to pass hands the flag back at zero.
-__device__ __forceinline__ bool part_wait(uint32_t* flag, int count, volatile int* abort, int* status) {
-    if (!join_wait(flag, uint32_t(count), abort, status)) return false;
+__device__ __forceinline__ bool part_wait(uint32_t* flag, int count, volatile int* abort, int* status, uint64_t limit_ns = kWaitLimitNs) {
+    if (!join_wait(flag, uint32_t(count), abort, status, limit_ns)) return false;
     if (atomicAdd(flag, 1u) == 2u * uint32_t(count) - 1u) ptx::st_relaxed_gpu(flag, 0u);
     return true;
 }

@@ -333,13 +333,13 @@ struct PagedJoin {
 __device__ __forceinline__ int64_t part_slot(int c, int first) { return 2 * int64_t(c) + (c == first ? 1 : 0); }
 
 // Waits until *flag >= count (acquire); gives up like ptx::mbar_wait.
-__device__ __forceinline__ bool join_wait(const uint32_t* flag, uint32_t count, volatile int* abort, int* status) {
+__device__ __forceinline__ bool join_wait(const uint32_t* flag, uint32_t count, volatile int* abort, int* status, uint64_t limit_ns) {
     if (ptx::ld_acquire_gpu(flag) >= count) return true;
     const uint64_t t0 = ptx::globaltimer();
     for (;;) {
         if (ptx::ld_acquire_gpu(flag) >= count) return true;
         if (*abort) return false;
-        if (ptx::globaltimer() - t0 > kWaitLimitNs) {
+        if (ptx::globaltimer() - t0 > limit_ns) {
             atomicOr(status, kStatusTimeout);
             *abort = 1;
             return false;
