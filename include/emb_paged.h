@@ -110,7 +110,8 @@ EMB_API emb_status emb_qk_norm_rope(const uint16_t* q, int64_t q_stride, const u
  * the largest they are zero). Up to 16 query rows (max_q queries times heads per key/value head), the
  * weights enter the value product as bf16 hi + lo (2^-16); above, they may be rounded once to bf16 (2^-9 each).
  * kv_len above max_pages * page_size counts as that; q_start past n_tokens as n_tokens, and a decreasing
- * q_start as no queries; a page id outside [0, n_pages) as a page of zeros. Rows of O from q_start[n_req] to
+ * q_start as no queries (rows of O that more than one request then claims, or a request and the padding, hold what any of
+ * them gives; if the requests claim more queries than n_tokens in all, the rows of all are undefined); a page id outside [0, n_pages) as a page of zeros. Rows of O from q_start[n_req] to
  * n_tokens (padding) are zeroed.
  * Q, O: bf16 [n_tokens][n_heads][head_dim]; k_cache, v_cache as above, 16-byte aligned; table: int32
  * [n_req][max_pages]; q_start: int32 [n_req + 1], starting at 0; kv_len, prefix: int32 [n_req]. max_q: the most queries

@@ -173,6 +173,7 @@ __device__ __forceinline__ PagedStretch paged_stretch_by(const PagedParams& p) {
     constexpr int kWarps = NT / 32;
     __shared__ PagedPlace found;
     __shared__ uint32_t warp_sum[kWarps], warp_max[kWarps], warp_items[kWarps];
+    __shared__ float warp_claim[kWarps];
     const int tid = kBlock ? int(threadIdx.x) : int(threadIdx.x & 31), lane = tid & 31, warp = tid >> 5;
     int sub = 32, per = 1;
     if constexpr (!ONE) {
@@ -200,8 +201,13 @@ __device__ __forceinline__ PagedStretch paged_stretch_by(const PagedParams& p) {
         return s;
     };
     uint32_t sum = 0;
+    float claim = 0.0f;  // queries of all requests
     for (int k = 0; k < per; ++k)
-        if (r0 + k < p.n_req) sum += units_of(paged_req(p, r0 + k)) * uint32_t(p.Hk);
+        if (r0 + k < p.n_req) {
+            const PagedReq q = paged_req(p, r0 + k);
+            sum += units_of(q) * uint32_t(p.Hk);
+            if (l == 0) claim += float(q.n);
+        }
     __syncwarp();
     uint32_t incl = l == 0 || ONE ? sum : 0u;
     if constexpr (!ONE) {
@@ -211,6 +217,9 @@ __device__ __forceinline__ PagedStretch paged_stretch_by(const PagedParams& p) {
             if (lane >= o) incl += u;
         }
     }
+    if constexpr (!ONE)
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) claim += __shfl_xor_sync(0xffffffffu, claim, o);
     biggest = __reduce_max_sync(0xffffffffu, biggest);
     items = __reduce_add_sync(0xffffffffu, items);
     uint32_t total = ONE ? sum : __shfl_sync(0xffffffffu, incl, 31), before = 0;
@@ -219,17 +228,23 @@ __device__ __forceinline__ PagedStretch paged_stretch_by(const PagedParams& p) {
             warp_sum[warp] = total;
             warp_max[warp] = biggest;
             warp_items[warp] = items;
+            warp_claim[warp] = claim;
         }
         __syncthreads();
         total = biggest = items = 0;
+        claim = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             if (w < warp) before += warp_sum[w];
             total += warp_sum[w];
             biggest = max(biggest, warp_max[w]);
             items += warp_items[w];
+            claim += warp_claim[w];
         }
     }
+    // Starts that go back can let requests claim more queries than there are tokens, and then the units may pass 32 bits:
+    // there is no telling whose work is whose, so none is done.
+    if (!ONE && claim > 1.0001f * float(p.n_tokens)) return PagedStretch{};
     // (lane 0 of a group holds the sum up to and with its group)
     const uint32_t end = ONE ? sum : __shfl_sync(0xffffffffu, incl, lane & ~(sub - 1)) + before, begin = end - sum;
     auto find = [&](uint32_t x) {
