@@ -118,7 +118,7 @@ EMB_API emb_status emb_qk_norm_rope(const uint16_t* q, int64_t q_stride, const u
  * that a request of the call has, as far as the host knows; it picks the kernel, any value >= 1 is right.
  * head_dim 64, 128 or 256, page_size 16, 32, 64, 128 or 256, n_heads / n_kv_heads at most 64 (else
  * EMB_EUNSUPPORTED). 1 <= n_req <= 65536; 1 <= n_tokens < 2^31; n_heads <= 4096; scale and cap finite, cap >= 0; window >= 0;
- * max_pages * page_size < 2^31. A call whose key tiles could number 2^31 is EMB_EUNSUPPORTED.
+ * max_pages * page_size <= 2^31 - 512. A call whose key tiles could number 2^31 is EMB_EUNSUPPORTED.
  * workspace: EMB_PAGED_WORKSPACE bytes (EMB_ENOSPC if ws_bytes says less), 256-byte aligned, zero-filled before its
  * first use; a call leaves it ready for the next one unless emb_paged_status reports EMB_ETIMEOUT: then zero
  * its first 4 KB again. One workspace serves one stream at a time; calls on other streams with a workspace of their own may

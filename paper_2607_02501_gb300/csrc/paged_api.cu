@@ -191,7 +191,8 @@ emb_status emb_paged_attention(const uint16_t* Q, const uint16_t* k_cache, const
     if ((head_dim != 64 && head_dim != 128 && head_dim != 256) || n_heads / n_kv_heads > 64 ||
         (page_size != 16 && page_size != 32 && page_size != 64 && page_size != 128 && page_size != 256))
         return EMB_EUNSUPPORTED;
-    if (max_pages * page_size >= k31 || n_tokens >= k46 / (n_heads * head_dim) ||
+    // (a key's number plus two tiles stays within 31 bits)
+    if (max_pages * page_size > k31 - 512 || n_tokens >= k46 / (n_heads * head_dim) ||
         n_pages * page_size >= k46 / (n_kv_heads * head_dim))
         return EMB_EINVAL;
     const void* rows[] = {Q, k_cache, v_cache, O};

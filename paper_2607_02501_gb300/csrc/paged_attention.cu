@@ -732,7 +732,7 @@ cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s) {
     p.n_req = int(a.n_req);
     p.n_pages = int(a.n_pages);
     while ((int64_t(1) << p.page_shift) < a.page_size) ++p.page_shift;
-    p.kv_limit = int(std::min<int64_t>(a.max_pages * a.page_size, 2147483647));
+    p.kv_limit = int(a.max_pages * a.page_size);
     p.window = int(std::min<int64_t>(a.window, 2147483647));
     p.H = int(a.n_heads);
     p.Hk = int(a.n_kv_heads);
