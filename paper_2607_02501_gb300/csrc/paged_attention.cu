@@ -672,9 +672,11 @@ int few_cluster(const PagedAttnArgs& a) {
     if (a.window > 0) keys = std::min(keys, double(a.window) + kFewRows + kFewTile);
     const double items = double(a.n_req * a.n_kv_heads) * few_blocks(a), tiles = std::ceil(keys / kFewTile);
     const double ctas = (a.head_dim == 256 ? 1.0 : 2.0) * std::max(1, device_sm_count());
-    // a CTA's tiles, at most; more where a cap makes the other kernels dearer (24 requests of up to 7 queries, heads of 64, window
-    // of 1024: capped 18.6 and, by clusters of one, 15.5, uncapped 13.6 and 17.0)
-    const double longest = a.cap > 0.0f ? 24.0 : 16.0;
+    // A CTA's tiles, at most. 144 calls drawn where limits of 16 and 24 differ (1 to 64 requests, heads of 64 to 256, capped and
+    // not, windows and none): with 24 the time is 0.83 of that with 16 called and 0.90 replayed (geometric means), for calls of
+    // up to 16 rows and larger ones, capped and not alike; dearer by more than a tenth for 4 of them called and 9 replayed, by
+    // 0.6 at most (few items of long requests, which stretches spread over more SMs).
+    constexpr double longest = 24.0;
     int S = kFewCluster;
     while (S > 0 && items * S > ctas) S /= 2;
     return S > 0 && tiles <= longest * S && tiles / S <= items * tiles / ctas + 8.0 ? S : 0;
