@@ -33,8 +33,9 @@ __device__ __forceinline__ void ldsm_x4_trans(uint32_t saddr, uint32_t (&r)[4]) 
 // four warps compute. An item has 16 rows (queries times heads), every warp takes 16 of a tile's keys, and the
 // warps' results are merged at the item's end. Scores, softmax in base 2 with a running maximum and the value
 // product (weights as bf16 hi + lo) stay in registers. HBM bounds it: the cache is read once for the 16 rows (64
-// requests of 32 heads on 8 of 128, 100 to 16384 keys: 2.2 GB in 340 us, 97 % of the measured copy rate; 75 % of the DRAM's own
-// peak in the counters, 26 % of the tensor pipe). Small calls are latency: one token over 867 keys 5.9 us.
+// requests of 32 heads on 8 of 128, 100 to 16384 keys: 2.2 GB in 334 to 348 us, 0.94 to 0.98 of the measured copy rate; 78 % of
+// the DRAM's own peak in the counters of a smaller call, 26 % of the tensor pipe). Small calls are latency: one token over 867
+// keys 6.0 to 6.2 us.
 // CL: for few and short requests a cluster of CTAs takes a request's key/value head and shares out its tiles, and
 // the results are joined through distributed shared memory: no search for the work, no workspace.
 constexpr int kFewWarps = 4;
@@ -664,9 +665,10 @@ int few_blocks(const PagedAttnArgs& a) {
 }
 // CTAs of the cluster that takes a block, or 0 where equal stretches of all the work are sooner done: a cluster keeps its
 // CTAs for the longest request that the table has room for, stretches take their share of the total and a join worth eight
-// tiles. Measured (us, stretches and clusters): one token of 8 heads on one of 128 over 867 keys 7.6 and 5.9, 3000 9.5 and
-// 8.8, 6000 10.8 and 12.8; 32 heads on 8 over 4000 13.9 and 10.4; 8 requests of them over 900 16.7 and 8.9; 32 requests on
-// one over up to 1500 14.7 and 8.1.
+// tiles. Measured (us replayed, stretches and clusters; called, stretches take 2 to 3 more, being cooperative): one token of 8
+// heads on one of 128 over 867 keys 7.5 and 6.0, 3000 9.1 and 8.8, 6000 10.0 and 13.1; 32 heads on 8 over 4000 13.0 and 11.0; 8
+// requests of them over 900 16.2 and 8.8; 32 requests on one over up to 1500 14.8 and 8.2. The table's room stands for the
+// length, which the host does not know: one token over 867 keys with room for 16384 takes 7.7 (10.4 called).
 int few_cluster(const PagedAttnArgs& a) {
     double keys = double(a.max_pages * a.page_size);
     if (a.window > 0) keys = std::min(keys, double(a.window) + kFewRows + kFewTile);
@@ -747,9 +749,9 @@ cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s) {
         p.cap2 = float(std::min(kLog2e * double(a.cap), double(FLT_MAX)));
     }
     // Up to 16 rows of a request go to the mma.sync kernel, and more where all its blocks of 16 have a cluster at once: such
-    // calls are small, and it has them sooner done (us, tcgen05 and mma.sync: 50 queries of 8 heads over 866 keys 11.3
-    // and 8.5, 8 over 816 10.3 and 6.8, 24 requests of 3 queries of 14 heads on 2 of 64 12.1 and 7.6, 280 of 8 heads of 64 alone
-    // 10.0 and 6.7). The rest goes to the tcgen05 kernel.
+    // calls are small, and it has them sooner done (us replayed, tcgen05 and mma.sync: 50 queries of 8 heads over 866 keys 11.0
+    // and 8.3, 8 over 816 10.1 and 6.5, 24 requests of 3 queries of 14 heads on 2 of 64 over up to 900 15.4 and 9.7, 280 of 8
+    // heads of 64 alone 9.6 and 6.5). The rest goes to the tcgen05 kernel.
     const bool few = p.G <= 16 && (a.max_q * p.G <= 16 || few_cluster(a) > 0);
     if (!few) {
         p.negate = a.scale < 0.0f;

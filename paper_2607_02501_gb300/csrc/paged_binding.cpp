@@ -6,7 +6,7 @@
 // values behind them, and returns the status, or a sentence if a tensor is not what the call would take it for: the ABI sees
 // addresses and a few sizes only, so a shorter or strided tensor would be read and written beyond its elements. Looking them
 // over takes 0.5 to 1.3 us of the host (a call of emb_paged_slots with its ten tensors 3.8 -> 5.1, of emb_qk_norm_rope
-// 5.8 -> 6.3). bind() is given the addresses of the library's entry points first.
+// 5.7 -> 6.5). bind() is given the addresses of the library's entry points first.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 

@@ -20,7 +20,7 @@ namespace {
 // another; a request that overlaps the CTA's tokens leaves its numbers in shared memory at its first token
 // there, and a maximum scan over those marks gives every token its request. A new page's table entry is written by
 // the token at the page's start, which is always new. Latency bounds it: two dependent loads, two scans (50 tokens of one
-// request 2.9 us, 500 of 1000 requests 4.7, 417000 of 512 requests, 5 MB written, 6.6).
+// request 2.9 to 3.2 us, 500 of 1000 requests 4.7 to 5.0, 417000 of 512 requests, 5 MB written, 6.5).
 constexpr int kSlotTokens = 1024;
 
 struct PageDiv {

@@ -10,10 +10,12 @@
 // grows by more than 2^8 (P and its sums stay far within fp32 and bf16's relative precision), so the output in tensor
 // memory is seldom rescaled. The weights are rounded once to bf16: hi + lo would double the value product for outputs
 // that are rounded to bf16 anyway (error against 64 bits 0.0023 of the outputs' norm, of which 0.0017 is that rounding).
-// What bounds it, measured: heads of 128, 4096 new tokens of 32 heads over 16384 keys 582 us (1650 TFLOP/s, 86 % of the
-// measured matrix rate): by nominal rates the softmax's powers of two (16 a cycle and SM) take as long as the MMAs. Heads of 64: half the MMAs for
-// the same powers. Heads of 256: every key and value is fetched for 128 rows instead of 256, which is probably the bound (2048
-// over 4096, 16 heads 137 us, 129 with the softmax left out; L2's own limit was not measured). Small calls: latency and the join.
+// What bounds it. Heads of 128: 4096 new tokens of 32 heads over 16384 keys take 599 to 639 us, called or replayed (1600 to 1510
+// TFLOP/s, 0.84 to 0.79 of the measured matrix rate; the spread, also between boxes, was not traced); by nominal rates the
+// softmax's powers of two (16 a cycle and SM) take as long as the MMAs. Heads of 64: half the MMAs for the same powers. Heads of
+// 256: not established. Every key and value is fetched for 128 rows instead of 256, and one row tile with one softmax warpgroup
+// leaves a tile's chain of steps exposed (2048 over 4096, 16 heads on 2, 135 us; 129 of then 137 with the softmax left out). Small
+// calls: latency and the join.
 #include <algorithm>
 #include <mutex>
 
@@ -623,7 +625,7 @@ cudaError_t launch_many(PagedParams& p, const PagedAttnArgs& a, cudaStream_t s) 
         }
     }
     // An item has two full row tiles (one with heads of 256), less while the call would leave SMs without a unit: a small
-    // item's partial results are sooner written and joined (50 queries of 8 heads over 866 keys: 256 rows 16.5 us)
+    // item's partial results are sooner written and joined (50 queries of 8 heads over 866 keys: 256 rows 16.2 us, 32 rows 11.0)
     const int sms = std::max(1, device_sm_count());
     p.QT = 128 / p.G;
     p.QB = T::NQ * p.QT;
