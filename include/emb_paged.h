@@ -76,7 +76,8 @@ EMB_API emb_status emb_paged_slots(const int32_t* cached, const int32_t* added, 
  * packed projection's row, or heads * head_dim), multiples of 8 and at least a token's elements.
  * gammas: fp32 [head_dim]. positions: int32 [n_axes][pos_stride], 1 <= n_axes <= 4. axis_of_pair: HOST memory,
  * uint8 [rot_dim / 2] with entries below n_axes, read during the call; NULL: axis 0 for every pair.
- * Angles are formed as two floats: the cosine and sine are within 1e-6 for |position| < 2^24, 1e-5 beyond.
+ * Angles are formed as two floats: the cosine and sine are within 1e-6 for |position| < 2^24, 1e-5 beyond, for base >= 1 (below,
+ * pairs turn faster than one radian a position, and the bounds grow with that).
  * 1 <= n_tokens < 2^31; head_dim % 8 == 0, 8..256; rot_dim % 8 == 0, 0..head_dim; n_heads, n_kv_heads 1..4096;
  * base > 0, eps >= 0. Device pointers 16-byte aligned, but positions (4) and slots (8). No output may
  * overlap another buffer. Errors: EMB_EINVAL, EMB_EALIGN, EMB_ECUDA. */
