@@ -12,6 +12,7 @@
  *   per layer, behind the q/k/v projection of emb_qlayer_seq:
  *     emb_qk_norm_rope   queries and keys normalised and rotated, keys and values stored
  *     emb_paged_attention  the new tokens attend to their request's whole history
+ * or, with the cache in 8 bits (half the bytes, last part of this file), emb_paged8_store and emb_paged8_attention.
  *
  * The cache of one layer is two arrays, K and V, bf16 [n_pages][page_size][n_kv_heads][head_dim].
  * A request's tokens lie in the pages that its row of the block table names, in order: token
@@ -145,6 +146,88 @@ EMB_API emb_status emb_paged_status(emb_stream_t stream);
  * never comes, giving up after timeout_ns nanoseconds (1e3 .. 1e9): emb_paged_status then returns EMB_ETIMEOUT, and the
  * workspace's first 4 KB are to be zeroed. Errors: EMB_EINVAL, EMB_EALIGN, EMB_ENOSPC, EMB_ECUDA. */
 EMB_API emb_status emb_paged_selftest_wait_timeout(void* workspace, size_t ws_bytes, int64_t timeout_ns, emb_stream_t stream);
+
+/* ---- The cache in 8 bits -----------------------------------------------------------------------------------------
+ * A layer's cache is four arrays then. The codes of the keys and of the values, uint8
+ * [n_pages][page_size][n_kv_heads][head_dim], are e4m3 numbers (sign, 4 bits of exponent with bias 7, 3 of mantissa;
+ * largest 448; 0x7F and 0xFF are NaN). The exponents of both, uint8 [n_pages][page_size / 16][n_kv_heads], give each
+ * BLOCK of 16 places of a page and head its power of two: a code c under a byte x stands for c * 2^(x - 127), where x - 127
+ * below -48 counts as -48 and above 48 as 48. A power of two moves no mantissa bits, so a block that takes a larger one
+ * re-encodes what it holds without another rounding, but for codes that become subnormal (below 2^-6 of the new unit). A new cache
+ * needs no initial values. The paper defines no cache format; this one is the library's own. Block tables, slots, positions
+ * and lengths are those above (emb_paged_slots); conventions too. */
+
+/* Section 3.2 (the shared backbone layer). HOST memory, computed on the host: how fast the pairs of a rotary embedding turn.
+ * turns[i], i < rot_dim / 2: the turns per position of pair i in units of 2^-64, modulo one turn. Pair i turns by
+ * f_i = base^(-2 i / rot_dim) radians a position. For contexts longer than the `original` one that the model was made for
+ * (stretch > 1): f_i * (k + (1 - k) / stretch), with k = 0 if original = 0 (every position is divided by stretch), else
+ * k = clamp((original * f_i / 2 pi - low) / (high - low), 0, 1): pairs that turn `high` times within the original context
+ * keep their rate, those that turn `low` times or less are stretched.
+ * rot_dim even, 2..256; base > 0; stretch >= 1; original >= 0; 0 <= low < high. Errors: EMB_EINVAL. */
+EMB_API emb_status emb_rotary_turns(int64_t rot_dim, double base, double stretch, double original, double low, double high,
+                                    uint64_t* turns);
+
+/* Section 3.2, principle 2 (fusion: one pass from the projections to the cache).
+ * Per-head RMSNorm of queries and keys (skipped where the gamma is NULL), rotary embedding, and the store into the cache.
+ * For token t, every query head and every key head x [head_dim]:
+ *   y_i = x_i / sqrt(mean_i x_i^2 + eps) * gamma_i  (fp32; y = x without gamma);
+ *   pair i < rot_dim / 2 is (y_i, y_(i + rot_dim / 2)), or with `neighbours` (y_2i, y_(2i + 1)); it is turned by
+ *     positions[axis_of_pair[i]][t] * turns[i]: (a, b) -> factor * (a cos - b sin, b cos + a sin); elements from rot_dim on stay y.
+ * Queries go to q_out [n_tokens][n_heads][head_dim], rounded once to bf16. Keys and the values (as they are) go to slot slots[t]
+ * in 8 bits; a token whose slot is negative or beyond the cache stores neither. For a block and head that tokens of the
+ * call are stored in, keys and values alike, with `need` the least exponent in -48..48 under which the largest of their magnitudes
+ * is at most 448 (not counting those above 448 * 2^48, infinities and NaN):
+ *   if place 0 of the block is among them, its exponent becomes `need` and the places that the call does not store to become zero
+ *     (a block starts anew, whatever it held);
+ *   else its exponent becomes the larger of its own and `need`, and the places that the call does not store to keep their
+ *     values, re-encoded under it.
+ * Each element is rounded once, to the nearest code (ties to even); magnitudes above 448 * 2^48 (1.26e17), infinities and NaN
+ * become the NaN code.
+ * The tokens of a call that share a block stand within 16 consecutive tokens (those that emb_paged_slots gives stand side by
+ * side); blocks for which that does not hold, or slots that come twice, hold undefined values afterwards.
+ * q, k, v: bf16, heads of a token contiguous, tokens q_stride, k_stride, v_stride elements apart, multiples of 8 and at least a
+ * token's elements. gammas: fp32 [head_dim]. positions: int32 [n_axes][pos_stride], 1 <= n_axes <= 4, any value.
+ * turns: device, uint64 [rot_dim / 2] (emb_rotary_turns), may be NULL if rot_dim is 0; axis_of_pair: device, uint8 [rot_dim / 2], entries of
+ * n_axes or more count as n_axes - 1; NULL: axis 0 for every pair. The angle is exact modulo a turn but for the rounding of turns[i]
+ * (2^-65 turns a position); cosine and sine are within 1e-6.
+ * 1 <= n_tokens < 2^31; head_dim 64, 128 or 256, page_size 16, 32, 64, 128 or 256 (else EMB_EUNSUPPORTED); rot_dim % 8 == 0,
+ * 0..head_dim; n_heads, n_kv_heads 1..4096; eps >= 0 and factor finite. Device pointers 16-byte aligned, but positions (4), slots and
+ * turns (8), exponents and axis_of_pair (1). No output may overlap another buffer. Errors: EMB_EINVAL, EMB_EALIGN, EMB_EUNSUPPORTED,
+ * EMB_ECUDA. */
+EMB_API emb_status emb_paged8_store(const uint16_t* q, int64_t q_stride, const uint16_t* k, int64_t k_stride,
+                                    const uint16_t* v, int64_t v_stride, int64_t n_tokens, int64_t n_heads,
+                                    int64_t n_kv_heads, int64_t head_dim, const float* q_gamma, const float* k_gamma,
+                                    float eps, const int32_t* positions, int64_t pos_stride, int64_t n_axes,
+                                    const uint8_t* axis_of_pair, const uint64_t* turns, int64_t rot_dim, int32_t neighbours,
+                                    float factor, const int64_t* slots, uint16_t* q_out, uint8_t* k_codes, uint8_t* v_codes,
+                                    uint8_t* k_exp, uint8_t* v_exp, int64_t n_pages, int64_t page_size, emb_stream_t stream);
+
+/* Section 3.1 ("prefix once, head many": what the cache holds, for other uses).
+ * Rows of the cache as bf16 (exact): row i of k_out and v_out, [n_rows][n_kv_heads][head_dim], is what slot slots[i] holds;
+ * zeros where that is negative or beyond the cache. Slots may repeat.
+ * 0 <= n_rows < 2^31; sizes as for emb_paged8_store; codes and outputs 16-byte aligned, slots 8. No output may overlap another
+ * buffer. Errors: EMB_EINVAL, EMB_EALIGN, EMB_EUNSUPPORTED, EMB_ECUDA. */
+EMB_API emb_status emb_paged8_read(const uint8_t* k_codes, const uint8_t* v_codes, const uint8_t* k_exp, const uint8_t* v_exp,
+                                   int64_t n_pages, int64_t page_size, int64_t n_kv_heads, int64_t head_dim,
+                                   const int64_t* slots, int64_t n_rows, uint16_t* k_out, uint16_t* v_out,
+                                   emb_stream_t stream);
+
+/* Section 3.1 and Section 3.2, as emb_paged_attention, whose arguments, masks, limits, workspace and treatment of impossible
+ * lengths, pages, hidden and odd values this call shares, over keys and values that are the codes' values.
+ * Queries enter the score product as f16 times a power of two per query and head: exact, but for elements below 2^-28 of the
+ * row's largest magnitude, which are within 2^-39 of that. The scores of a block are multiplied by its power of two in fp32. A
+ * weight, times its block's power for the values, enters the value product rounded once to f16: within a relative 2^-11, or within
+ * 2^-31 of the row's largest such product. A page id outside [0, n_pages) is a page of zeros. A NaN code in a visible key makes
+ * its queries' outputs NaN, one in a visible value that element of them. One workspace serves this call and emb_paged_attention
+ * in turn.
+ * Codes 16-byte aligned. Errors: those of emb_paged_attention. */
+EMB_API emb_status emb_paged8_attention(const uint16_t* Q, const uint8_t* k_codes, const uint8_t* v_codes,
+                                        const uint8_t* k_exp, const uint8_t* v_exp, int64_t n_pages, int64_t page_size,
+                                        const int32_t* table, int64_t max_pages, const int32_t* q_start,
+                                        const int32_t* kv_len, const int32_t* prefix, int64_t n_req, int64_t n_tokens,
+                                        int64_t max_q, uint16_t* O, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim,
+                                        float scale, float cap, int64_t window, void* workspace, size_t ws_bytes,
+                                        emb_stream_t stream);
 
 #ifdef __cplusplus
 }

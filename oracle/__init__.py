@@ -276,3 +276,5 @@ from .layer import attention_reference, rmsnorm_reference, rope_reference  # noq
 
 # The paged key/value cache (slots, norm with rotation and cache write, attention): oracle/paged.py.
 from .paged import paged_attention_reference, paged_slots_reference, qk_norm_rope_reference  # noqa: E402,F401
+from .paged8 import (bf16_bound, e4m3_codes, e4m3_values, exponent_of, need_of, norm_turn_reference,  # noqa: E402,F401
+                     paged8_encode, paged8_store_reference, paged8_values, rotary_turns_reference)

@@ -148,9 +148,16 @@ def paged_lib():
     L.emb_paged_attention.argtypes = [vp, vp, vp, i64, i64, vp, i64, vp, vp, vp, i64, i64, i64, vp, i64, i64,
                                       i64, f32, f32, i64, vp, ctypes.c_size_t, vp]
     L.emb_paged_status.argtypes = [vp]
+    f64, i32 = ctypes.c_double, ctypes.c_int32
+    L.emb_rotary_turns.argtypes = [i64, f64, f64, f64, f64, f64, vp]
+    L.emb_paged8_store.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i64, i64, vp, vp, f32, vp, i64, i64, vp, vp, i64, i32, f32,
+                                   vp, vp, vp, vp, vp, vp, i64, i64, vp]
+    L.emb_paged8_read.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, vp, i64, vp, vp, vp]
+    L.emb_paged8_attention.argtypes = [vp, vp, vp, vp, vp, i64, i64, vp, i64, vp, vp, vp, i64, i64, i64, vp, i64, i64,
+                                       i64, f32, f32, i64, vp, ctypes.c_size_t, vp]
     L.emb_paged_selftest_wait_timeout.argtypes = [vp, ctypes.c_size_t, i64, vp]
     for name in ("emb_paged_slots", "emb_qk_norm_rope", "emb_paged_attention", "emb_paged_status",
-                 "emb_paged_selftest_wait_timeout"):
+                 "emb_paged_selftest_wait_timeout", "emb_rotary_turns", "emb_paged8_store", "emb_paged8_read", "emb_paged8_attention"):
         getattr(L, name).restype = ctypes.c_int
     _paged = L
     return L
@@ -168,7 +175,9 @@ def _binding():
         if not os.path.exists(BINDING):  # (another interpreter's must not be taken for it)
             raise RuntimeError(f"{BINDING} is missing: run paper_2607_02501_gb300.build() with this interpreter first")
         from . import _paged_binding as m
-        m.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.emb_paged_slots, L.emb_qk_norm_rope, L.emb_paged_attention)))
+        address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
+        m.bind(*map(address, (L.emb_paged_slots, L.emb_qk_norm_rope, L.emb_paged_attention)))
+        m.bind8(*map(address, (L.emb_paged8_store, L.emb_paged8_read, L.emb_paged8_attention)))
         _marshal = m
     return _marshal
 
@@ -453,8 +462,54 @@ def emb_paged_attention(Q, k_cache, v_cache, table, q_start, kv_len, O, scale: f
         _refused(status, "emb_paged_attention")
 
 
+def emb_rotary_turns(rot_dim: int, base: float = 10000.0, stretch: float = 1.0, original: float = 0.0, low: float = 1.0,
+                     high: float = 32.0):
+    """How fast the pairs of a rotary embedding turn, for emb_paged8_store: an int64 tensor [rot_dim / 2] in host memory
+    (the bits of unsigned numbers)."""
+    import torch
+    turns = torch.zeros(max(rot_dim, 0) // 2, dtype=torch.int64)
+    _check(paged_lib().emb_rotary_turns(rot_dim, base, stretch, original, low, high, _ptr(turns)), "emb_rotary_turns")
+    return turns
+
+
+def emb_paged8_store(q, k, v, q_out, k_codes, v_codes, k_exp, v_exp, slots, positions, turns, q_gamma=None, k_gamma=None,
+                     eps: float = 1e-6, axis_of_pair=None, neighbours: bool = False, factor: float = 1.0, stream=None) -> None:
+    """q: bf16 [T][H * d], k, v: bf16 [T][Hk * d] (rows may be strided); q_out: bf16 [T][H * d]; codes: uint8 (or e4m3)
+    [n_pages][page_size][Hk][d]; exponents: uint8 [n_pages][page_size / 16][Hk]; slots: int64 [T]; positions: int32 [T] or
+    [n_axes][T]; turns: int64 [rot_dim / 2] on the device (emb_rotary_turns), None: no rotation; gammas: fp32 [d]; axis_of_pair:
+    uint8 [rot_dim / 2] on the device."""
+    status = (_marshal or _binding()).store8(q, k, v, q_out, k_codes, v_codes, k_exp, v_exp, slots, positions, turns, q_gamma,
+                                             k_gamma, axis_of_pair, eps, neighbours, factor, _stream(stream))
+    if status:
+        _refused(status, "emb_paged8_store")
+
+
+def emb_paged8_read(k_codes, v_codes, k_exp, v_exp, slots, k_out, v_out, stream=None) -> None:
+    """The cache as for emb_paged8_store; slots: int64 [n]; k_out, v_out: bf16 [n][Hk * d]."""
+    status = (_marshal or _binding()).read8(k_codes, v_codes, k_exp, v_exp, slots, k_out, v_out, _stream(stream))
+    if status:
+        _refused(status, "emb_paged8_read")
+
+
+def emb_paged8_attention(Q, k_codes, v_codes, k_exp, v_exp, table, q_start, kv_len, O, scale: float, max_q: int,
+                         workspace, prefix=None, cap: float = 0.0, window: int = 0, stream=None) -> None:
+    """The cache as for emb_paged8_store, everything else as for emb_paged_attention."""
+    status = (_marshal or _binding()).attention8(Q, k_codes, v_codes, k_exp, v_exp, table, q_start, kv_len, O, workspace, prefix,
+                                                 scale, max_q, cap, window, workspace.nbytes, _stream(stream))
+    if status:
+        _refused(status, "emb_paged8_attention")
+
+
+def paged8_cache(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, device=None):
+    """A layer's cache in 8 bits on the current (or given) CUDA device: (k_codes, v_codes, k_exp, v_exp), all zeros."""
+    import torch
+    new = lambda *shape: torch.zeros(*shape, dtype=torch.uint8, device=device if device is not None else "cuda")
+    codes, exps = (n_pages, page_size, n_kv_heads, head_dim), (n_pages, page_size // 16, n_kv_heads)
+    return new(*codes), new(*codes), new(*exps), new(*exps)
+
+
 def paged_workspace(device=None):
-    """A zero-filled workspace for emb_paged_attention on the current (or given) CUDA device."""
+    """A zero-filled workspace for emb_paged_attention and emb_paged8_attention on the current (or given) CUDA device."""
     import torch
     return torch.zeros(EMB_PAGED_WORKSPACE, dtype=torch.uint8, device=device if device is not None else "cuda")
 

@@ -1,9 +1,10 @@
 // C ABI of libembpaged.so (declarations and contracts in include/emb_paged.h): argument validation, every
 // error reported before anything is enqueued, and the status word that bounded device-side waits report into.
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 
-#include "paged.cuh"
+#include "paged8.cuh"
 
 namespace emb {
 namespace {
@@ -55,6 +56,71 @@ bool clash(const Span* outs, int n_out, const Span* ins, int n_in) {
 }
 emb_status from_cuda(cudaError_t e) { return e == cudaSuccess ? EMB_OK : EMB_ECUDA; }
 cudaStream_t stream_of(emb_stream_t s) { return reinterpret_cast<cudaStream_t>(s); }
+
+bool cache8_supported(int64_t head_dim, int64_t page_size) {
+    return (head_dim == 64 || head_dim == 128 || head_dim == 256) &&
+           (page_size == 16 || page_size == 32 || page_size == 64 || page_size == 128 || page_size == 256);
+}
+
+// The checks of an attention call over a cache whose elements have `size` bytes, and its arguments for a launch. `exps`: what else
+// the cache consists of, or nothing.
+emb_status attention_args(PagedAttnArgs& a, int64_t size, const Span (&exps)[2], const uint16_t* Q, const void* k_cache,
+                          const void* v_cache, int64_t n_pages, int64_t page_size, const int32_t* table, int64_t max_pages,
+                          const int32_t* q_start, const int32_t* kv_len, const int32_t* prefix, int64_t n_req, int64_t n_tokens,
+                          int64_t max_q, uint16_t* O, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim, float scale,
+                          float cap, int64_t window, void* workspace, size_t ws_bytes) {
+    if (!within(n_req, 1, 65537) || !within(n_tokens, 1, k31) || !within(n_pages, 1, k31) || max_q < 1 ||
+        !within(max_pages, 1, k31) || !within(n_heads, 1, 4097) || n_kv_heads < 1 || n_heads % n_kv_heads != 0 ||
+        !std::isfinite(scale) || !std::isfinite(cap) || cap < 0.0f || window < 0 || head_dim < 1 || page_size < 1 ||
+        n_req * max_pages >= k46)
+        return EMB_EINVAL;
+    if (!Q || !k_cache || !v_cache || !table || !q_start || !kv_len || !O || !workspace) return EMB_EINVAL;
+    if ((head_dim != 64 && head_dim != 128 && head_dim != 256) || n_heads / n_kv_heads > 64 ||
+        (page_size != 16 && page_size != 32 && page_size != 64 && page_size != 128 && page_size != 256))
+        return EMB_EUNSUPPORTED;
+    // (a key's number plus two tiles stays within 31 bits)
+    if (max_pages * page_size > k31 - 512 || n_tokens >= k46 / (n_heads * head_dim) ||
+        n_pages * page_size >= k46 / (n_kv_heads * head_dim))
+        return EMB_EINVAL;
+    const void* rows[] = {Q, k_cache, v_cache, O};
+    for (const void* w : rows)
+        if (!aligned(w, 16)) return EMB_EALIGN;
+    const void* ints[] = {table, q_start, kv_len, prefix};
+    for (const void* w : ints)
+        if (!aligned(w, 4)) return EMB_EALIGN;
+    if (!aligned(workspace, 256)) return EMB_EALIGN;
+    if (ws_bytes < EMB_PAGED_WORKSPACE) return EMB_ENOSPC;
+    const int64_t rows_bytes = n_tokens * n_heads * head_dim * 2, cache = n_pages * page_size * n_kv_heads * head_dim * size;
+    const Span ins[] = {{Q, rows_bytes}, {k_cache, cache}, {v_cache, cache}, {table, n_req * max_pages * 4},
+                        {q_start, (n_req + 1) * 4}, {kv_len, n_req * 4}, {prefix, n_req * 4}, exps[0], exps[1]};
+    const Span outs[] = {{O, rows_bytes}, {workspace, int64_t(EMB_PAGED_WORKSPACE)}};
+    if (clash(outs, 2, ins, 9)) return EMB_EINVAL;
+    a = PagedAttnArgs{};
+    a.Q = Q;
+    a.k_cache = static_cast<const uint16_t*>(k_cache);
+    a.v_cache = static_cast<const uint16_t*>(v_cache);
+    a.table = table;
+    a.q_start = q_start;
+    a.kv_len = kv_len;
+    a.prefix = prefix;
+    a.O = O;
+    a.workspace = workspace;
+    a.n_pages = n_pages;
+    a.page_size = page_size;
+    a.max_pages = max_pages;
+    a.n_req = n_req;
+    a.n_tokens = n_tokens;
+    a.max_q = max_q;
+    a.n_heads = n_heads;
+    a.n_kv_heads = n_kv_heads;
+    a.head_dim = head_dim;
+    a.window = window;
+    a.scale = scale;
+    a.cap = cap;
+    if (paged_attention_tiles(a) >= double(k31)) return EMB_EUNSUPPORTED;
+    a.status = device_words(false);
+    return a.status ? EMB_OK : EMB_ECUDA;
+}
 
 }  // namespace
 
@@ -182,58 +248,11 @@ emb_status emb_paged_attention(const uint16_t* Q, const uint16_t* k_cache, const
                                int64_t n_tokens, int64_t max_q, uint16_t* O, int64_t n_heads, int64_t n_kv_heads,
                                int64_t head_dim, float scale, float cap, int64_t window, void* workspace,
                                size_t ws_bytes, emb_stream_t stream) {
-    if (!within(n_req, 1, 65537) || !within(n_tokens, 1, k31) || !within(n_pages, 1, k31) || max_q < 1 ||
-        !within(max_pages, 1, k31) || !within(n_heads, 1, 4097) || n_kv_heads < 1 || n_heads % n_kv_heads != 0 ||
-        !std::isfinite(scale) || !std::isfinite(cap) || cap < 0.0f || window < 0 || head_dim < 1 || page_size < 1 ||
-        n_req * max_pages >= k46)
-        return EMB_EINVAL;
-    if (!Q || !k_cache || !v_cache || !table || !q_start || !kv_len || !O || !workspace) return EMB_EINVAL;
-    if ((head_dim != 64 && head_dim != 128 && head_dim != 256) || n_heads / n_kv_heads > 64 ||
-        (page_size != 16 && page_size != 32 && page_size != 64 && page_size != 128 && page_size != 256))
-        return EMB_EUNSUPPORTED;
-    // (a key's number plus two tiles stays within 31 bits)
-    if (max_pages * page_size > k31 - 512 || n_tokens >= k46 / (n_heads * head_dim) ||
-        n_pages * page_size >= k46 / (n_kv_heads * head_dim))
-        return EMB_EINVAL;
-    const void* rows[] = {Q, k_cache, v_cache, O};
-    for (const void* w : rows)
-        if (!aligned(w, 16)) return EMB_EALIGN;
-    const void* ints[] = {table, q_start, kv_len, prefix};
-    for (const void* w : ints)
-        if (!aligned(w, 4)) return EMB_EALIGN;
-    if (!aligned(workspace, 256)) return EMB_EALIGN;
-    if (ws_bytes < EMB_PAGED_WORKSPACE) return EMB_ENOSPC;
-    const int64_t rows_bytes = n_tokens * n_heads * head_dim * 2, cache = n_pages * page_size * n_kv_heads * head_dim * 2;
-    const Span ins[] = {{Q, rows_bytes}, {k_cache, cache}, {v_cache, cache}, {table, n_req * max_pages * 4},
-                        {q_start, (n_req + 1) * 4}, {kv_len, n_req * 4}, {prefix, n_req * 4}};
-    const Span outs[] = {{O, rows_bytes}, {workspace, int64_t(EMB_PAGED_WORKSPACE)}};
-    if (clash(outs, 2, ins, 7)) return EMB_EINVAL;
-    PagedAttnArgs a = {};
-    a.Q = Q;
-    a.k_cache = k_cache;
-    a.v_cache = v_cache;
-    a.table = table;
-    a.q_start = q_start;
-    a.kv_len = kv_len;
-    a.prefix = prefix;
-    a.O = O;
-    a.workspace = workspace;
-    a.n_pages = n_pages;
-    a.page_size = page_size;
-    a.max_pages = max_pages;
-    a.n_req = n_req;
-    a.n_tokens = n_tokens;
-    a.max_q = max_q;
-    a.n_heads = n_heads;
-    a.n_kv_heads = n_kv_heads;
-    a.head_dim = head_dim;
-    a.window = window;
-    a.scale = scale;
-    a.cap = cap;
-    if (paged_attention_tiles(a) >= double(k31)) return EMB_EUNSUPPORTED;
-    a.status = device_words(false);
-    if (!a.status) return EMB_ECUDA;
-    return from_cuda(launch_paged_attention(a, stream_of(stream)));
+    PagedAttnArgs a;
+    const emb_status e = attention_args(a, 2, {{nullptr, 0}, {nullptr, 0}}, Q, k_cache, v_cache, n_pages, page_size, table, max_pages,
+                                        q_start, kv_len, prefix, n_req, n_tokens, max_q, O, n_heads, n_kv_heads, head_dim, scale,
+                                        cap, window, workspace, ws_bytes);
+    return e != EMB_OK ? e : from_cuda(launch_paged_attention(a, stream_of(stream)));
 }
 
 emb_status emb_paged_status(emb_stream_t stream) {
@@ -258,6 +277,138 @@ emb_status emb_paged_selftest_wait_timeout(void* workspace, size_t ws_bytes, int
     int* st = device_words(false);
     if (!st) return EMB_ECUDA;
     return from_cuda(launch_paged_selftest(workspace, uint64_t(timeout_ns), st, stream_of(stream)));
+}
+
+// ------------------------------------------------------------------ the 8-bit cache (include/emb_paged.h)
+
+emb_status emb_rotary_turns(int64_t rot_dim, double base, double stretch, double original, double low, double high, uint64_t* turns) {
+    if (!within(rot_dim, 2, 257) || rot_dim % 2 != 0 || !(base > 0.0) || !std::isfinite(base) || !(stretch >= 1.0) ||
+        !std::isfinite(stretch) || !(original >= 0.0) || !std::isfinite(original) || !(low >= 0.0) || !(high > low) ||
+        !std::isfinite(high) || !turns)
+        return EMB_EINVAL;
+    constexpr double kTurn = 6.283185307179586476925;
+    for (int64_t i = 0; i < rot_dim / 2; ++i) {
+        double f = std::pow(base, -2.0 * double(i) / double(rot_dim)) / kTurn;  // turns a position
+        if (stretch > 1.0) {
+            const double keep = original > 0.0 ? std::min(1.0, std::max(0.0, (original * f - low) / (high - low))) : 0.0;
+            f *= keep + (1.0 - keep) / stretch;
+        }
+        f -= std::floor(f);  // whole turns are none
+        const double units = std::floor(std::ldexp(f, 64) + 0.5);
+        turns[i] = units >= 18446744073709551616.0 ? 0 : uint64_t(units);
+    }
+    return EMB_OK;
+}
+
+emb_status emb_paged8_store(const uint16_t* q, int64_t q_stride, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                            int64_t v_stride, int64_t n_tokens, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim,
+                            const float* q_gamma, const float* k_gamma, float eps, const int32_t* positions, int64_t pos_stride,
+                            int64_t n_axes, const uint8_t* axis_of_pair, const uint64_t* turns, int64_t rot_dim,
+                            int32_t neighbours, float factor, const int64_t* slots, uint16_t* q_out, uint8_t* k_codes,
+                            uint8_t* v_codes, uint8_t* k_exp, uint8_t* v_exp, int64_t n_pages, int64_t page_size,
+                            emb_stream_t stream) {
+    if (head_dim < 1 || page_size < 1) return EMB_EINVAL;
+    if (!cache8_supported(head_dim, page_size)) return EMB_EUNSUPPORTED;
+    if (!within(n_tokens, 1, k31) || !within(n_heads, 1, 4097) || !within(n_kv_heads, 1, 4097) ||
+        !within(rot_dim, 0, head_dim + 1) || rot_dim % 8 != 0 || !within(n_axes, 1, 5) ||
+        !within(pos_stride, n_tokens, k46) || !within(n_pages, 1, k31) || !(eps >= 0.0f) || !std::isfinite(eps) ||
+        !std::isfinite(factor) || (neighbours != 0 && neighbours != 1))
+        return EMB_EINVAL;
+    const int64_t qw = n_heads * head_dim, kw = n_kv_heads * head_dim;
+    const int64_t strides[] = {q_stride - qw, k_stride - kw, v_stride - kw};
+    for (int64_t over : strides)
+        if (over < 0 || over % 8 != 0) return EMB_EINVAL;
+    if (q_stride >= k46 / n_tokens || k_stride >= k46 / n_tokens || v_stride >= k46 / n_tokens || n_pages * page_size >= k46 / kw)
+        return EMB_EINVAL;
+    // (its CTAs stay within a launch's grid)
+    if (n_tokens * (n_heads + n_kv_heads) >= (int64_t(1) << 34)) return EMB_EUNSUPPORTED;
+    if (!q || !k || !v || !positions || (rot_dim > 0 && !turns) || !slots || !q_out || !k_codes || !v_codes || !k_exp || !v_exp)
+        return EMB_EINVAL;
+    const void* rows[] = {q, k, v, q_gamma, k_gamma, q_out, k_codes, v_codes};
+    for (const void* w : rows)
+        if (!aligned(w, 16)) return EMB_EALIGN;
+    if (!aligned(positions, 4) || !aligned(slots, 8) || !aligned(turns, 8)) return EMB_EALIGN;
+    auto rows_bytes = [&](int64_t stride, int64_t width) { return ((n_tokens - 1) * stride + width) * 2; };
+    const Span ins[] = {{q, rows_bytes(q_stride, qw)}, {k, rows_bytes(k_stride, kw)}, {v, rows_bytes(v_stride, kw)},
+                        {q_gamma, head_dim * 4}, {k_gamma, head_dim * 4},
+                        {positions, ((n_axes - 1) * pos_stride + n_tokens) * 4}, {slots, n_tokens * 8},
+                        {turns, rot_dim / 2 * 8}, {axis_of_pair, rot_dim / 2}};
+    const int64_t codes = n_pages * page_size * kw, exps = n_pages * (page_size / kBlock8) * n_kv_heads;
+    const Span outs[] = {{q_out, n_tokens * qw * 2}, {k_codes, codes}, {v_codes, codes}, {k_exp, exps}, {v_exp, exps}};
+    if (clash(outs, 5, ins, 9)) return EMB_EINVAL;
+    Store8Args a = {};
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_gamma = q_gamma;
+    a.k_gamma = k_gamma;
+    a.positions = positions;
+    a.axis_of_pair = axis_of_pair;
+    a.turns = turns;
+    a.slots = slots;
+    a.q_out = q_out;
+    a.k_codes = k_codes;
+    a.v_codes = v_codes;
+    a.k_exp = k_exp;
+    a.v_exp = v_exp;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.pos_stride = pos_stride;
+    a.n_tokens = n_tokens;
+    a.n_slots = n_pages * page_size;
+    a.n_heads = int(n_heads);
+    a.n_kv_heads = int(n_kv_heads);
+    a.head_dim = int(head_dim);
+    a.rot_dim = int(rot_dim);
+    a.n_axes = int(n_axes);
+    a.eps = eps;
+    a.factor = factor;
+    a.neighbours = neighbours != 0;
+    return from_cuda(launch_paged8_store(a, stream_of(stream)));
+}
+
+emb_status emb_paged8_read(const uint8_t* k_codes, const uint8_t* v_codes, const uint8_t* k_exp, const uint8_t* v_exp,
+                           int64_t n_pages, int64_t page_size, int64_t n_kv_heads, int64_t head_dim, const int64_t* slots,
+                           int64_t n_rows, uint16_t* k_out, uint16_t* v_out, emb_stream_t stream) {
+    if (!within(n_rows, 0, k31) || !within(n_kv_heads, 1, 4097) || !within(n_pages, 1, k31) || head_dim < 1 || page_size < 1)
+        return EMB_EINVAL;
+    if (!cache8_supported(head_dim, page_size)) return EMB_EUNSUPPORTED;
+    const int64_t kw = n_kv_heads * head_dim;
+    if (n_pages * page_size >= k46 / kw || n_rows >= k46 / kw) return EMB_EINVAL;
+    if (!k_codes || !v_codes || !k_exp || !v_exp || (n_rows > 0 && (!slots || !k_out || !v_out))) return EMB_EINVAL;
+    const void* rows[] = {k_codes, v_codes, k_out, v_out};
+    for (const void* w : rows)
+        if (!aligned(w, 16)) return EMB_EALIGN;
+    if (!aligned(slots, 8)) return EMB_EALIGN;
+    const int64_t codes = n_pages * page_size * kw, exps = n_pages * (page_size / kBlock8) * n_kv_heads;
+    const Span ins[] = {{k_codes, codes}, {v_codes, codes}, {k_exp, exps}, {v_exp, exps}, {slots, n_rows * 8}};
+    const Span outs[] = {{k_out, n_rows * kw * 2}, {v_out, n_rows * kw * 2}};
+    if (clash(outs, 2, ins, 5)) return EMB_EINVAL;
+    if (n_rows == 0) return EMB_OK;
+    Read8Args a = {k_codes, v_codes, k_exp, v_exp, slots, k_out, v_out, n_rows, n_pages * page_size, int(n_kv_heads), int(head_dim)};
+    return from_cuda(launch_paged8_read(a, stream_of(stream)));
+}
+
+emb_status emb_paged8_attention(const uint16_t* Q, const uint8_t* k_codes, const uint8_t* v_codes, const uint8_t* k_exp,
+                                const uint8_t* v_exp, int64_t n_pages, int64_t page_size, const int32_t* table,
+                                int64_t max_pages, const int32_t* q_start, const int32_t* kv_len, const int32_t* prefix,
+                                int64_t n_req, int64_t n_tokens, int64_t max_q, uint16_t* O, int64_t n_heads,
+                                int64_t n_kv_heads, int64_t head_dim, float scale, float cap, int64_t window, void* workspace,
+                                size_t ws_bytes, emb_stream_t stream) {
+    Paged8AttnArgs a;
+    if (!k_exp || !v_exp) return EMB_EINVAL;
+    // (sizes that make no sense are refused below; here they only must not overflow)
+    const bool sane = within(n_pages, 1, k31) && within(page_size, 1, 65537) && within(n_kv_heads, 1, 4097);
+    const int64_t exps = sane ? n_pages * (page_size / kBlock8) * n_kv_heads : 0;
+    const emb_status e = attention_args(a.a, 1, {{k_exp, exps}, {v_exp, exps}}, Q, k_codes, v_codes, n_pages, page_size, table,
+                                        max_pages, q_start, kv_len, prefix, n_req, n_tokens, max_q, O, n_heads, n_kv_heads,
+                                        head_dim, scale, cap, window, workspace, ws_bytes);
+    if (e != EMB_OK) return e;
+    if (n_heads / n_kv_heads > 16) return EMB_EUNSUPPORTED;
+    a.k_exp = k_exp;
+    a.v_exp = v_exp;
+    return from_cuda(launch_paged8_attention(a, stream_of(stream)));
 }
 
 }  // extern "C"

@@ -6,7 +6,7 @@
 #include <cstring>
 #include <mutex>
 
-#include "paged_math.cuh"
+#include "paged8.cuh"
 
 namespace emb {
 namespace {
@@ -610,6 +610,18 @@ bool encode_cache(CUtensorMap* m, const void* base, const PagedAttnArgs& a, uint
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool encode_codes(CUtensorMap* m, const void* base, const PagedAttnArgs& a, uint32_t box) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t D = cuuint64_t(a.head_dim), Hk = cuuint64_t(a.n_kv_heads), P = cuuint64_t(a.page_size);
+    const cuuint64_t dims[4] = {D, Hk, P, cuuint64_t(a.n_pages)};
+    const cuuint64_t strides[3] = {D, Hk * D, P * Hk * D};
+    const cuuint32_t boxes[4] = {cuuint32_t(std::min<cuuint64_t>(D, 128)), 1, box, 1}, ones[4] = {1, 1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, boxes, ones,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool encode_queries(CUtensorMap* m, const PagedAttnArgs& a, uint32_t heads, uint32_t tokens) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
@@ -717,7 +729,7 @@ cudaError_t launch_paged_selftest(void* workspace, uint64_t limit_ns, int* statu
     return cudaGetLastError();
 }
 
-cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s) {
+PagedParams paged_params(const PagedAttnArgs& a) {
     PagedParams p;
     std::memset(&p, 0, sizeof(p));
     p.Q = reinterpret_cast<const __nv_bfloat16*>(a.Q);
@@ -748,6 +760,11 @@ cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s) {
         p.scale2 = float(std::max(-double(FLT_MAX), std::min(2.0 * kLog2e * double(a.scale) / double(a.cap), double(FLT_MAX))));
         p.cap2 = float(std::min(kLog2e * double(a.cap), double(FLT_MAX)));
     }
+    return p;
+}
+
+cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t s) {
+    PagedParams p = paged_params(a);
     // Up to 16 rows of a request go to the mma.sync kernel, and more where all its blocks of 16 have a cluster at once: such
     // calls are small, and it has them sooner done (us replayed, tcgen05 and mma.sync: 50 queries of 8 heads over 866 keys 11.0
     // and 8.3, 8 over 816 10.1 and 6.5, 24 requests of 3 queries of 14 heads on 2 of 64 over up to 900 15.4 and 9.7, 280 of 8

@@ -19,6 +19,9 @@ namespace {
 decltype(&emb_paged_slots) f_slots;
 decltype(&emb_qk_norm_rope) f_qk;
 decltype(&emb_paged_attention) f_attention;
+decltype(&emb_paged8_store) f_store8;
+decltype(&emb_paged8_read) f_read8;
+decltype(&emb_paged8_attention) f_attention8;
 PyObject *s_data_ptr, *s_shape, *s_stride, *s_nbytes, *s_itemsize, *s_is_contiguous;
 
 // Reads arguments one after another; `ok` turns false, with a Python exception set, at the first that cannot be read.
@@ -102,6 +105,34 @@ struct Reader {
         else if (bytes / size < count) refuse("%s has %lld elements, %lld needed", name, static_cast<long long>(bytes / size), static_cast<long long>(count));
         contiguous(o, name);
     }
+    // Positions of T tokens, [tokens] or [axes][tokens]: their axes and the elements between those. False: an exception is set.
+    bool positions(PyObject* o, int64_t T, int64_t& axes, int64_t& pos_stride) {
+        if (!ok) return true;
+        PyObject* shape = PyObject_GetAttr(o, s_shape);
+        const bool several = shape && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 2;
+        Py_XDECREF(shape);
+        if (!shape) return false;
+        if (!several) {
+            holds(o, "positions", T, 4);
+            return true;
+        }
+        int64_t at[2] = {};
+        sizes(o, 2, at);
+        axes = at[0];
+        pos_stride = row_stride(o, "positions", T);
+        if (axes == 1 && pos_stride < T) pos_stride = T;  // (of one row it says nothing)
+        if (at[1] < T) refuse("positions has %lld columns, %lld needed", static_cast<long long>(at[1]), static_cast<long long>(T));
+        if (attribute(o, s_itemsize) != 4) refuse("positions: elements of 4 bytes expected");
+        return true;
+    }
+    // Codes and exponents of an 8-bit cache of the sizes pages, page size, heads, head dim.
+    void cache8(PyObject* k_codes, PyObject* v_codes, PyObject* k_exp, PyObject* v_exp, const int64_t (&c)[4]) {
+        const int64_t codes = c[0] * c[1] * c[2] * c[3], exps = c[0] * (c[1] / 16) * c[2];
+        holds(k_codes, "k_codes", codes, 1);
+        holds(v_codes, "v_codes", codes, 1);
+        holds(k_exp, "k_exp", exps, 1);
+        holds(v_exp, "v_exp", exps, 1);
+    }
 };
 
 bool enough(Py_ssize_t n, Py_ssize_t want) {
@@ -159,30 +190,14 @@ PyObject* slots(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!enough(n, 15)) return nullptr;
     Reader r;
-    int64_t cache[4] = {}, q[2] = {}, k[2] = {}, v[2] = {}, at[2] = {};
+    int64_t cache[4] = {}, q[2] = {}, k[2] = {}, v[2] = {};
     r.sizes(a[4], 4, cache);  // pages, page size, heads, head dim
     r.sizes(a[0], 2, q);
     r.sizes(a[1], 2, k);
     r.sizes(a[2], 2, v);
-    // positions: [tokens] or [axes][tokens]
     const int64_t T = q[0], kw = cache[2] * cache[3];
     int64_t axes = 1, pos_stride = T;
-    if (r.ok) {
-        PyObject* shape = PyObject_GetAttr(a[7], s_shape);
-        const bool several = shape && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 2;
-        Py_XDECREF(shape);
-        if (!shape) return nullptr;
-        if (several) {
-            r.sizes(a[7], 2, at);
-            axes = at[0];
-            pos_stride = r.row_stride(a[7], "positions", T);
-            if (axes == 1 && pos_stride < T) pos_stride = T;  // (of one row it says nothing)
-            if (at[1] < T) r.refuse("positions has %lld columns, %lld needed", static_cast<long long>(at[1]), static_cast<long long>(T));
-            if (r.attribute(a[7], s_itemsize) != 4) r.refuse("positions: elements of 4 bytes expected");
-        } else {
-            r.holds(a[7], "positions", T, 4);
-        }
-    }
+    if (!r.positions(a[7], T, axes, pos_stride)) return nullptr;
     void* p[10];
     for (int i = 0; i < 10; ++i) p[i] = r.address(a[i]);
     const int64_t qs = r.row_stride(a[0], "q", q[1]), ks = r.row_stride(a[1], "k", k[1]), vs = r.row_stride(a[2], "v", v[1]);
@@ -253,12 +268,128 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return PyLong_FromLong(st);
 }
 
+// The addresses of the 8-bit cache's entry points.
+PyObject* bind8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!enough(n, 3)) return nullptr;
+    Reader r;
+    f_store8 = reinterpret_cast<decltype(f_store8)>(r.address(a[0]));
+    f_read8 = reinterpret_cast<decltype(f_read8)>(r.address(a[1]));
+    f_attention8 = reinterpret_cast<decltype(f_attention8)>(r.address(a[2]));
+    if (!r.ok) return nullptr;
+    Py_RETURN_NONE;
+}
+
+// q, k, v, q_out, k_codes, v_codes, k_exp, v_exp, slots, positions, turns, q_gamma, k_gamma, axis_of_pair, eps, neighbours, factor,
+// stream
+PyObject* store8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!enough(n, 18)) return nullptr;
+    Reader r;
+    int64_t cache[4] = {}, q[2] = {}, k[2] = {}, v[2] = {}, pairs = 0;
+    r.sizes(a[4], 4, cache);
+    r.sizes(a[0], 2, q);
+    r.sizes(a[1], 2, k);
+    r.sizes(a[2], 2, v);
+    if (a[10] != Py_None) r.sizes(a[10], 1, &pairs);
+    const int64_t T = q[0], d = cache[3], kw = cache[2] * d;
+    int64_t axes = 1, pos_stride = T;
+    if (!r.positions(a[9], T, axes, pos_stride)) return nullptr;
+    void* p[14];
+    for (int i = 0; i < 14; ++i) p[i] = r.address(a[i]);
+    const int64_t qs = r.row_stride(a[0], "q", q[1]), ks = r.row_stride(a[1], "k", k[1]), vs = r.row_stride(a[2], "v", v[1]);
+    if (r.attribute(a[0], s_itemsize) != 2 || r.attribute(a[1], s_itemsize) != 2 || r.attribute(a[2], s_itemsize) != 2)
+        r.refuse("q, k, v: elements of 2 bytes expected");
+    if (d > 0 && q[1] % d != 0) r.refuse("q: rows of %lld elements are no whole heads of %lld", static_cast<long long>(q[1]), static_cast<long long>(d));
+    if (k[0] < T || k[1] < kw) r.refuse("k: fewer rows than q, or heads than the cache");
+    if (v[0] < T || v[1] < kw) r.refuse("v: fewer rows than q, or heads than the cache");
+    r.holds(a[3], "q_out", T * q[1], 2);
+    r.cache8(a[4], a[5], a[6], a[7], cache);
+    r.holds(a[8], "slots", T, 8);
+    r.holds(a[10], "turns", pairs, 8);
+    r.holds(a[11], "q_gamma", d, 4);
+    r.holds(a[12], "k_gamma", d, 4);
+    r.holds(a[13], "axis_of_pair", pairs, 1);
+    const float eps = float(r.real(a[14])), factor = float(r.real(a[16]));
+    const int64_t neighbours = r.integer(a[15]);
+    void* stream = r.address(a[17]);
+    if (!r.ok) return nullptr;
+    if (r.why[0]) return PyUnicode_FromString(r.why);
+    emb_status st;
+    Py_BEGIN_ALLOW_THREADS;
+    st = f_store8(static_cast<uint16_t*>(p[0]), qs, static_cast<uint16_t*>(p[1]), ks, static_cast<uint16_t*>(p[2]), vs, T,
+                  d > 0 ? q[1] / d : 0, cache[2], d, static_cast<float*>(p[11]), static_cast<float*>(p[12]), eps,
+                  static_cast<int32_t*>(p[9]), pos_stride, axes, static_cast<uint8_t*>(p[13]), static_cast<uint64_t*>(p[10]), 2 * pairs,
+                  neighbours == 0 ? 0 : 1, factor, static_cast<int64_t*>(p[8]), static_cast<uint16_t*>(p[3]), static_cast<uint8_t*>(p[4]),
+                  static_cast<uint8_t*>(p[5]), static_cast<uint8_t*>(p[6]), static_cast<uint8_t*>(p[7]), cache[0], cache[1],
+                  static_cast<emb_stream_t>(stream));
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(st);
+}
+
+// k_codes, v_codes, k_exp, v_exp, slots, k_out, v_out, stream
+PyObject* read8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!enough(n, 8)) return nullptr;
+    Reader r;
+    int64_t cache[4] = {}, rows = 0;
+    r.sizes(a[0], 4, cache);
+    r.sizes(a[4], 1, &rows);
+    void* p[7];
+    for (int i = 0; i < 7; ++i) p[i] = r.address(a[i]);
+    r.cache8(a[0], a[1], a[2], a[3], cache);
+    r.holds(a[4], "slots", rows, 8);
+    r.holds(a[5], "k_out", rows * cache[2] * cache[3], 2);
+    r.holds(a[6], "v_out", rows * cache[2] * cache[3], 2);
+    void* stream = r.address(a[7]);
+    if (!r.ok) return nullptr;
+    if (r.why[0]) return PyUnicode_FromString(r.why);
+    emb_status st;
+    Py_BEGIN_ALLOW_THREADS;
+    st = f_read8(static_cast<uint8_t*>(p[0]), static_cast<uint8_t*>(p[1]), static_cast<uint8_t*>(p[2]), static_cast<uint8_t*>(p[3]),
+                 cache[0], cache[1], cache[2], cache[3], static_cast<int64_t*>(p[4]), rows, static_cast<uint16_t*>(p[5]),
+                 static_cast<uint16_t*>(p[6]), static_cast<emb_stream_t>(stream));
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(st);
+}
+
+// Q, k_codes, v_codes, k_exp, v_exp, table, q_start, kv_len, O, workspace, prefix, scale, max_q, cap, window, ws_bytes, stream
+PyObject* attention8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!enough(n, 17)) return nullptr;
+    Reader r;
+    int64_t cache[4] = {}, q[2] = {}, table[2] = {};
+    r.sizes(a[1], 4, cache);
+    r.sizes(a[0], 2, q);
+    r.sizes(a[5], 2, table);
+    void* p[11];
+    for (int i = 0; i < 11; ++i) p[i] = r.address(a[i]);
+    const float scale = float(r.real(a[11])), cap = float(r.real(a[13]));
+    const int64_t max_q = r.integer(a[12]), window = r.integer(a[14]), bytes = r.integer(a[15]), d = cache[3];
+    void* stream = r.address(a[16]);
+    if (d > 0 && q[1] % d != 0) r.refuse("Q: rows of %lld elements are no whole heads of %lld", static_cast<long long>(q[1]), static_cast<long long>(d));
+    r.holds(a[0], "Q", q[0] * q[1], 2);
+    r.cache8(a[1], a[2], a[3], a[4], cache);
+    r.holds(a[5], "table", table[0] * table[1], 4);
+    r.holds(a[6], "q_start", table[0] + 1, 4);
+    r.holds(a[7], "kv_len", table[0], 4);
+    r.holds(a[8], "O", q[0] * q[1], 2);
+    r.holds(a[10], "prefix", table[0], 4);
+    if (!r.ok) return nullptr;
+    if (r.why[0]) return PyUnicode_FromString(r.why);
+    emb_status st;
+    Py_BEGIN_ALLOW_THREADS;
+    st = f_attention8(static_cast<uint16_t*>(p[0]), static_cast<uint8_t*>(p[1]), static_cast<uint8_t*>(p[2]), static_cast<uint8_t*>(p[3]),
+                      static_cast<uint8_t*>(p[4]), cache[0], cache[1], static_cast<int32_t*>(p[5]), table[1], static_cast<int32_t*>(p[6]),
+                      static_cast<int32_t*>(p[7]), static_cast<int32_t*>(p[10]), table[0], q[0], max_q, static_cast<uint16_t*>(p[8]),
+                      d > 0 ? q[1] / d : 0, cache[2], d, scale, cap, window, p[9], size_t(bytes), static_cast<emb_stream_t>(stream));
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(st);
+}
+
 using Fast = PyObject* (*)(PyObject*, PyObject* const*, Py_ssize_t);
 PyMethodDef method(const char* name, Fast f) {
     return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr};
 }
 PyMethodDef methods[] = {method("bind", bind), method("slots", slots), method("qk_norm_rope", qk_norm_rope),
-                         method("attention", attention), {nullptr, nullptr, 0, nullptr}};
+                         method("attention", attention), method("bind8", bind8), method("store8", store8),
+                         method("read8", read8), method("attention8", attention8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_paged_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -372,6 +372,8 @@ bool encode_cache(CUtensorMap* m, const void* base, const PagedAttnArgs& a, uint
 bool encode_queries(CUtensorMap* m, const PagedAttnArgs& a, uint32_t heads, uint32_t tokens);
 // Units of work of a call, at most: every block of every request over a full block table.
 double unit_bound(const PagedAttnArgs& a, int qb, int kt);
+// What the kernels are told of a call, but for the tensor maps, the work's split and the grid.
+PagedParams paged_params(const PagedAttnArgs& a);
 // What a launch of `grid` CTAs (two at least), of which joining an item costs join_units, tells its kernel.
 inline void set_grid(PagedParams& p, unsigned grid, unsigned join_units) {
     p.join_units = join_units;
