@@ -97,13 +97,14 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
 }
 
 // The power of two that a row of queries of largest magnitude `top` is multiplied by before it is rounded to f16 (its elements
-// then stay below 2^15, and those above 2^-28 of the largest are exact), and that power's inverse.
+// then stay below 2^15, and those above 2^-28 of the largest are exact), and that power's inverse. Of a row with an infinity
+// nothing is left but NaN, which its scores then are.
 struct RowPower {
     float to, back;
 };
 __device__ __forceinline__ RowPower row_power(float top) {
     const int e = max(int(__float_as_uint(top) >> 23) - 127, -100);  // floor(log2(top))
-    return top > 0.0f || top != top ? RowPower{pow2i(14 - e), pow2i(e - 14)} : RowPower{1.0f, 1.0f};
+    return RowPower{top == INFINITY ? NAN : pow2i(14 - e), pow2i(e - 14)};
 }
 // A block's factor of the raw products, held within fp32's range (a product of 0 stays 0 under the largest of them).
 __device__ __forceinline__ float score_factor(float x) { return fminf(fmaxf(x, -3.0e38f), 3.0e38f); }

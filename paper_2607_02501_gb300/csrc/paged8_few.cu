@@ -712,6 +712,14 @@ cudaError_t launch_paged8_attention(const Paged8AttnArgs& args, cudaStream_t s) 
     static_cast<PagedParams&>(p) = paged_params(a);
     p.k_exp = args.k_exp;
     p.v_exp = args.v_exp;
+    // (the bf16 cache's rule, see launch_paged_attention)
+    const bool few = p.G <= 16 && (a.max_q * p.G <= 16 || few8_cluster(a) > 0);
+    if (!few) {
+        p.negate = a.scale < 0.0f;
+        p.scale2 = std::max(std::fabs(p.scale2), 1e-37f);  // (hidden scores are the lowest there are times this)
+        p.lin2 = std::max(std::fabs(p.lin2), 1e-37f);
+        return launch_paged8_many(p, a, s);
+    }
     return launch_paged8_few(p, a, s);
 }
 

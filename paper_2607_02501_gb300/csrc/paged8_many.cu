@@ -1,0 +1,808 @@
+// Attention of new tokens over the 8-bit paged cache, many query rows per request: tcgen05 (definition in
+// include/emb_paged.h, work split in paged_sched.cuh).
+//
+// As the kernel for the bf16 cache (paged_many.cu): an item has two tiles of up to 128 rows (one with heads of 256), S = Q K^T
+// into tensor memory, a warpgroup of softmax per row tile with a thread a row, O += P V with P in the place of its
+// scores. What differs:
+// - Keys stay codes: they are the B operand of kind::f8f6f4 as TMA brings them. A row of queries, times a power of two, is
+//   split into two e4m3 numbers per element, the nearest and the rest, by its softmax thread and in place when the tile has arrived:
+//   8 bits of significand together, as bf16 has, so the split is exact but for elements below 2^-9 of the row's largest
+//   (within 2^-17 of it). Two products at twice the f16 rate cost what one would, the keys need no conversion, and shared
+//   memory, whose bandwidth f16 operands of this shape use up, has less to move.
+// - Values become f16 tiles in shared memory by two warps of their own. Weights are f16 (as e4m3, also in two parts, tails of
+//   many small ones would be lost).
+// - The blocks' powers: a row's scores of a block are multiplied by its key power, the running maximum is that of score plus value
+//   exponent, and the sum of weights takes the value power out again (see paged8_few.cu). Weights are times 2^6, and
+//   the maximum may lag by 2^8: below f16's largest.
+#include <algorithm>
+#include <mutex>
+
+#include "paged8.cuh"
+
+namespace emb {
+namespace {
+
+template <int D>
+struct Many8Traits {
+    static constexpr int NQ = D == 256 ? 1 : 2;        // row tiles of an item
+    static constexpr int KT = D == 256 ? 64 : 128;     // keys of a tile
+    static constexpr int NB = KT / kBlock8;            // blocks of a tile
+    static constexpr int kSoftWarps = 4 * NQ;
+    // then the MMA and the producer warp and two that convert values; with two row tiles these hand registers to the
+    // softmax, a thread of which holds 128 scores: 384 threads x 168 at launch, then 2 x 128 x 216 + 128 x 72
+    static constexpr int kThreads = 32 * (kSoftWarps + 4);
+    static constexpr int kQTile = 128 * D * 2;         // bytes of a row tile's queries
+    static constexpr int kRaw = KT * D;                // bytes of a tile of codes
+    static constexpr int kConv = KT * D * 2;           // bytes of a tile of f16 values
+    static constexpr int kKeys = D == 64 ? 6 : 3, kVals = D == 64 ? 6 : 3, kConvs = D == 64 ? 4 : 2;  // ring places
+    static constexpr int kSmem = 1024 + NQ * kQTile + (kKeys + kVals) * kRaw + kConvs * kConv;
+    static constexpr int W = D < 128 ? D : 128;        // bytes of a row of a code tile's part
+    static constexpr int kSub = KT * 128;              // bytes of 64 dims of an f16 tile, and of 128 of a code tile
+    // columns of tensor memory: scores (two places), outputs
+    static constexpr int kO = 2 * KT;
+    // Byte offset of 16-byte chunk c of row r in a code tile as TMA swizzles it.
+    static __device__ __forceinline__ uint32_t place(int r, int c) {
+        if constexpr (D == 64) return uint32_t(r * 64 + ((c ^ (r >> 1 & 3)) << 4));
+        return uint32_t((c >> 3) * kSub + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+    }
+};
+constexpr uint32_t kTmemAll = 512;
+static_assert(Many8Traits<64>::kSmem > 114 * 1024 && Many8Traits<128>::kSmem > 114 * 1024 && Many8Traits<256>::kSmem > 114 * 1024,
+              "one CTA per SM: tensor memory is allocated whole (see ptx::tmem_alloc)");
+// Tiles whose exponents are held: the producer is at most five ahead of the softmax, as keys' places are handed back behind the
+// products of a tile, and those wait for the softmax of the tile before it.
+constexpr int kScaleTiles = 8;
+constexpr float kLift = 6.0f;          // log2 of what weights are multiplied by
+constexpr float kMostLag = 8.0f;       // of the running maximum
+// Above this a maximum's rounding is felt in f16's range: the weights' exponents are then held to kLift + kMostLag one by one.
+constexpr float kLargeScore = 524288.0f;
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// A place of a ring and the parity of the turn it is in, carried along.
+template <int S>
+struct RingPlace {
+    int slot = 0;
+    uint32_t turn = 0;
+    __device__ __forceinline__ void next() {
+        if (++slot == S) {
+            slot = 0;
+            turn ^= 1u;
+        }
+    }
+};
+
+// The part of an item that lies in this CTA's stretch: tiles [j0, j1), of which row tile t has [a[t], b[t]).
+template <int D>
+struct Segment {
+    PagedItem it;
+    uint32_t take;
+    int j0, j1;
+    int a[2], b[2], nq[2];
+};
+template <int D>
+__device__ __forceinline__ Segment<D> segment_of(const PagedParams& p, int r, int g, int b, uint32_t off, uint32_t x, uint32_t x1) {
+    using T = Many8Traits<D>;
+    Segment<D> s;
+    s.it = paged_item<T::KT>(p, r, g, b);
+    s.take = min(x1 - x, uint32_t(s.it.units) - off);
+    s.j0 = s.it.t0 + int(off);
+    s.j1 = s.it.t0 + min(int(off + s.take), s.it.nt);
+    const int qt = p.QT;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        s.nq[t] = t < T::NQ ? max(0, min(qt, s.it.nq - t * qt)) : 0;
+        s.a[t] = s.b[t] = 0;
+        if (s.nq[t] == 0) continue;
+        const int i0 = s.it.i0 + t * qt;
+        const KeyRange first = query_keys(p, s.it.q, i0), last = query_keys(p, s.it.q, i0 + s.nq[t] - 1);
+        if (last.hi <= first.lo) continue;
+        s.a[t] = max(s.j0, first.lo / T::KT);
+        s.b[t] = min(s.j1, (last.hi + T::KT - 1) / T::KT);
+        if (s.b[t] < s.a[t]) s.b[t] = s.a[t];
+    }
+    return s;
+}
+
+// Row `row` of a tile of bf16 queries (rows of 64 dims, 128 bytes, swizzled), split in place: the nearest codes of 64-dim parts 0 ..
+// D / 128 - 1 in those, the rests' behind them (D = 64: both in the one row). Returns the power that takes the scores back.
+template <int D>
+__device__ __forceinline__ float split_row(uint8_t* tile, int row, bool negate) {
+    constexpr int C = D / 8;  // 16-byte chunks of the row
+    auto chunk = [&](int c) { return reinterpret_cast<uint4*>(tile + (c >> 3) * 16384 + row * 128 + (((c & 7) ^ (row & 7)) << 4)); };
+    float top = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const uint4 w = *chunk(c);
+        const uint32_t h[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 u = unpack_bf16x2(h[e]);
+            top = max3(top, fabsf(u.x), fabsf(u.y));
+        }
+    }
+    const RowPower pr = row_power(top);
+    const float by = pr.to * (negate ? -0.0078125f : 0.0078125f);  // below 2^8
+    // (the nearest codes take the place of what has been read, the rests wait until all has been)
+    uint4 rest[C / 2];
+#pragma unroll
+    for (int c = 0; c < C; c += 2) {
+        const uint4 w0 = *chunk(c), w1 = *chunk(c + 1);
+        const uint32_t h[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float2 x = unpack_bf16x2(h[2 * q]), y = unpack_bf16x2(h[2 * q + 1]);
+            const float f[4] = {x.x * by, x.y * by, y.x * by, y.y * by};
+            hi[q] = codes_of(f[0], f[1]) | codes_of(f[2], f[3]) << 16;
+            uint32_t h0, h1;
+            codes_to_f16x4(hi[q], h0, h1);
+            const float2 g0 = __half22float2(*reinterpret_cast<__half2*>(&h0)), g1 = __half22float2(*reinterpret_cast<__half2*>(&h1));
+            lo[q] = codes_of(f[0] - g0.x, f[1] - g0.y) | codes_of(f[2] - g1.x, f[3] - g1.y) << 16;
+        }
+        *chunk(c / 2) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        rest[c / 2] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+#pragma unroll
+    for (int c = 0; c < C / 2; ++c) *chunk(C / 2 + c) = rest[c];
+    return pr.back * 128.0f;
+}
+
+template <int D, int CAP>
+__global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kernel(const __grid_constant__ Paged8Params p) {
+    using T = Many8Traits<D>;
+    constexpr int NQ = T::NQ, KT = T::KT, NB = T::NB;
+    constexpr int kRows = 128 * NQ;
+    using PL = PartLayout<D, kRows>;
+    // what stands for the score of a key that a row does not see (a cap would make -infinity finite)
+    constexpr float kHidden = CAP ? -3.402823466e38f : -INFINITY;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t k_full[T::kKeys], k_empty[T::kKeys], raw_full[T::kVals], raw_empty[T::kVals], v_full[T::kConvs], v_empty[T::kConvs];
+    __shared__ uint64_t q_full, q_ready, q_empty, scale_full[kScaleTiles], s_full[2], p_ready[2], o_done[2], o_free[2], drain;
+    __shared__ float4 scales[kScaleTiles][NB];  // of a block: 2^e of its keys; e and 2^-e of its values
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag, joined, odd_seen;
+    __shared__ PagedJoin cut[2];
+    uint8_t* sq = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* kring = sq + NQ * T::kQTile;
+    uint8_t* vring = kring + T::kKeys * T::kRaw;
+    uint8_t* conv = vring + T::kVals * T::kRaw;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned all = 0xffffffffu;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < T::kKeys; ++i) {
+            ptx::mbar_init(&k_full[i], 1);
+            ptx::mbar_init(&k_empty[i], 1);
+        }
+        for (int i = 0; i < T::kVals; ++i) {
+            ptx::mbar_init(&raw_full[i], 1);
+            ptx::mbar_init(&raw_empty[i], 2);
+        }
+        for (int i = 0; i < T::kConvs; ++i) {
+            ptx::mbar_init(&v_full[i], 2);
+            ptx::mbar_init(&v_empty[i], 1);
+        }
+        for (int i = 0; i < kScaleTiles; ++i) ptx::mbar_init(&scale_full[i], 1);
+        ptx::mbar_init(&q_full, 1);
+        ptx::mbar_init(&q_ready, T::kSoftWarps);
+        ptx::mbar_init(&q_empty, 1);
+        for (int t = 0; t < 2; ++t) {
+            ptx::mbar_init(&s_full[t], 1);
+            ptx::mbar_init(&p_ready[t], 4);
+            ptx::mbar_init(&o_done[t], 1);
+            ptx::mbar_init(&o_free[t], 4);
+        }
+        ptx::mbar_init(&drain, 1);
+        abort_flag = 0;
+        odd_seen = 0;
+        ptx::fence_mbar_init();
+        ptx::prefetch_tmap(&p.q_map);
+        ptx::prefetch_tmap(&p.k_map);
+        ptx::prefetch_tmap(&p.v_map);
+    }
+    if (warp == T::kSoftWarps) {
+        ptx::tmem_alloc(&tmem_slot, kTmemAll);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = ptx::warp_uniform(tmem_slot);
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();  // lengths, queries and the new tokens' keys and values come from earlier launches
+    const PagedStretch st = paged_stretch<KT, T::kThreads>(p);
+
+    int r = st.r, g = st.g, b = st.b;
+    uint32_t x = st.x0, off = st.off;
+    auto wait = [&](uint64_t* bar, uint32_t phase) {
+        return __all_sync(all, ptx::mbar_wait(bar, phase & 1, &abort_flag, p.status, kWaitLimitNs)) != 0;
+    };
+    // (the tiles of the stretch are numbered through, over all its items)
+
+    if (warp == T::kSoftWarps + 1) {
+        // ---------------------------------------------------------------------- producer
+        if constexpr (NQ == 2) ptx::regs_down<72>();
+        ptx::fence_proxy_async_global();  // (the cache and the queries were written by ordinary stores)
+        const int page_size = 1 << p.page_shift, box = min(page_size, KT), n_box = KT / box;
+        const int qt = p.QT;
+        uint32_t keys = 0, values = 0, items = 0;  // tiles of codes and items with queries issued
+        RingPlace<T::kKeys> ka;
+        RingPlace<T::kVals> va;
+        bool ok = true;
+        while (x < st.x1 && ok) {
+            const Segment<D> sg = segment_of<D>(p, r, g, b, off, x, st.x1);
+            const PagedItem& it = sg.it;
+            if (sg.j1 > sg.j0) {
+                if (items > 0) ok = wait(&q_empty, items - 1);
+                if (!ok) break;
+                const int tiles_q = sg.nq[1] > 0 ? 2 : 1;
+                if (ptx::elect_one()) {
+                    ptx::mbar_arrive_expect_tx(&q_full, uint32_t(tiles_q * (D / 64) * qt * p.G * 128));
+                    for (int t = 0; t < tiles_q; ++t)
+#pragma unroll
+                        for (int c = 0; c < D / 64; ++c)
+                            ptx::tma_load_3d(sq + t * T::kQTile + c * 16384, &p.q_map, &q_full, c * 64, g * p.G, it.q.q0 + it.i0 + t * qt);
+                }
+                __syncwarp();
+                ++items;
+            }
+            const int32_t* row = p.table + int64_t(r) * p.max_pages;
+            // Lane i looks up the page of the tile's block i % NB; boxes that no query sees, and pages that do not exist, are
+            // fetched from behind the cache: zeros.
+            auto page_of = [&](int j) {
+                const int key = j * KT + (lane & (NB - 1)) * kBlock8, key_box = key & ~(box - 1);
+                int page = p.n_pages;
+                if (lane < 2 * NB && j < sg.j1 && key_box < it.hi && key_box + box > it.lo) {
+                    page = row[key >> p.page_shift];
+                    if (page < 0 || page > p.n_pages) page = p.n_pages;
+                }
+                return page;
+            };
+            // and the lanes below NB the exponent of its keys, the next NB that of its values
+            auto exp_of = [&](int j, int page) {
+                const int key = j * KT + (lane & (NB - 1)) * kBlock8;
+                const int64_t at = ((int64_t(page) << p.page_shift) + (key & (page_size - 1))) / kBlock8 * p.Hk + g;
+                uint32_t e = kExpBias;
+                if (page < p.n_pages) e = (lane < NB ? p.k_exp : p.v_exp)[at];
+                return e;
+            };
+            int page = page_of(sg.j0), page1 = page_of(sg.j0 + 1);
+            uint32_t ex = exp_of(sg.j0, page);
+            for (int j = sg.j0; j < sg.j1 && ok; ++j) {
+                const int page2 = page_of(j + 2);
+                const uint32_t ex1 = exp_of(j + 1, page1);
+                const int place = (j * KT) & (page_size - 1);
+                auto fetch = [&](uint8_t* to, const CUtensorMap* map, uint64_t* bar) {
+                    if (ptx::elect_one()) ptx::mbar_arrive_expect_tx(bar, T::kRaw);
+                    __syncwarp();
+                    for (int i = 0; i < n_box; ++i) {
+                        const int pg = __shfl_sync(all, page, i * (box / kBlock8));
+                        if (ptx::elect_one()) {
+#pragma unroll
+                            for (int c = 0; c < D / T::W; ++c)
+                                ptx::tma_load_4d(to + c * T::kSub + i * box * T::W, map, bar, c * T::W, g, place, pg);
+                        }
+                        __syncwarp();
+                    }
+                };
+                if (keys >= uint32_t(T::kKeys)) ok = wait(&k_empty[ka.slot], ka.turn ^ 1u);
+                if (!ok) break;
+                const int e = exp_of_byte(ex), s = int(keys % kScaleTiles);
+                if (lane < NB) {
+                    scales[s][lane].x = pow2i(e);
+                } else if (lane < 2 * NB) {
+                    scales[s][lane - NB].y = float(e);
+                    scales[s][lane - NB].z = pow2i(-e);
+                }
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&scale_full[s]);
+                fetch(kring + ka.slot * T::kRaw, &p.k_map, &k_full[ka.slot]);
+                ++keys;
+                ka.next();
+                if (values >= uint32_t(T::kVals)) ok = wait(&raw_empty[va.slot], va.turn ^ 1u);
+                if (!ok) break;
+                fetch(vring + va.slot * T::kRaw, &p.v_map, &raw_full[va.slot]);
+                ++values;
+                va.next();
+                page = page1;
+                page1 = page2;
+                ex = ex1;
+            }
+            x += sg.take;
+            off = 0;
+            if (x < st.x1) next_item(p, r, g, b, it.q.n);
+        }
+        // every copy must land before this CTA's shared memory is released
+        for (uint32_t i = keys > uint32_t(T::kKeys) ? keys - T::kKeys : 0; i < keys; ++i)
+            ptx::mbar_wait(&k_full[i % T::kKeys], (i / T::kKeys) & 1, nullptr, p.status, kWaitLimitNs);
+        for (uint32_t i = values > uint32_t(T::kVals) ? values - T::kVals : 0; i < values; ++i)
+            ptx::mbar_wait(&raw_full[i % T::kVals], (i / T::kVals) & 1, nullptr, p.status, kWaitLimitNs);
+        if (items > 0) ptx::mbar_wait(&q_full, (items - 1) & 1, nullptr, p.status, kWaitLimitNs);
+    } else if (warp == T::kSoftWarps) {
+        // ------------------------------------------------------------------------- MMAs
+        if constexpr (NQ == 2) ptx::regs_down<72>();
+        constexpr uint32_t idesc_qk = ptx::idesc_e4m3_f32(128, KT), idesc_pv = ptx::idesc_f16_f32(128, D) | ptx::kIdescMnMajorB;
+        const uint32_t sq_u = ptx::smem_u32(sq), kring_u = ptx::smem_u32(kring), conv_u = ptx::smem_u32(conv);
+        uint32_t n = 0, items = 0;
+        RingPlace<T::kKeys> keys;     // of tile j
+        RingPlace<T::kConvs> values;  // of the tile before it
+        uint32_t scores[2] = {0, 0}, owned[2] = {0, 0};  // score tiles by place, items with outputs by row tile
+        bool ok = true;
+        // (operands in a form that the compiler knows to be uniform: see ptx::elect_one)
+        auto qk = [&](int t, int place, int slot) {  // S[place] = Q[t] K^T, nearest codes and rests
+            const uint32_t k = ptx::warp_uniform(kring_u + uint32_t(slot * T::kRaw)), q = sq_u + uint32_t(t * T::kQTile);
+            const uint32_t d = ptx::warp_uniform(tmem + uint32_t(place * KT));
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+                for (int ks = 0; ks < D / 32; ++ks) {
+                    uint64_t da, db;
+                    if constexpr (D == 64) {
+                        da = ptx::smem_desc_sw128(q) + 4 * part + 2 * ks;
+                        db = ptx::smem_desc_sw64(k) + 2 * ks;
+                    } else {
+                        da = ptx::smem_desc_sw128(q + (part * (D / 128) + ks / 4) * 16384) + 2 * (ks & 3);
+                        db = ptx::smem_desc_sw128(k + (ks / 4) * T::kSub) + 2 * (ks & 3);
+                    }
+                    ptx::mma_f8_ss(d, da, db, idesc_qk, part + ks != 0);
+                }
+            ptx::mma_commit(&s_full[place]);
+        };
+        auto pv = [&](int t, int place, int slot, bool first) {  // O[t] (+)= P[place] V
+            const uint64_t desc = ptx::smem_desc_mn_sw128(ptx::warp_uniform(conv_u + uint32_t(slot * T::kConv)), T::kSub);
+            const uint32_t d = ptx::warp_uniform(tmem + uint32_t(T::kO + t * D)), a = ptx::warp_uniform(tmem + uint32_t(place * KT));
+            const uint32_t more = ptx::warp_uniform(first ? 0u : 1u);
+#pragma unroll
+            for (int kk = 0; kk < KT / 16; ++kk)
+                ptx::mma_f16_ta(d, a + uint32_t(8 * kk), desc + uint32_t(kk * 2048 / 16), idesc_pv, kk == 0 ? more : 1u);
+            ptx::mma_commit(&o_done[t]);
+        };
+        while (x < st.x1 && ok) {
+            const Segment<D> sg = segment_of<D>(p, r, g, b, off, x, st.x1);
+            if (sg.j1 > sg.j0) {
+                ok = wait(&q_ready, items++);
+                for (int j = sg.j0; j <= sg.j1 && ok; ++j) {
+                    if (j < sg.j1) ok = wait(&k_full[keys.slot], keys.turn);
+                    if (!ok) break;
+                    ptx::tc_fence_after();
+                    auto finish = [&](int t, int place) {  // P V of tile j - 1
+                        const bool first = j - 1 == sg.a[t];
+                        ok = wait(&v_full[values.slot], values.turn) && wait(&p_ready[place], scores[place] - 1);
+                        if (ok && first && owned[t] > 0) ok = wait(&o_free[t], owned[t] - 1);
+                        if (!ok) return;
+                        ptx::tc_fence_after();
+                        pv(t, place, values.slot, first);
+                        if (first) ++owned[t];
+                    };
+                    if constexpr (NQ == 2) {
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            if (j > sg.a[t] && j <= sg.b[t]) finish(t, t);
+                            if (!ok) break;
+                            if (j >= sg.a[t] && j < sg.b[t]) {
+                                qk(t, t, keys.slot);
+                                ++scores[t];
+                            }
+                        }
+                    } else {
+                        if (j < sg.j1) {
+                            qk(0, int(n & 1), keys.slot);
+                            ++scores[n & 1];
+                        }
+                        if (j > sg.j0) finish(0, int((n - 1) & 1));
+                    }
+                    if (!ok) break;
+                    if (j > sg.j0) {
+                        // (a tile that no row tile needed is handed back no sooner than it has arrived)
+                        ok = wait(&v_full[values.slot], values.turn);
+                        if (!ok) break;
+                        ptx::mma_commit(&v_empty[values.slot]);
+                        values.next();
+                    }
+                    if (j < sg.j1) {
+                        ptx::mma_commit(&k_empty[keys.slot]);
+                        ++n;
+                        keys.next();
+                        if (j == sg.j1 - 1) ptx::mma_commit(&q_empty);
+                    }
+                }
+            }
+            x += sg.take;
+            off = 0;
+            if (x < st.x1) next_item(p, r, g, b, sg.it.q.n);
+        }
+        // whatever was issued finishes before tensor memory is freed
+        ptx::mma_commit(&drain);
+        ptx::mbar_wait(&drain, 0, nullptr, p.status, kWaitLimitNs);
+    } else if (warp >= T::kSoftWarps) {
+        // ------------------------------------------------------ values to f16, half a tile a warp
+        if constexpr (NQ == 2) ptx::regs_down<72>();
+        uint32_t n = 0;
+        RingPlace<T::kVals> from;
+        RingPlace<T::kConvs> to;
+        bool ok = true;
+        while (x < st.x1 && ok) {
+            const Segment<D> sg = segment_of<D>(p, r, g, b, off, x, st.x1);
+            const PagedItem& it = sg.it;
+            for (int j = sg.j0; j < sg.j1 && ok; ++j, ++n) {
+                const int key0 = j * KT;
+                // Values behind the request's last key are anything: zeros. NaN codes hidden from some rows may not be
+                // multiplied by their weights of 0: they leave the tile here and are added at the item's end for the rows that
+                // see them.
+                const bool tail = key0 + KT > it.q.L, hidden = key0 < it.lo_all || min(key0 + KT, it.q.L) > it.hi_all;
+                ok = wait(&raw_full[from.slot], from.turn);
+                if (ok && n >= uint32_t(T::kConvs)) ok = wait(&v_empty[to.slot], to.turn ^ 1u);
+                if (!ok) break;
+                const uint8_t* in = vring + from.slot * T::kRaw;
+                uint8_t* out = conv + to.slot * T::kConv;
+                uint32_t odd = 0;
+                // 16 codes of a key at a time; eight lanes have neighbouring keys, which meet in no bank
+                constexpr int kChunks = D / 16, kEach = KT * kChunks / 64;
+#pragma unroll 8
+                for (int i = 0; i < kEach; ++i) {
+                    const int e = (i * 2 + (warp & 1)) * 32 + lane, key = (e & 7) | (e / 8 / kChunks) << 3, c = e / 8 % kChunks;
+                    uint4 w = *reinterpret_cast<const uint4*>(in + T::place(key, c));
+                    if (tail && key0 + key >= it.q.L) w = make_uint4(0, 0, 0, 0);
+                    if (hidden) {
+                        const uint32_t bx = nan_codes(w.x), by = nan_codes(w.y), bz = nan_codes(w.z), bw = nan_codes(w.w);
+                        odd |= bx | by | bz | bw;
+                        w = make_uint4(without(w.x, bx), without(w.y, by), without(w.z, bz), without(w.w, bw));
+                    }
+                    uint4 a, d;
+                    codes_to_f16x4(w.x, a.x, a.y);
+                    codes_to_f16x4(w.y, a.z, a.w);
+                    codes_to_f16x4(w.z, d.x, d.y);
+                    codes_to_f16x4(w.w, d.z, d.w);
+                    uint8_t* row = out + (c >> 2) * T::kSub + key * 128;
+                    const int k2 = (c & 3) * 2;
+                    *reinterpret_cast<uint4*>(row + ((k2 ^ (key & 7)) << 4)) = a;
+                    *reinterpret_cast<uint4*>(row + (((k2 + 1) ^ (key & 7)) << 4)) = d;
+                }
+                // (never taken back: the softmax may be some items behind. Items without such codes are then searched for nothing)
+                if (odd) *reinterpret_cast<volatile int*>(&odd_seen) = 1;
+                ptx::fence_proxy_async_smem();
+                __threadfence_block();
+                __syncwarp();
+                if (lane == 0) {
+                    ptx::mbar_arrive(&v_full[to.slot]);
+                    ptx::mbar_arrive(&raw_empty[from.slot]);
+                }
+                from.next();
+                to.next();
+            }
+            x += sg.take;
+            off = 0;
+            if (x < st.x1) next_item(p, r, g, b, it.q.n);
+        }
+    } else {
+        // ---------------------------------------------------------------------- softmax
+        if constexpr (NQ == 2) ptx::regs_up<216>();
+        zero_padding(p, D, threadIdx.x, 32 * T::kSoftWarps);
+        const int t = warp >> 2;  // row tile
+        const int row = 32 * (warp & 3) + lane, qt = p.QT, i = row / p.G;
+        const uint32_t lanes = uint32_t(32 * (warp & 3)) << 16;
+        const uint32_t o_col = tmem + lanes + uint32_t(T::kO + t * D);
+        uint32_t n = 0, seen[2] = {0, 0}, outs = 0, items = 0;
+        int joins = 0;
+        auto soft_bar = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * T::kSoftWarps) : "memory"); };
+        // A wait that gave up sets abort_flag; later waits then return at once, and the loops run to their end (the
+        // outputs are undefined then), so that every barrier still meets all its threads.
+        while (x < st.x1) {
+            const Segment<D> sg = segment_of<D>(p, r, g, b, off, x, st.x1);
+            const PagedItem& it = sg.it;
+            const bool live = i < (t ? sg.nq[1] : sg.nq[0]);
+            const KeyRange keys = live ? query_keys(p, it.q, it.i0 + t * qt + i) : KeyRange{0, 0};
+            // (selected, not indexed: t is a run-time value)
+            const int a_t = t ? sg.a[1] : sg.a[0], b_t = t ? sg.b[1] : sg.b[0];
+            float back = 1.0f;
+            if (sg.j1 > sg.j0) {
+                wait(&q_full, items++);
+                if (live) back = split_row<D>(sq + t * T::kQTile, row, p.negate);
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&q_ready);
+            }
+            if constexpr (!CAP) back *= p.scale2;
+            // whether the row has seen a score, its running maximum of score plus value exponent in base 2 (negated, so that it is
+            // added), sums of weights without the values' powers. A cap makes a score of -infinity one of -cap, which counts.
+            bool any = false;
+            float mc = 0.0f;
+            float2 l2 = make_float2(0, 0);
+            for (int j = sg.j0; j < sg.j1; ++j, ++n) {
+                if (j < a_t || j >= b_t) continue;
+                const int place = NQ == 2 ? t : int(n & 1);
+                const float4* block = scales[n % kScaleTiles];
+                wait(&s_full[place], seen[place]++);
+                wait(&scale_full[n % kScaleTiles], n / kScaleTiles);  // (behind the scores: of this turn, as tiles may be skipped)
+                ptx::tc_fence_after();
+                const uint32_t s_col = tmem + lanes + uint32_t(place * KT);
+                const int key0 = j * KT;
+                const bool edge = key0 < it.lo_all || key0 + KT > it.hi_all;
+                const int lo = keys.lo - key0, hi = keys.hi - key0;
+                // Votes are taken among rows that see a key of the tile. A tile's other rows are not of this request, or not
+                // even filled (3 heads: 126 of 128 rows), and what they hold may not decide how a warp computes.
+                const bool sees = max(lo, 0) < min(hi, KT);
+                // the factor of a block's raw scores (times what is hidden it stays hidden)
+                auto factor = [&](int k) { return fminf(fmaxf(back * block[k].x, 1e-37f), 3e38f); };
+                float far = 0.0f;  // for a cap: the largest magnitude of q.k that the row sees
+                if (edge) {
+                    // scores that the row does not see, in tensor memory: rolled up and away from the path of most tiles
+#pragma unroll 1
+                    for (int c = 0; c < KT; c += 32) {
+                        float v[32];
+                        uint32_t w[32];
+                        ptx::tmem_ld_32(s_col + c, v);
+                        ptx::tmem_ld_wait_32(v);
+                        const float f[2] = {CAP ? factor(c / 16) : 0.0f, CAP ? factor(c / 16 + 1) : 0.0f};
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const bool in = c + e >= lo && c + e < hi;
+                            if (CAP && in) far = fmaxf(far, fabsf(v[e] * f[e / 16]));
+                            w[e] = __float_as_uint(in ? v[e] : kHidden);
+                        }
+                        ptx::tmem_st_32(s_col + c, w);
+                    }
+                    ptx::tmem_st_wait();
+                }
+                float s[KT];
+#pragma unroll
+                for (int c = 0; c < KT; c += 32) ptx::tmem_ld_32(s_col + c, s + c);
+                float zt = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < KT; c += 32) {
+                    ptx::tmem_ld_wait_32(s + c);
+#pragma unroll
+                    for (int h = 0; h < 32; h += 16) {
+                        float top[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) top[k] = max3(max3(-INFINITY, s[c + h + k], s[c + h + 4 + k]), s[c + h + 8 + k], s[c + h + 12 + k]);
+                        const float mt = fmaxf(max3(top[0], top[1], top[2]), top[3]);
+                        const float4 bl = block[(c + h) / 16];
+                        const float f = fminf(fmaxf(back * bl.x, 1e-37f), 3e38f);
+                        if constexpr (CAP) {
+                            if (!edge) {
+                                float least = s[c + h];
+#pragma unroll
+                                for (int e = 1; e < 16; ++e) least = fminf(least, s[c + h + e]);
+                                far = max3(far, fabsf(mt * f), fabsf(least * f));
+                            }
+                            const float z = capped2<CAP>(make_float2(mt * f, mt * f), p).x + bl.y;
+                            zt = mt == kHidden ? zt : fmaxf(zt, z);
+                        } else {
+                            zt = fmaxf(zt, fmaf(mt, f, bl.y));
+                        }
+                    }
+                }
+                const bool grow = sees && (any ? zt + mc > kMostLag : CAP || zt > -INFINITY);
+                if (__any_sync(all, grow)) {
+                    const float f = !grow ? 1.0f : any ? exp2_fast(-mc - zt) : 0.0f;
+                    if (j > a_t) {
+                        wait(&o_done[t], outs - 1);  // every product issued so far is in
+                        ptx::tc_fence_after();
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 32) {
+                            float o[32];
+                            uint32_t w[32];
+                            ptx::tmem_ld_32(o_col + c, o);
+                            ptx::tmem_ld_wait_32(o);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(o[e] * f);
+                            ptx::tmem_st_32(o_col + c, w);
+                        }
+                    }
+                    if (grow) {
+                        l2.x *= f;
+                        l2.y *= f;
+                        any = true;
+                        mc = -zt;
+                    }
+                }
+                // The weights, two blocks at a time, over the scores. base(u, f, m) gives two scores in base 2 plus m, the block's value
+                // exponent less the row's maximum.
+                auto weights = [&](auto base) {
+#pragma unroll
+                    for (int c = 0; c < KT; c += 32) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int h = 0; h < 32; h += 16) {
+                            const float4 bl = block[(c + h) / 16];
+                            const float f = fminf(fmaxf(back * bl.x, 1e-37f), 3e38f), m = (bl.y + mc) + kLift;
+                            float2 sum = make_float2(0, 0);
+#pragma unroll
+                            for (int e = 0; e < 16; e += 2) {
+                                float2 u = base(make_float2(s[c + h + e], s[c + h + e + 1]), make_float2(f, f), make_float2(m, m));
+                                u.x = exp2_fast(u.x);
+                                u.y = exp2_fast(u.y);
+                                sum = add2(sum, u);
+                                w[(h + e) / 2] = pack_f16x2(u.x, u.y);
+                            }
+                            l2 = fma2(sum, make_float2(bl.z, bl.z), l2);
+                        }
+                        ptx::tmem_st_16(s_col + c / 2, w);
+                    }
+                };
+                const bool large = __any_sync(all, sees && fabsf(mc) > kLargeScore);
+                auto held = [](float2 u) { return make_float2(fminf(u.x, kLift + kMostLag), fminf(u.y, kLift + kMostLag)); };
+                if constexpr (!CAP) {
+                    if (!large) weights([&](float2 u, float2 f, float2 m) { return fma2(u, f, m); });
+                    // (NaN stays NaN: the minimum would hide it)
+                    else weights([&](float2 u, float2 f, float2 m) {
+                        const float2 z = fma2(u, f, m), h = held(z);
+                        return make_float2(z.x != z.x ? z.x : h.x, z.y != z.y ? z.y : h.y);
+                    });
+                } else {
+                    const bool near = !large && __all_sync(all, !sees || far * p.scale2 < kNearCap);
+                    auto shown = [](float2 u, float2 z) {
+                        return make_float2(u.x == kHidden ? -INFINITY : z.x, u.y == kHidden ? -INFINITY : z.y);
+                    };
+                    // far below the cap one power of two per score, where exponential and reciprocal take two more turns of
+                    // the same unit
+                    if (near && !edge) weights([&](float2 u, float2 f, float2 m) { return capped_near2(mul2(u, f), p, m); });
+                    else if (near) weights([&](float2 u, float2 f, float2 m) { return shown(u, capped_near2(mul2(u, f), p, m)); });
+                    else weights([&](float2 u, float2 f, float2 m) {
+                        const float2 z = add2(capped2<CAP>(mul2(u, f), p), m), h = held(z);
+                        return shown(u, make_float2(z.x != z.x ? z.x : h.x, z.y != z.y ? z.y : h.y));
+                    });
+                }
+                // every phase of o_done is waited for, so that a wait cannot take the one before the last for the last:
+                // with two score places the last scores do not tell that the product before theirs is in
+                if (NQ == 1 && j > a_t) wait(&o_done[t], outs - 1);
+                ptx::tmem_st_wait();
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&p_ready[place]);
+                ++outs;
+            }
+            // the segment's result: outputs, or this CTA's part of them
+            const bool has = b_t > a_t;
+            const float l = l2.x + l2.y;
+            if (has) {
+                wait(&o_done[t], outs - 1);
+                ptx::tc_fence_after();
+            }
+            const bool whole = off == 0 && sg.take == uint32_t(it.units);
+            const uint32_t a = x - off;  // the item's first unit
+            PagedJoin J{r, g, b, int(a / st.chunk), 0};
+            J.count = int((a + uint32_t(it.units) - 1) / st.chunk) - J.first + 1;
+            float* part = p.part + part_slot(int(blockIdx.x), J.first) * PL::kFloats;
+            const int prow = t * qt * p.G + row;  // rows of both tiles in order
+            __nv_bfloat16* out = p.O + (int64_t(it.q.q0 + it.i0 + t * qt + i) * p.H + g * p.G + (row - i * p.G)) * D;
+            const float inv = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
+            const bool odd = has && *reinterpret_cast<volatile int*>(&odd_seen) != 0;
+            if (!whole && live) {
+                part[prow] = any ? -mc : -INFINITY;
+                part[kRows + prow] = l;
+            }
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+                float o[32];
+                __syncwarp();
+                if (has) {
+                    ptx::tmem_ld_32(o_col + c, o);
+                    ptx::tmem_ld_wait_32(o);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0.0f;
+                }
+                if (odd) {
+                    for (int j = sg.j0; j < sg.j1; ++j) {  // the tiles that such codes left
+                        const int key0 = j * KT;
+                        if (!(key0 < it.lo_all || min(key0 + KT, it.q.L) > it.hi_all)) continue;
+                        for (int key = max(keys.lo, key0); key < min(keys.hi, key0 + KT); ++key) {
+                            const int page = p.table[int64_t(r) * p.max_pages + (key >> p.page_shift)];
+                            if (page < 0 || page >= p.n_pages) continue;
+                            const int64_t slot = (int64_t(page) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
+                            const uint32_t* v = reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(p.V) + (slot * p.Hk + g) * D + c);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (nan_codes(v[e / 4]) >> (8 * (e & 3) + 7) & 1u) o[e] = NAN;
+                        }
+                    }
+                }
+                if (!live) continue;
+                if (whole) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        uint4 u;
+                        u.x = pack_bf16x2(__fmul_rn(o[e], inv), __fmul_rn(o[e + 1], inv));
+                        u.y = pack_bf16x2(__fmul_rn(o[e + 2], inv), __fmul_rn(o[e + 3], inv));
+                        u.z = pack_bf16x2(__fmul_rn(o[e + 4], inv), __fmul_rn(o[e + 5], inv));
+                        u.w = pack_bf16x2(__fmul_rn(o[e + 6], inv), __fmul_rn(o[e + 7], inv));
+                        *reinterpret_cast<uint4*>(out + c + e) = u;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<float4*>(PL::value(part, prow, c + e)) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                }
+            }
+            if (has) {
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&o_free[t]);
+            }
+            if (!whole) {
+                soft_bar();
+                if (threadIdx.x == 0) part_publish(p.flags + J.first);
+                if (threadIdx.x == 0) cut[joins] = J;
+                ++joins;
+            }
+            x += sg.take;
+            off = 0;
+            if (x < st.x1) next_item(p, r, g, b, it.q.n);
+        }
+        // Every CTA joins its share of the items that it has a part in, once all their parts are there. The CTAs of
+        // the grid all run at once (a cooperative launch), and each publishes its parts before it waits.
+        if (joins > 0) soft_bar();
+        for (int k = 0; k < joins; ++k) {
+            const PagedJoin J = cut[k];
+            if (threadIdx.x == 0) joined = part_wait(p.flags + J.first, J.count, &abort_flag, p.status);
+            soft_bar();
+            const bool in = joined != 0;
+            if (in) join_store<D, kRows, 4, 2>(p, J, paged_req(p, J.r), int(blockIdx.x) - J.first, threadIdx.x, 32 * T::kSoftWarps);
+            soft_bar();  // before the next item's answer
+        }
+    }
+    __syncwarp();
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == T::kSoftWarps) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, kTmemAll);
+    }
+}
+
+template <int D, int CAP>
+cudaError_t launch_many8(Paged8Params& p, const PagedAttnArgs& a, cudaStream_t s) {
+    using T = Many8Traits<D>;
+    // the opt-in shared-memory size is a per-device function attribute
+    static std::mutex mu;
+    static bool done[64] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (dev < 0 || dev >= 64 || !done[dev]) {
+            e = cudaFuncSetAttribute(paged8_many_kernel<D, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::kSmem);
+            if (e != cudaSuccess) return e;
+            if (dev >= 0 && dev < 64) done[dev] = true;
+        }
+    }
+    // (as for the bf16 cache: full row tiles, less while the call would leave SMs without a unit)
+    const int sms = std::max(1, device_sm_count());
+    p.QT = 128 / p.G;
+    p.QB = T::NQ * p.QT;
+    while (p.QB * p.G > 16 && p.QB > 1 && unit_bound(a, p.QB, T::KT) < 0.6 * sms) {
+        if (p.QB > p.QT) p.QB = p.QT;
+        else p.QB = p.QT = (p.QT + 1) / 2;
+    }
+    const uint32_t box = uint32_t(std::min<int64_t>(a.page_size, T::KT));
+    if (!encode_codes(&p.k_map, a.k_cache, a, box) || !encode_codes(&p.v_map, a.v_cache, a, box) ||
+        !encode_queries(&p.q_map, a, uint32_t(p.G), uint32_t(p.QT)))
+        return cudaErrorInvalidValue;
+    const size_t part = size_t(128 * T::NQ) * (D + 2) * 4;
+    const int fit = int((EMB_PAGED_WORKSPACE - kPagedFlagBytes) / (2 * part));
+    const int ctas = std::max(1, std::min({sms, fit, int(kPagedFlagBytes / 4)}));
+    void* args[] = {&p};
+    const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, T::KT))));
+    set_grid(p, grid, D == 256 ? 8 : 2);
+    return launch_serialised(reinterpret_cast<const void*>(paged8_many_kernel<D, CAP>), grid, T::kThreads, T::kSmem, s, args, 1, true);
+}
+
+template <int D>
+cudaError_t launch_many8_d(Paged8Params& p, const PagedAttnArgs& a, cudaStream_t s) {
+    return a.cap > kMostLowCap ? launch_many8<D, kAnyCap>(p, a, s) : a.cap > 0.0f ? launch_many8<D, kLowCap>(p, a, s) : launch_many8<D, kUncapped>(p, a, s);
+}
+
+}  // namespace
+
+cudaError_t launch_paged8_many(Paged8Params& p, const PagedAttnArgs& a, cudaStream_t s) {
+    return a.head_dim == 64 ? launch_many8_d<64>(p, a, s) : a.head_dim == 128 ? launch_many8_d<128>(p, a, s) : launch_many8_d<256>(p, a, s);
+}
+
+}  // namespace emb

@@ -405,7 +405,6 @@ emb_status emb_paged8_attention(const uint16_t* Q, const uint8_t* k_codes, const
                                         max_pages, q_start, kv_len, prefix, n_req, n_tokens, max_q, O, n_heads, n_kv_heads,
                                         head_dim, scale, cap, window, workspace, ws_bytes);
     if (e != EMB_OK) return e;
-    if (n_heads / n_kv_heads > 16) return EMB_EUNSUPPORTED;
     a.k_exp = k_exp;
     a.v_exp = v_exp;
     return from_cuda(launch_paged8_attention(a, stream_of(stream)));

@@ -338,6 +338,20 @@ __device__ __forceinline__ void mma_bf16_ss(uint32_t d_tmem, uint64_t a_desc, ui
         : "memory");
 }
 
+// The same for f16 (the instruction descriptor tells A's and B's type), and for e4m3 codes from shared memory (kind::f8f6f4).
+__device__ __forceinline__ void mma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    mma_bf16_ta(d_tmem, a_tmem, b_desc, idesc, accumulate);
+}
+__device__ __forceinline__ void mma_f8_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
 // Arrive (once) on the mbarrier when every tcgen05 operation issued so far by the elected
 // thread has completed (call it converged).
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
@@ -412,7 +426,18 @@ __device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t saddr) {
     return d;
 }
 
-// The same for an MN-major operand: rows of 64 consecutive M/N elements (128 bytes, swizzled), one per k, so
+// The same for 64-byte-swizzled atoms of 8 rows x 64 bytes, every 512 B.
+__device__ __forceinline__ uint64_t smem_desc_sw64(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= uint64_t((saddr & 0x3FFFFu) >> 4);
+    d |= uint64_t(1) << 16;
+    d |= uint64_t(512 >> 4) << 32;
+    d |= uint64_t(1) << 46;
+    d |= uint64_t(4) << 61;  // layout: 64-byte swizzle
+    return d;
+}
+
+// As smem_desc_sw128, for an MN-major operand: rows of 64 consecutive M/N elements (128 bytes, swizzled), one per k, so
 // atoms of 64 elements x 8 k; `next_mn` bytes to the next 64 M/N elements, atoms of the next 8 k every 1024 B.
 __device__ __forceinline__ uint64_t smem_desc_mn_sw128(uint32_t saddr, uint32_t next_mn) {
     uint64_t d = 0;
@@ -434,6 +459,13 @@ __host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N) {
            | (uint32_t(N >> 3) << 17)       // N / 8
            | (uint32_t(M >> 4) << 24);      // M / 16
 }
+
+// Instruction descriptors for kind::f16 with f16 A/B and for kind::f8f6f4 with e4m3 A/B (both types are number 0 of their
+// kind), fp32 D, K-major.
+__host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N) {
+    return (1u << 4) | (uint32_t(N >> 3) << 17) | (uint32_t(M >> 4) << 24);
+}
+__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N) { return idesc_f16_f32(M, N); }
 
 }  // namespace ptx
 }  // namespace emb

@@ -22,7 +22,7 @@ def kernel(request):
     Paged8.many = False
 
 
-@pytest.mark.parametrize("new,kv,H,Hk,d,page", [c for c in CASES if c[2] // c[3] <= 16])
+@pytest.mark.parametrize("new,kv,H,Hk,d,page", CASES)
 @pytest.mark.parametrize("mask", ["causal", "prefix", "window", "capped", "wide cap"])
 def test_parity(cuda_device, new, kv, H, Hk, d, page, mask):
     s = Paged8(new, kv, H, Hk, d, page, seed=len(new) + sum(kv) + d)
