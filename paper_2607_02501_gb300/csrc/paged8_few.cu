@@ -1,11 +1,13 @@
 // Attention of new tokens over the 8-bit paged cache, few query rows per request: mma.sync (definition in
 // include/emb_paged.h, work split in paged_sched.cuh), and the choice between this kernel and that for many rows.
 //
-// As the kernel for the bf16 cache: a producer warp brings tiles of 64 keys and values by TMA into a ring, an item has 16 rows
-// (queries times heads), and each of four warps takes 16 of a tile's keys; the warps' results are merged at the
+// As the kernel for the bf16 cache: a producer warp brings tiles of keys and values by TMA into a ring, an item has 16 rows
+// (queries times heads), and each of four warps takes a quarter of a tile's keys; the warps' results are merged at the
 // item's end. What differs:
-// - A warp's 16 keys are one block of the cache, so a tile has one key power and one value power for each warp. The producer
-//   looks them up two tiles ahead and lays them beside the tile.
+// - Tiles of 128 keys: twice the keys for the same steps of a warp, which are a chain of latencies (64 requests of up to 16384 keys
+//   with tiles of 64: 252 us, whatever the stages).
+// - A warp's 32 keys are two blocks of the cache, with a key power and a value power each. The producer looks them up two
+//   rounds ahead and lays them beside the tile.
 // - Codes become f16 in registers, after ldmatrix, by the hardware's conversion of two at a time. A key's 16 bytes give a lane four
 //   neighbouring dims, so the queries' fragments have their dims in that order; transposed by pairs of bytes, a value's 16 bytes
 //   give it two dims of two keys, whose even and odd bytes are one fragment of the even dims' outputs and one of the odd dims'.
@@ -40,25 +42,25 @@ __device__ __forceinline__ void ldsm_x4_trans(uint32_t saddr, uint32_t (&r)[4]) 
 
 constexpr int kFewWarps = 4;
 constexpr int kFewThreads = 32 * (kFewWarps + 1);
-constexpr int kFewTile = 64;
+constexpr int kFewTile = 128;
 constexpr int kFewBlocks = kFewTile / kBlock8;
 constexpr int kFewRows = 16;
 constexpr int kFewCluster = 8;    // CTAs of a cluster, at most (the portable size)
 constexpr float kWeightUnit = 16384.0f;  // the largest weight
-static_assert(kFewBlocks == kFewWarps, "a warp's keys are a block");
+static_assert(kFewBlocks == 2 * kFewWarps, "a warp's keys are two blocks");
 
 template <int D>
 struct Few8Traits {
     static constexpr int kHalf = kFewTile * D;         // bytes of a tile's keys, and of its values
     static constexpr int kStage = 2 * kHalf;
-    static constexpr int kStages = D == 64 ? 8 : 4;
+    static constexpr int kStages = D == 64 ? 6 : 3;
     static constexpr int kCtas = D == 256 ? 1 : 2;     // per SM
-    static constexpr int kMerge = kFewWarps * kFewRows * D * 4;  // the warps' results
     static constexpr int kQPitch = D + 8;              // queries in shared memory (D = 256), f16 per padded row
     static constexpr int kQBytes = D == 256 ? kFewRows * kQPitch * 2 : 0;
     static constexpr int kFinPitch = D + 4;            // a CTA's result for its cluster, fp32 per padded row
-    static constexpr int kSmem = 1024 + kStages * kStage + kMerge + kQBytes;
+    static constexpr int kSmem = 1024 + kStages * kStage + kQBytes;
     static constexpr int kSmemCluster = kSmem + kFewRows * (kFinPitch + 2) * 4;
+    static_assert(kFewWarps * kFewRows * D * 4 <= kStage, "the warps' results fit where a tile was");
     // Byte offset of 16-byte chunk c of row r in a tile as TMA swizzles it.
     static __device__ __forceinline__ uint32_t place(int r, int c) {
         if constexpr (D == 64) return uint32_t(r * 64 + ((c ^ (r >> 1 & 3)) << 4));
@@ -74,8 +76,7 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
     using PL = PartLayout<D, ROWS>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full[T::kStages], empty[T::kStages];
-    __shared__ float key_by[T::kStages][kFewBlocks];   // 2^e of a tile's keys
-    __shared__ float2 val_exp[T::kStages][kFewBlocks];  // e of its values, 2^-e
+    __shared__ float4 powers[T::kStages][kFewBlocks];  // of a block: 2^e of its keys; e of its values, 2^-e
     __shared__ int abort_flag, joined;
     __shared__ PagedJoin cut[2];
     __shared__ float warp_m[kFewWarps][16], warp_l[kFewWarps][16], row_back[16];
@@ -127,30 +128,39 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
             const uint32_t take = min(st.x1 - x, uint32_t(it.units) - off);
             const int j0 = CL ? rank * it.nt / S : int(off), j1 = CL ? (rank + 1) * it.nt / S : min(int(off + take), it.nt);
             const int32_t* row = p.table + int64_t(r) * p.max_pages;
-            // Lane i looks up the page of the tile's block i % 4; boxes that no query sees, and pages that do not
-            // exist, are fetched from behind the cache: zeros.
+            // Two tiles at a time, sixteen lanes each: eight for the tile's blocks of keys, eight for those of values. A lane looks up its
+            // block's page one round ahead of its exponent, and that a round before it is used. Boxes that no query sees, and
+            // pages that do not exist, are fetched from behind the cache: zeros.
+            constexpr int kRound = 32 / (2 * kFewBlocks);
+            auto key_of = [&](int j) { return (it.t0 + j + lane / (2 * kFewBlocks)) * kFewTile + (lane & (kFewBlocks - 1)) * kBlock8; };
             auto page_of = [&](int j) {
-                const int key = (it.t0 + j) * kFewTile + (lane & (kFewBlocks - 1)) * kBlock8, key_box = key & ~(box - 1);
+                const int key = key_of(j), key_box = key & ~(box - 1);
                 int page = p.n_pages;
-                if (lane < 2 * kFewBlocks && j < j1 && key_box < it.hi && key_box + box > it.lo) {
+                if (j + lane / (2 * kFewBlocks) < j1 && key_box < it.hi && key_box + box > it.lo) {
                     page = row[key >> p.page_shift];
                     if (page < 0 || page > p.n_pages) page = p.n_pages;
                 }
                 return page;
             };
-            // and lanes 0 to 3 the exponent of its keys, 4 to 7 that of its values
             auto exp_of = [&](int j, int page) {
-                const int key = (it.t0 + j) * kFewTile + (lane & (kFewBlocks - 1)) * kBlock8;
-                const int64_t at = ((int64_t(page) << p.page_shift) + (key & (page_size - 1))) / kBlock8 * p.Hk + g;
+                const int64_t at = ((int64_t(page) << p.page_shift) + (key_of(j) & (page_size - 1))) / kBlock8 * p.Hk + g;
                 uint32_t e = kExpBias;
-                if (page < p.n_pages) e = (lane < kFewBlocks ? p.k_exp : p.v_exp)[at];
+                if (page < p.n_pages) e = (lane & kFewBlocks ? p.v_exp : p.k_exp)[at];
                 return e;
             };
-            int page = page_of(j0), page1 = page_of(j0 + 1);
-            uint32_t ex = exp_of(j0, page);
+            int page = page_of(j0), page1 = page_of(j0 + kRound), page2 = 0;
+            uint32_t ex = exp_of(j0, page), ex1 = 0;
             for (int j = j0; j < j1; ++j, ++issued) {
-                const int page2 = page_of(j + 2);
-                const uint32_t ex1 = exp_of(j + 1, page1);
+                const int in = (j - j0) & (kRound - 1);
+                if (in == 0) {
+                    if (j > j0) {
+                        page = page1;
+                        page1 = page2;
+                        ex = ex1;
+                    }
+                    page2 = page_of(j + 2 * kRound);
+                    ex1 = exp_of(j + kRound, page1);
+                }
                 const int s = issued % T::kStages;
                 if (issued >= uint32_t(T::kStages))
                     ptx::mbar_wait(&empty[s], (issued / T::kStages - 1) & 1, &abort_flag, p.status, kWaitLimitNs);
@@ -159,14 +169,17 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
                 uint8_t* v = k + T::kHalf;
                 if (!stop) {
                     const int e = exp_of_byte(ex);
-                    if (lane < kFewBlocks) key_by[s][lane] = pow2i(e);
-                    else if (lane < 2 * kFewBlocks) val_exp[s][lane - kFewBlocks] = make_float2(float(e), pow2i(-e));
+                    if (lane / (2 * kFewBlocks) == in) {
+                        float4& to = powers[s][lane & (kFewBlocks - 1)];
+                        if (lane & kFewBlocks) to.y = float(e), to.z = pow2i(-e);
+                        else to.x = pow2i(e);
+                    }
                     __syncwarp();
                     if (ptx::elect_one()) ptx::mbar_arrive_expect_tx(&full[s], T::kStage);
                     __syncwarp();
                     const int place = ((it.t0 + j) * kFewTile) & (page_size - 1);
                     for (int i = 0; i < n_box; ++i) {
-                        const int pg = __shfl_sync(0xffffffffu, page, i * (box / kBlock8));
+                        const int pg = __shfl_sync(0xffffffffu, page, in * 2 * kFewBlocks + i * (box / kBlock8));
                         if (ptx::elect_one()) {
                             constexpr int W = D < 128 ? D : 128;
 #pragma unroll
@@ -179,9 +192,6 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
                     }
                     ++loads;
                 }
-                page = page1;
-                page1 = page2;
-                ex = ex1;
             }
             if constexpr (CL) {
                 ptx::cluster_sync();  // (the compute warps' two)
@@ -205,10 +215,9 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
     zero_padding(p, D, threadIdx.x, 32 * kFewWarps);
     auto bar = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };
     const int quad = lane >> 2, qc = lane & 3;
-    const int wkey = warp * 16;  // the warp's keys of a tile
+    const int wkey = warp * 32;  // the warp's keys of a tile
     const uint32_t ring_u = ptx::smem_u32(ring);
-    float4* merge = reinterpret_cast<float4*>(ring + T::kStages * T::kStage);  // [warp][n-tile][lane]
-    uint8_t* behind = ring + T::kStages * T::kStage + T::kMerge;
+    uint8_t* behind = ring + T::kStages * T::kStage;
     __half* sq = reinterpret_cast<__half*>(behind);
     float* fin = reinterpret_cast<float*>(behind + T::kQBytes);  // [rows][pitch], CL only
     float *fin_m = fin + ROWS * T::kFinPitch, *fin_l = fin_m + ROWS;
@@ -314,17 +323,17 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
             const bool edge = key0 < it.lo_all || key0 + kFewTile > it.hi_all;
             // whether it holds places behind the request's last key, and keys that some row does not see
             const bool tail = key0 + kFewTile > it.q.L, hidden = key0 < it.lo_all || min(key0 + kFewTile, it.q.L) > it.hi_all;
-            const float kp = key_by[s][warp], ve = val_exp[s][warp].x, vi = val_exp[s][warp].y;
+            const float4 pw[2] = {powers[s][2 * warp], powers[s][2 * warp + 1]};
 
-            // S = Q K^T, the warp's 16 keys in two n-tiles; one ldmatrix gives the codes of four k-steps
-            float sc[2][4];
+            // S = Q K^T, the warp's 32 keys in four n-tiles; one ldmatrix gives the codes of four k-steps
+            float sc[4][4];
 #pragma unroll
-            for (int n = 0; n < 2; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.0f;
+            for (int n = 0; n < 4; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.0f;
 #pragma unroll
             for (int k4 = 0; k4 < KS; k4 += 4) {
-                uint32_t bk[2][4];
+                uint32_t bk[4][4];
 #pragma unroll
-                for (int n = 0; n < 2; ++n) ldsm_x4(kb + T::place(wkey + n * 8 + (lane & 7), k4 + (lane >> 3)), bk[n]);
+                for (int n = 0; n < 4; ++n) ldsm_x4(kb + T::place(wkey + n * 8 + (lane & 7), k4 + (lane >> 3)), bk[n]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     uint32_t a[4];
@@ -340,16 +349,16 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
                         for (int e = 0; e < 4; ++e) a[e] = qf[k4 + i][e];
                     }
 #pragma unroll
-                    for (int n = 0; n < 2; ++n) {
+                    for (int n = 0; n < 4; ++n) {
                         uint32_t b0, b1;
                         codes_to_f16x4(bk[n][i], b0, b1);
                         mma_f16(sc[n], a, b0, b1);
                     }
                 }
             }
-            const float fA = score_factor(backA * kp), fB = score_factor(backB * kp);
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
+            for (int n = 0; n < 4; ++n) {
+                const float fA = score_factor(backA * pw[n / 2].x), fB = score_factor(backB * pw[n / 2].x), ve = pw[n / 2].y;
                 float2 zA = mul2(make_float2(sc[n][0], sc[n][1]), make_float2(fA, fA));
                 float2 zB = mul2(make_float2(sc[n][2], sc[n][3]), make_float2(fB, fB));
                 if constexpr (CAP) {
@@ -363,7 +372,7 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
             }
             if (edge) {
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                for (int n = 0; n < 4; ++n)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int key = key0 + wkey + n * 8 + 2 * qc + e;
@@ -371,8 +380,12 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
                         if (key < kB.lo || key >= kB.hi) sc[n][2 + e] = -INFINITY;
                     }
             }
-            float tA = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[1][0], sc[1][1]));
-            float tB = fmaxf(fmaxf(sc[0][2], sc[0][3]), fmaxf(sc[1][2], sc[1][3]));
+            float tA = -INFINITY, tB = -INFINITY;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                tA = fmaxf(tA, fmaxf(sc[n][0], sc[n][1]));
+                tB = fmaxf(tB, fmaxf(sc[n][2], sc[n][3]));
+            }
 #pragma unroll
             for (int i = 1; i <= 2; i <<= 1) {
                 tA = fmaxf(tA, __shfl_xor_sync(0xffffffffu, tA, i));
@@ -382,19 +395,24 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
             // (a row without a finite score so far subtracts 0: its weights are 2^-inf = 0)
             const float sA0 = nA == -INFINITY ? 0.0f : nA, sB0 = nB == -INFINITY ? 0.0f : nB;
             const float cA = exp2_fast(mA - sA0), cB = exp2_fast(mB - sB0);
-            float sA = 0.0f, sB = 0.0f;
+            lA *= cA;  // lane-partial sums; the four lanes of a row are added at the end
+            lB *= cB;
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int n = 0; n < 4; n += 2) {
+                float sA = 0.0f, sB = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    // (the difference first: it is never above 0, however large the scores)
-                    sc[n][e] = exp2_fast(sc[n][e] - sA0) * kWeightUnit;
-                    sc[n][2 + e] = exp2_fast(sc[n][2 + e] - sB0) * kWeightUnit;
-                    sA += sc[n][e];
-                    sB += sc[n][2 + e];
-                }
-            lA = fmaf(lA, cA, sA * vi);  // lane-partial sums; the four lanes of a row are added at the end
-            lB = fmaf(lB, cB, sB * vi);
+                for (int m = n; m < n + 2; ++m)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        // (the difference first: it is never above 0, however large the scores)
+                        sc[m][e] = exp2_fast(sc[m][e] - sA0) * kWeightUnit;
+                        sc[m][2 + e] = exp2_fast(sc[m][2 + e] - sB0) * kWeightUnit;
+                        sA += sc[m][e];
+                        sB += sc[m][2 + e];
+                    }
+                lA = fmaf(sA, pw[n / 2].z, lA);
+                lB = fmaf(sB, pw[n / 2].z, lB);
+            }
             if (__any_sync(0xffffffffu, nA != mA || nB != mB)) {  // else every factor is 1
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
@@ -406,42 +424,48 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
             }
             mA = nA;
             mB = nB;
-            // O += P V over the 16 keys
-            const uint32_t pf[4] = {pack_f16x2(sc[0][0], sc[0][1]), pack_f16x2(sc[0][2], sc[0][3]), pack_f16x2(sc[1][0], sc[1][1]), pack_f16x2(sc[1][2], sc[1][3])};
-            // (of the fragments' keys 2 qc, 2 qc + 1 and the same + 8, those that the request has)
-            const int left = it.q.L - (key0 + wkey + 2 * qc);
-            const uint32_t in0 = (left > 0 ? 0x0000FFFFu : 0u) | (left > 1 ? 0xFFFF0000u : 0u);
-            const uint32_t in1 = (left > 8 ? 0x0000FFFFu : 0u) | (left > 9 ? 0xFFFF0000u : 0u);
-            const int vrow = wkey + (lane & 15);
+            // O += P V in two k-steps of 16 keys
 #pragma unroll
-            for (int c = 0; c < KS; c += 2) {
-                uint32_t bv[4];  // chunk c: keys 0-7, 8-15; chunk c + 1
-                ldsm_x4_trans(vb + T::place(vrow, c + (lane >> 4)), bv);
-                // values behind the request's last key are anything; NaN codes hidden from some rows may not be multiplied
-                // by their weights of 0: they are left out here and added at the end for the rows that see them
-                if (tail) {
+            for (int kk = 0; kk < 2; ++kk) {
+                const float* s0 = sc[2 * kk];
+                const float* s1 = sc[2 * kk + 1];
+                const uint32_t pf[4] = {pack_f16x2(s0[0], s0[1]), pack_f16x2(s0[2], s0[3]), pack_f16x2(s1[0], s1[1]), pack_f16x2(s1[2], s1[3])};
+                // (of the fragments' keys 2 qc, 2 qc + 1 and the same + 8, those that the request has)
+                const int left = it.q.L - (key0 + wkey + kk * 16 + 2 * qc);
+                const uint32_t in0 = (left > 0 ? 0x0000FFFFu : 0u) | (left > 1 ? 0xFFFF0000u : 0u);
+                const uint32_t in1 = (left > 8 ? 0x0000FFFFu : 0u) | (left > 9 ? 0xFFFF0000u : 0u);
+                const int vrow = wkey + kk * 16 + (lane & 15);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) bv[e] &= e & 1 ? in1 : in0;
-                }
-                if (hidden) {
-                    const uint32_t bad = nan_codes(bv[0]) | nan_codes(bv[1]) | nan_codes(bv[2]) | nan_codes(bv[3]);
-                    if (__any_sync(0xffffffffu, bad != 0)) {
-                        odd = true;
+                for (int c = 0; c < KS; c += 2) {
+                    uint32_t bv[4];  // chunk c: keys 0-7, 8-15; chunk c + 1
+                    ldsm_x4_trans(vb + T::place(vrow, c + (lane >> 4)), bv);
+                    // values behind the request's last key are anything; NaN codes hidden from some rows may not be multiplied
+                    // by their weights of 0: they are left out here and added at the end for the rows that see them
+                    if (tail) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) bv[e] = without(bv[e], nan_codes(bv[e]));
+                        for (int e = 0; e < 4; ++e) bv[e] &= e & 1 ? in1 : in0;
                     }
-                }
+                    if (hidden) {
+                        const uint32_t bad = nan_codes(bv[0]) | nan_codes(bv[1]) | nan_codes(bv[2]) | nan_codes(bv[3]);
+                        if (__any_sync(0xffffffffu, bad != 0)) {
+                            odd = true;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    uint32_t e0, o0, e1, o1;  // even and odd dims, keys 0-7 and 8-15
-                    codes_to_f16x4(__byte_perm(bv[2 * i], 0, 0x3120), e0, o0);
-                    codes_to_f16x4(__byte_perm(bv[2 * i + 1], 0, 0x3120), e1, o1);
-                    mma_f16(o[2 * (c + i)], pf, e0, e1);
-                    mma_f16(o[2 * (c + i) + 1], pf, o0, o1);
+                            for (int e = 0; e < 4; ++e) bv[e] = without(bv[e], nan_codes(bv[e]));
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t e0, o0, e1, o1;  // even and odd dims, keys 0-7 and 8-15
+                        codes_to_f16x4(__byte_perm(bv[2 * i], 0, 0x3120), e0, o0);
+                        codes_to_f16x4(__byte_perm(bv[2 * i + 1], 0, 0x3120), e1, o1);
+                        mma_f16(o[2 * (c + i)], pf, e0, e1);
+                        mma_f16(o[2 * (c + i) + 1], pf, o0, o1);
+                    }
                 }
             }
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&empty[s]);
+            // (the last tile makes room for the warps' merge first)
+            if (lane == 0 && j + 1 < j1) ptx::mbar_arrive(&empty[s]);
         }
 #pragma unroll
         for (int i = 1; i <= 2; i <<= 1) {
@@ -452,7 +476,7 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
             for (int key = (it.t0 + j0) * kFewTile; key < min((it.t0 + j1) * kFewTile, it.hi); ++key) {
                 const int in = key & (kFewTile - 1), key0 = key - in;
                 if (!(key0 < it.lo_all || min(key0 + kFewTile, it.q.L) > it.hi_all)) continue;
-                if (in < wkey || in >= wkey + 16) continue;
+                if (in < wkey || in >= wkey + 32) continue;
                 const int page = p.table[int64_t(r) * p.max_pages + (key >> p.page_shift)];
                 if (page < 0 || page >= p.n_pages) continue;
                 const int64_t slot = (int64_t(page) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
@@ -472,12 +496,14 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
             }
         }
 
-        // The warps lay their results side by side (a lane's four values of n-tile n at [n][lane]: no two lanes meet in a
-        // bank), and each adds up a quarter of the n-tiles.
+        // The warps lay their results side by side where the last tile was (a lane's four values of n-tile n at [n][lane]: no two
+        // lanes meet in a bank), and each adds up a quarter of the n-tiles.
         constexpr int kMine = NT / kFewWarps;
         const int n0 = warp * kMine;
         if (j1 > j0) {
-            bar();  // every warp is done with the last item's
+            const int s = (issued - 1) % T::kStages;
+            float4* merge = reinterpret_cast<float4*>(ring + s * T::kStage);  // [warp][n-tile][lane]
+            bar();  // every warp is done with the keys and values
 #pragma unroll
             for (int n = 0; n < NT; ++n) merge[(warp * NT + n) * 32 + lane] = make_float4(o[n][0], o[n][1], o[n][2], o[n][3]);
             if (qc == 0) {
@@ -512,6 +538,9 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
                     o[n][3] = fmaf(u.w, wB, o[n][3]);
                 }
             }
+            ptx::fence_proxy_async_smem();  // before the next copy into this buffer
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&empty[s]);
         }
 
         // a lane's four neighbouring dims of its n-tiles 2 c and 2 c + 1, for row A (h = 0) or B (h = 2)
@@ -668,10 +697,10 @@ int few8_cluster(const PagedAttnArgs& a) {
     if (a.window > 0) keys = std::min(keys, double(a.window) + kFewRows + kFewTile);
     const double items = double(a.n_req * a.n_kv_heads) * few8_blocks(a), tiles = std::ceil(keys / kFewTile);
     const double ctas = (a.head_dim == 256 ? 1.0 : 2.0) * std::max(1, device_sm_count());
-    constexpr double longest = 24.0;
+    constexpr double longest = 12.0;
     int S = kFewCluster;
     while (S > 0 && items * S > ctas) S /= 2;
-    return S > 0 && tiles <= longest * S && tiles / S <= items * tiles / ctas + 8.0 ? S : 0;
+    return S > 0 && tiles <= longest * S && tiles / S <= items * tiles / ctas + 4.0 ? S : 0;
 }
 
 template <int D, int CAP>
@@ -689,7 +718,7 @@ cudaError_t launch_few8(Paged8Params& p, const PagedAttnArgs& a, cudaStream_t s)
         return launch_serialised(reinterpret_cast<const void*>(paged8_few_kernel<D, CAP, true>), unsigned(a.n_req * a.n_kv_heads * p.side * p.cluster),
                                  kFewThreads, Few8Traits<D>::kSmemCluster, s, args, unsigned(p.cluster));
     const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, kFewTile))));
-    set_grid(p, grid, 3);
+    set_grid(p, grid, 2);
     return launch_serialised(reinterpret_cast<const void*>(paged8_few_kernel<D, CAP, false>), grid, kFewThreads, Few8Traits<D>::kSmem, s, args, 1, true);
 }
 

@@ -52,10 +52,9 @@ static_assert(Many8Traits<64>::kSmem > 114 * 1024 && Many8Traits<128>::kSmem > 1
 // Tiles whose exponents are held: the producer is at most five ahead of the softmax, as keys' places are handed back behind the
 // products of a tile, and those wait for the softmax of the tile before it.
 constexpr int kScaleTiles = 8;
-constexpr float kLift = 6.0f;          // log2 of what weights are multiplied by
-constexpr float kMostLag = 8.0f;       // of the running maximum
-// Above this a maximum's rounding is felt in f16's range: the weights' exponents are then held to kLift + kMostLag one by one.
-constexpr float kLargeScore = 524288.0f;
+constexpr float kLift = 6.0f;     // the running maximum is held that much lower: weights are times 2^6,
+constexpr float kMostLag = 8.0f;  // and it moves when it is exceeded by as much more
+constexpr float kLargeScore = 4194304.0f;  // 2^22
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
@@ -157,12 +156,10 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
     constexpr int NQ = T::NQ, KT = T::KT, NB = T::NB;
     constexpr int kRows = 128 * NQ;
     using PL = PartLayout<D, kRows>;
-    // what stands for the score of a key that a row does not see (a cap would make -infinity finite)
-    constexpr float kHidden = CAP ? -3.402823466e38f : -INFINITY;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t k_full[T::kKeys], k_empty[T::kKeys], raw_full[T::kVals], raw_empty[T::kVals], v_full[T::kConvs], v_empty[T::kConvs];
     __shared__ uint64_t q_full, q_ready, q_empty, scale_full[kScaleTiles], s_full[2], p_ready[2], o_done[2], o_free[2], drain;
-    __shared__ float4 scales[kScaleTiles][NB];  // of a block: 2^e of its keys; e and 2^-e of its values
+    __shared__ float2 scales[kScaleTiles][NB];  // of a block: 2^e of its keys, e of its values
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag, joined, odd_seen;
     __shared__ PagedJoin cut[2];
@@ -251,36 +248,45 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
                 ++items;
             }
             const int32_t* row = p.table + int64_t(r) * p.max_pages;
-            // Lane i looks up the page of the tile's block i % NB; boxes that no query sees, and pages that do not exist, are
-            // fetched from behind the cache: zeros.
+            // A round of tiles at a time, 2 NB lanes each: first for the tile's blocks of keys, then for those of values. A lane looks up its
+            // block's page one round ahead of its exponent, and that a round before it is used. Boxes that no query sees, and pages
+            // that do not exist, are fetched from behind the cache: zeros.
+            constexpr int kRound = 32 / (2 * NB);
+            auto key_of = [&](int j) { return (j + lane / (2 * NB)) * KT + (lane & (NB - 1)) * kBlock8; };
             auto page_of = [&](int j) {
-                const int key = j * KT + (lane & (NB - 1)) * kBlock8, key_box = key & ~(box - 1);
+                const int key = key_of(j), key_box = key & ~(box - 1);
                 int page = p.n_pages;
-                if (lane < 2 * NB && j < sg.j1 && key_box < it.hi && key_box + box > it.lo) {
+                if (j + lane / (2 * NB) < sg.j1 && key_box < it.hi && key_box + box > it.lo) {
                     page = row[key >> p.page_shift];
                     if (page < 0 || page > p.n_pages) page = p.n_pages;
                 }
                 return page;
             };
-            // and the lanes below NB the exponent of its keys, the next NB that of its values
             auto exp_of = [&](int j, int page) {
-                const int key = j * KT + (lane & (NB - 1)) * kBlock8;
-                const int64_t at = ((int64_t(page) << p.page_shift) + (key & (page_size - 1))) / kBlock8 * p.Hk + g;
+                const int64_t at = ((int64_t(page) << p.page_shift) + (key_of(j) & (page_size - 1))) / kBlock8 * p.Hk + g;
                 uint32_t e = kExpBias;
-                if (page < p.n_pages) e = (lane < NB ? p.k_exp : p.v_exp)[at];
+                if (page < p.n_pages) e = (lane & NB ? p.v_exp : p.k_exp)[at];
                 return e;
             };
-            int page = page_of(sg.j0), page1 = page_of(sg.j0 + 1);
-            uint32_t ex = exp_of(sg.j0, page);
+            int page = page_of(sg.j0), page1 = page_of(sg.j0 + kRound), page2 = 0;
+            uint32_t ex = exp_of(sg.j0, page), ex1 = 0;
             for (int j = sg.j0; j < sg.j1 && ok; ++j) {
-                const int page2 = page_of(j + 2);
-                const uint32_t ex1 = exp_of(j + 1, page1);
+                const int turn = (j - sg.j0) & (kRound - 1);
+                if (turn == 0) {
+                    if (j > sg.j0) {
+                        page = page1;
+                        page1 = page2;
+                        ex = ex1;
+                    }
+                    page2 = page_of(j + 2 * kRound);
+                    ex1 = exp_of(j + kRound, page1);
+                }
                 const int place = (j * KT) & (page_size - 1);
                 auto fetch = [&](uint8_t* to, const CUtensorMap* map, uint64_t* bar) {
                     if (ptx::elect_one()) ptx::mbar_arrive_expect_tx(bar, T::kRaw);
                     __syncwarp();
                     for (int i = 0; i < n_box; ++i) {
-                        const int pg = __shfl_sync(all, page, i * (box / kBlock8));
+                        const int pg = __shfl_sync(all, page, turn * 2 * NB + i * (box / kBlock8));
                         if (ptx::elect_one()) {
 #pragma unroll
                             for (int c = 0; c < D / T::W; ++c)
@@ -292,11 +298,9 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
                 if (keys >= uint32_t(T::kKeys)) ok = wait(&k_empty[ka.slot], ka.turn ^ 1u);
                 if (!ok) break;
                 const int e = exp_of_byte(ex), s = int(keys % kScaleTiles);
-                if (lane < NB) {
-                    scales[s][lane].x = pow2i(e);
-                } else if (lane < 2 * NB) {
-                    scales[s][lane - NB].y = float(e);
-                    scales[s][lane - NB].z = pow2i(-e);
+                if (lane / (2 * NB) == turn) {
+                    if (lane & NB) scales[s][lane & (NB - 1)].y = float(e);
+                    else scales[s][lane & (NB - 1)].x = pow2i(e);
                 }
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&scale_full[s]);
@@ -308,9 +312,6 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
                 fetch(vring + va.slot * T::kRaw, &p.v_map, &raw_full[va.slot]);
                 ++values;
                 va.next();
-                page = page1;
-                page1 = page2;
-                ex = ex1;
             }
             x += sg.take;
             off = 0;
@@ -331,7 +332,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
         RingPlace<T::kKeys> keys;     // of tile j
         RingPlace<T::kConvs> values;  // of the tile before it
         uint32_t scores[2] = {0, 0}, owned[2] = {0, 0};  // score tiles by place, items with outputs by row tile
-        bool ok = true;
+        bool ok = true, used = false;  // used: a product of the tile's values was issued
         // (operands in a form that the compiler knows to be uniform: see ptx::elect_one)
         auto qk = [&](int t, int place, int slot) {  // S[place] = Q[t] K^T, nearest codes and rests
             const uint32_t k = ptx::warp_uniform(kring_u + uint32_t(slot * T::kRaw)), q = sq_u + uint32_t(t * T::kQTile);
@@ -376,6 +377,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
                         if (!ok) return;
                         ptx::tc_fence_after();
                         pv(t, place, values.slot, first);
+                        used = true;
                         if (first) ++owned[t];
                     };
                     if constexpr (NQ == 2) {
@@ -398,8 +400,9 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
                     if (!ok) break;
                     if (j > sg.j0) {
                         // (a tile that no row tile needed is handed back no sooner than it has arrived)
-                        ok = wait(&v_full[values.slot], values.turn);
+                        if (!used) ok = wait(&v_full[values.slot], values.turn);
                         if (!ok) break;
+                        used = false;
                         ptx::mma_commit(&v_empty[values.slot]);
                         values.next();
                     }
@@ -421,19 +424,35 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
     } else if (warp >= T::kSoftWarps) {
         // ------------------------------------------------------ values to f16, half a tile a warp
         if constexpr (NQ == 2) ptx::regs_down<72>();
+        // a thread's first key and chunk, keys to its next one, steps over the keys (heads of 256: twice)
+        constexpr int kStep = D == 64 ? 16 : 8, kSteps = KT / kStep, kEach = KT * D / 16 / 64;
+        // Chunks in flight: more of them hold up the softmax, whose accesses stand behind these in the load and store unit (4096 tokens
+        // over 16384 keys: 2 793 us, 4 843, 8 936).
+        constexpr int kBatch = 2;
+        const int key_first = (lane & 7) + (D == 64 ? (warp & 1) * 8 : 0), c_first = (D == 64 ? 0 : (warp & 1) * 4) + lane / 8;
         uint32_t n = 0;
         RingPlace<T::kVals> from;
         RingPlace<T::kConvs> to;
         bool ok = true;
         while (x < st.x1 && ok) {
-            const Segment<D> sg = segment_of<D>(p, r, g, b, off, x, st.x1);
-            const PagedItem& it = sg.it;
-            for (int j = sg.j0; j < sg.j1 && ok; ++j, ++n) {
+            int j, j1, L, lo_all, hi_all, queries;  // (little of a segment is kept: registers are few here)
+            {
+                const Segment<D> sg = segment_of<D>(p, r, g, b, off, x, st.x1);
+                j = sg.j0;
+                j1 = sg.j1;
+                L = sg.it.q.L;
+                lo_all = sg.it.lo_all;
+                hi_all = sg.it.hi_all;
+                queries = sg.it.q.n;
+                x += sg.take;
+                off = 0;
+            }
+            for (; j < j1 && ok; ++j, ++n) {
                 const int key0 = j * KT;
                 // Values behind the request's last key are anything: zeros. NaN codes hidden from some rows may not be
                 // multiplied by their weights of 0: they leave the tile here and are added at the item's end for the rows that
                 // see them.
-                const bool tail = key0 + KT > it.q.L, hidden = key0 < it.lo_all || min(key0 + KT, it.q.L) > it.hi_all;
+                const bool tail = key0 + KT > L, hidden = key0 < lo_all || min(key0 + KT, L) > hi_all;
                 ok = wait(&raw_full[from.slot], from.turn);
                 if (ok && n >= uint32_t(T::kConvs)) ok = wait(&v_empty[to.slot], to.turn ^ 1u);
                 if (!ok) break;
@@ -441,26 +460,38 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
                 uint8_t* out = conv + to.slot * T::kConv;
                 uint32_t odd = 0;
                 // 16 codes of a key at a time; eight lanes have neighbouring keys, which meet in no bank
-                constexpr int kChunks = D / 16, kEach = KT * kChunks / 64;
-#pragma unroll 8
-                for (int i = 0; i < kEach; ++i) {
-                    const int e = (i * 2 + (warp & 1)) * 32 + lane, key = (e & 7) | (e / 8 / kChunks) << 3, c = e / 8 % kChunks;
-                    uint4 w = *reinterpret_cast<const uint4*>(in + T::place(key, c));
-                    if (tail && key0 + key >= it.q.L) w = make_uint4(0, 0, 0, 0);
-                    if (hidden) {
-                        const uint32_t bx = nan_codes(w.x), by = nan_codes(w.y), bz = nan_codes(w.z), bw = nan_codes(w.w);
-                        odd |= bx | by | bz | bw;
-                        w = make_uint4(without(w.x, bx), without(w.y, by), without(w.z, bz), without(w.w, bw));
+                const uint8_t* at = in + T::place(key_first, c_first);
+                uint8_t* row = out + (c_first >> 2) * T::kSub + key_first * 128;
+                const int s0 = (((c_first & 3) * 2) ^ (key_first & 7)) << 4, s1 = (((c_first & 3) * 2 + 1) ^ (key_first & 7)) << 4;
+                auto from_of = [](int i) { return (i % kSteps) * kStep * T::W + (i / kSteps) * T::kSub; };
+                auto to_of = [](int i) { return (i % kSteps) * kStep * 128 + (i / kSteps) * 2 * T::kSub; };
+                auto fetch = [&](int i, uint4 (&w)[kBatch]) {
+#pragma unroll
+                    for (int k = 0; k < kBatch; ++k) w[k] = *reinterpret_cast<const uint4*>(at + from_of(i + k));
+                };
+                auto put = [&](int i, uint4 (&w)[kBatch]) {
+#pragma unroll
+                    for (int k = 0; k < kBatch; ++k) {
+                        if (tail && key0 + key_first + (i + k) % kSteps * kStep >= L) w[k] = make_uint4(0, 0, 0, 0);
+                        if (hidden) {
+                            const uint32_t bx = nan_codes(w[k].x), by = nan_codes(w[k].y), bz = nan_codes(w[k].z), bw = nan_codes(w[k].w);
+                            odd |= bx | by | bz | bw;
+                            w[k] = make_uint4(without(w[k].x, bx), without(w[k].y, by), without(w[k].z, bz), without(w[k].w, bw));
+                        }
+                        uint4 a, d;
+                        codes_to_f16x4(w[k].x, a.x, a.y);
+                        codes_to_f16x4(w[k].y, a.z, a.w);
+                        codes_to_f16x4(w[k].z, d.x, d.y);
+                        codes_to_f16x4(w[k].w, d.z, d.w);
+                        *reinterpret_cast<uint4*>(row + to_of(i + k) + s0) = a;
+                        *reinterpret_cast<uint4*>(row + to_of(i + k) + s1) = d;
                     }
-                    uint4 a, d;
-                    codes_to_f16x4(w.x, a.x, a.y);
-                    codes_to_f16x4(w.y, a.z, a.w);
-                    codes_to_f16x4(w.z, d.x, d.y);
-                    codes_to_f16x4(w.w, d.z, d.w);
-                    uint8_t* row = out + (c >> 2) * T::kSub + key * 128;
-                    const int k2 = (c & 3) * 2;
-                    *reinterpret_cast<uint4*>(row + ((k2 ^ (key & 7)) << 4)) = a;
-                    *reinterpret_cast<uint4*>(row + (((k2 + 1) ^ (key & 7)) << 4)) = d;
+                };
+                uint4 w[kBatch];
+#pragma unroll 1
+                for (int i = 0; i < kEach; i += kBatch) {
+                    fetch(i, w);
+                    put(i, w);
                 }
                 // (never taken back: the softmax may be some items behind. Items without such codes are then searched for nothing)
                 if (odd) *reinterpret_cast<volatile int*>(&odd_seen) = 1;
@@ -474,9 +505,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
                 from.next();
                 to.next();
             }
-            x += sg.take;
-            off = 0;
-            if (x < st.x1) next_item(p, r, g, b, it.q.n);
+            if (x < st.x1) next_item(p, r, g, b, queries);
         }
     } else {
         // ---------------------------------------------------------------------- softmax
@@ -507,17 +536,28 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
                 if (lane == 0) ptx::mbar_arrive(&q_ready);
             }
             if constexpr (!CAP) back *= p.scale2;
-            // whether the row has seen a score, its running maximum of score plus value exponent in base 2 (negated, so that it is
-            // added), sums of weights without the values' powers. A cap makes a score of -infinity one of -cap, which counts.
+            // whether the row has seen a score, its running maximum of score plus value exponent in base 2 (negated and lifted, so
+            // that it is added), sums of weights without the values' powers
             bool any = false;
             float mc = 0.0f;
             float2 l2 = make_float2(0, 0);
+            bool large = false;  // a maximum is so large that its rounding is felt in f16's range: weights are held below it one by one
             for (int j = sg.j0; j < sg.j1; ++j, ++n) {
+                wait(&scale_full[n % kScaleTiles], n / kScaleTiles);  // (every turn of it, also of tiles that the row tile skips)
                 if (j < a_t || j >= b_t) continue;
                 const int place = NQ == 2 ? t : int(n & 1);
-                const float4* block = scales[n % kScaleTiles];
+                // The factors of the blocks' raw scores, held so that a product neither overflows nor makes NaN of what is hidden,
+                // and the values' exponents: read while the scores are still being made. (A load from shared memory between scores
+                // and weights costs its latency in every tile, more registers than these spill.)
+                const float2* block = scales[n % kScaleTiles];
+                float by[NB], up[NB];
+#pragma unroll
+                for (int k = 0; k < NB; ++k) {
+                    const float2 bl = block[k];
+                    by[k] = fminf(fmaxf(back * bl.x, 1e-37f), 1.2676506e30f);
+                    up[k] = bl.y;
+                }
                 wait(&s_full[place], seen[place]++);
-                wait(&scale_full[n % kScaleTiles], n / kScaleTiles);  // (behind the scores: of this turn, as tiles may be skipped)
                 ptx::tc_fence_after();
                 const uint32_t s_col = tmem + lanes + uint32_t(place * KT);
                 const int key0 = j * KT;
@@ -526,9 +566,6 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
                 // Votes are taken among rows that see a key of the tile. A tile's other rows are not of this request, or not
                 // even filled (3 heads: 126 of 128 rows), and what they hold may not decide how a warp computes.
                 const bool sees = max(lo, 0) < min(hi, KT);
-                // the factor of a block's raw scores (times what is hidden it stays hidden)
-                auto factor = [&](int k) { return fminf(fmaxf(back * block[k].x, 1e-37f), 3e38f); };
-                float far = 0.0f;  // for a cap: the largest magnitude of q.k that the row sees
                 if (edge) {
                     // scores that the row does not see, in tensor memory: rolled up and away from the path of most tiles
 #pragma unroll 1
@@ -537,13 +574,8 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
                         uint32_t w[32];
                         ptx::tmem_ld_32(s_col + c, v);
                         ptx::tmem_ld_wait_32(v);
-                        const float f[2] = {CAP ? factor(c / 16) : 0.0f, CAP ? factor(c / 16 + 1) : 0.0f};
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const bool in = c + e >= lo && c + e < hi;
-                            if (CAP && in) far = fmaxf(far, fabsf(v[e] * f[e / 16]));
-                            w[e] = __float_as_uint(in ? v[e] : kHidden);
-                        }
+                        for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(c + e >= lo && c + e < hi ? v[e] : -INFINITY);
                         ptx::tmem_st_32(s_col + c, w);
                     }
                     ptx::tmem_st_wait();
@@ -551,35 +583,31 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
                 float s[KT];
 #pragma unroll
                 for (int c = 0; c < KT; c += 32) ptx::tmem_ld_32(s_col + c, s + c);
-                float zt = -INFINITY;
+                float zt = -INFINITY, far = 0.0f;  // far, for a cap: the largest magnitude of q.k that the row sees
 #pragma unroll
                 for (int c = 0; c < KT; c += 32) {
                     ptx::tmem_ld_wait_32(s + c);
 #pragma unroll
-                    for (int h = 0; h < 32; h += 16) {
-                        float top[4];
+                    for (int h = c; h < c + 32; h += 16) {
+                        // (the maximum is of raw scores: their factor, positive, and a cap keep their order)
+                        float top[5];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) top[k] = max3(max3(-INFINITY, s[c + h + k], s[c + h + 4 + k]), s[c + h + 8 + k], s[c + h + 12 + k]);
-                        const float mt = fmaxf(max3(top[0], top[1], top[2]), top[3]);
-                        const float4 bl = block[(c + h) / 16];
-                        const float f = fminf(fmaxf(back * bl.x, 1e-37f), 3e38f);
+                        for (int k = 0; k < 5; ++k) top[k] = max3(s[h + 3 * k], s[h + 3 * k + 1], s[h + 3 * k + 2]);
+                        const float most = max3(max3(top[0], top[1], top[2]), max3(top[3], top[4], s[h + 15]), -INFINITY);
                         if constexpr (CAP) {
-                            if (!edge) {
-                                float least = s[c + h];
 #pragma unroll
-                                for (int e = 1; e < 16; ++e) least = fminf(least, s[c + h + e]);
-                                far = max3(far, fabsf(mt * f), fabsf(least * f));
-                            }
-                            const float z = capped2<CAP>(make_float2(mt * f, mt * f), p).x + bl.y;
-                            zt = mt == kHidden ? zt : fmaxf(zt, z);
+                            for (int e = 0; e < 16; ++e) far = fmaxf(far, s[h + e] == -INFINITY ? 0.0f : fabsf(s[h + e] * by[h / 16]));
+                            const float z = capped2<CAP>(make_float2(most * by[h / 16], most * by[h / 16]), p).x + up[h / 16];
+                            zt = most == -INFINITY ? zt : fmaxf(zt, z);
                         } else {
-                            zt = fmaxf(zt, fmaf(mt, f, bl.y));
+                            zt = fmaxf(zt, fmaf(most, by[h / 16], up[h / 16]));
                         }
                     }
                 }
-                const bool grow = sees && (any ? zt + mc > kMostLag : CAP || zt > -INFINITY);
+                const bool grow = sees && (any ? zt + mc > kLift + kMostLag : zt > -INFINITY);
                 if (__any_sync(all, grow)) {
-                    const float f = !grow ? 1.0f : any ? exp2_fast(-mc - zt) : 0.0f;
+                    const float now = kLift - zt;
+                    const float f = !grow ? 1.0f : any ? exp2_fast(now - mc) : 0.0f;
                     if (j > a_t) {
                         wait(&o_done[t], outs - 1);  // every product issued so far is in
                         ptx::tc_fence_after();
@@ -598,55 +626,51 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
                         l2.x *= f;
                         l2.y *= f;
                         any = true;
-                        mc = -zt;
+                        mc = now;
                     }
+                    large = __any_sync(all, any && fabsf(mc) > kLargeScore);
                 }
-                // The weights, two blocks at a time, over the scores. base(u, f, m) gives two scores in base 2 plus m, the block's value
-                // exponent less the row's maximum.
+                // The weights, 32 at a time, over the scores. base(u, f, m) gives two weights' exponents from raw scores, their
+                // block's factor, and its value exponent less the row's maximum.
                 auto weights = [&](auto base) {
 #pragma unroll
                     for (int c = 0; c < KT; c += 32) {
                         uint32_t w[16];
 #pragma unroll
-                        for (int h = 0; h < 32; h += 16) {
-                            const float4 bl = block[(c + h) / 16];
-                            const float f = fminf(fmaxf(back * bl.x, 1e-37f), 3e38f), m = (bl.y + mc) + kLift;
+                        for (int h = c; h < c + 32; h += 16) {
+                            const float m = up[h / 16] + mc;
                             float2 sum = make_float2(0, 0);
 #pragma unroll
                             for (int e = 0; e < 16; e += 2) {
-                                float2 u = base(make_float2(s[c + h + e], s[c + h + e + 1]), make_float2(f, f), make_float2(m, m));
+                                float2 u = base(make_float2(s[h + e], s[h + e + 1]), make_float2(by[h / 16], by[h / 16]), make_float2(m, m));
                                 u.x = exp2_fast(u.x);
                                 u.y = exp2_fast(u.y);
                                 sum = add2(sum, u);
-                                w[(h + e) / 2] = pack_f16x2(u.x, u.y);
+                                w[(h - c + e) / 2] = pack_f16x2(u.x, u.y);
                             }
-                            l2 = fma2(sum, make_float2(bl.z, bl.z), l2);
+                            const float inv = exp2_fast(-up[h / 16]);
+                            l2 = fma2(sum, make_float2(inv, inv), l2);
                         }
                         ptx::tmem_st_16(s_col + c / 2, w);
                     }
                 };
-                const bool large = __any_sync(all, sees && fabsf(mc) > kLargeScore);
-                auto held = [](float2 u) { return make_float2(fminf(u.x, kLift + kMostLag), fminf(u.y, kLift + kMostLag)); };
+                // (NaN stays NaN)
+                auto held = [](float2 z) {
+                    return make_float2(z.x > kLift + kMostLag ? kLift + kMostLag : z.x, z.y > kLift + kMostLag ? kLift + kMostLag : z.y);
+                };
                 if constexpr (!CAP) {
                     if (!large) weights([&](float2 u, float2 f, float2 m) { return fma2(u, f, m); });
-                    // (NaN stays NaN: the minimum would hide it)
-                    else weights([&](float2 u, float2 f, float2 m) {
-                        const float2 z = fma2(u, f, m), h = held(z);
-                        return make_float2(z.x != z.x ? z.x : h.x, z.y != z.y ? z.y : h.y);
-                    });
+                    else weights([&](float2 u, float2 f, float2 m) { return held(fma2(u, f, m)); });
                 } else {
-                    const bool near = !large && __all_sync(all, !sees || far * p.scale2 < kNearCap);
                     auto shown = [](float2 u, float2 z) {
-                        return make_float2(u.x == kHidden ? -INFINITY : z.x, u.y == kHidden ? -INFINITY : z.y);
+                        return make_float2(u.x == -INFINITY ? -INFINITY : z.x, u.y == -INFINITY ? -INFINITY : z.y);
                     };
                     // far below the cap one power of two per score, where exponential and reciprocal take two more turns of
                     // the same unit
-                    if (near && !edge) weights([&](float2 u, float2 f, float2 m) { return capped_near2(mul2(u, f), p, m); });
-                    else if (near) weights([&](float2 u, float2 f, float2 m) { return shown(u, capped_near2(mul2(u, f), p, m)); });
-                    else weights([&](float2 u, float2 f, float2 m) {
-                        const float2 z = add2(capped2<CAP>(mul2(u, f), p), m), h = held(z);
-                        return shown(u, make_float2(z.x != z.x ? z.x : h.x, z.y != z.y ? z.y : h.y));
-                    });
+                    if (!large && __all_sync(all, !sees || far * p.scale2 < kNearCap))
+                        weights([&](float2 u, float2 f, float2 m) { return shown(u, capped_near2(mul2(u, f), p, m)); });
+                    else
+                        weights([&](float2 u, float2 f, float2 m) { return shown(u, held(add2(capped2<CAP>(mul2(u, f), p), m))); });
                 }
                 // every phase of o_done is waited for, so that a wait cannot take the one before the last for the last:
                 // with two score places the last scores do not tell that the product before theirs is in

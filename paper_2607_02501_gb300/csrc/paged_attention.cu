@@ -610,6 +610,8 @@ bool encode_cache(CUtensorMap* m, const void* base, const PagedAttnArgs& a, uint
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// (A row of codes is 64 to 256 bytes: what lies behind it belongs to the next head, which another CTA fetches at its own time.
+// Promoted to 256 bytes, 64 requests of up to 16384 keys of 8 heads of 128 take 252 us instead of 212.)
 bool encode_codes(CUtensorMap* m, const void* base, const PagedAttnArgs& a, uint32_t box) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
@@ -619,7 +621,7 @@ bool encode_codes(CUtensorMap* m, const void* base, const PagedAttnArgs& a, uint
     const cuuint32_t boxes[4] = {cuuint32_t(std::min<cuuint64_t>(D, 128)), 1, box, 1}, ones[4] = {1, 1, 1, 1};
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, boxes, ones,
               CU_TENSOR_MAP_INTERLEAVE_NONE, D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 bool encode_queries(CUtensorMap* m, const PagedAttnArgs& a, uint32_t heads, uint32_t tokens) {
