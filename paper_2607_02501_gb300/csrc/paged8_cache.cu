@@ -10,278 +10,300 @@ namespace emb {
 namespace {
 
 // ------------------------------------------------------------------ norm, rotation, store
-// HBM bounds it. Every thread has eight elements of a row (a head of a token): the four pairs 4 u .. 4 u + 3, so the rotation
-// stays within the thread and the sum of squares is a shuffle over the row's d / 8 lanes.
-// A CTA (16 rows' threads) takes either queries of a few heads, or one key/value head of a window of 16 tokens. A block's exponent
+// HBM bounds it, and the instructions are not far behind. Every thread has E elements of a row (a head of a token): E / 2 pairs
+// one after another, so the rotation stays within the thread and the sum of squares is a shuffle over the row's d / E lanes. E is 16
+// where both halves of the turned elements are whole groups of eight, else 8.
+// A CTA takes either queries of a few heads, or the keys or the values of one head of a window of 16 tokens. A block's exponent
 // needs all tokens of the call that go into it, which stand within 16 of one another: the CTA takes those blocks whose first token
 // is in its window, up to 15 tokens beyond it, and leaves those that began before. So no two CTAs meet in a block, nothing is
-// exchanged between CTAs, and a token's rows stay in registers between the block's maximum and the rounding.
-constexpr int kRows8 = 16;   // rows that a CTA has threads for
-constexpr int kHeads8 = 4;   // heads that a thread takes of its token
+// exchanged between CTAs, and a token's rows stay in registers between the block's maximum and the rounding. Every warp works out
+// the blocks of all 32 tokens by itself, a lane a token, so there is one barrier.
+constexpr int kStoreThreads = 256;
+constexpr int kWindow8 = 16;  // tokens
+constexpr int kMostRounds = 4;  // pairs of heads that a thread takes of its token, at most
 
 struct Store8Params {
     Store8Args a;
-    int q_ctas, kv_windows;
-    int log_tokens, head_groups;  // queries: a CTA's tokens 2^n, CTAs to share a token's heads
+    int kv_ctas;                         // the first CTAs: keys and values
+    int log_tokens, rounds, head_groups; // queries: a CTA's tokens 2^n, a thread's pairs of heads, CTAs to share a token's heads
 };
 
 // Cosine and sine of `factor` times a pair's angle. The product of position and turns wraps at 2^64, one turn, so the
 // angle's fraction is exact; its upper 32 bits go to the hardware's sine and cosine in +-pi (error below 2^-21).
 __device__ __forceinline__ void angle_of(int32_t at, uint64_t turns, float factor, float& c, float& s) {
-    const uint64_t t = uint64_t(int64_t(at)) * turns;
-    __sincosf(float(int32_t(uint32_t(t >> 32))) * (6.283185307179586f / 4294967296.0f), &s, &c);
+    // (the upper half of the product modulo 2^64, from the 32-bit halves)
+    const uint32_t lo = uint32_t(turns), hi = uint32_t(turns >> 32), p = uint32_t(at);
+    const uint32_t top = __umulhi(p, lo) + p * hi - (at < 0 ? lo : 0u);
+    __sincosf(float(int32_t(top)) * (6.283185307179586f / 4294967296.0f), &s, &c);
     c *= factor;
     s *= factor;
 }
 
-// Where a thread's elements lie: two groups of four at e0 and e1. Halves: firsts and seconds of its pairs; elements behind the turned
-// ones likewise. Neighbours: eight in a row.
-template <int D, bool NB>
+// Where a thread's elements lie: two groups of E / 2 at e0 and e1. Halves: firsts and seconds of its pairs; elements behind the
+// turned ones likewise. Neighbours: E in a row.
+template <int D, bool NB, int E>
 struct Place8 {
     int e0, e1;
     bool turned;
     __device__ __forceinline__ Place8(int u, int rot) {
         if constexpr (NB) {
-            e0 = u * 8;
-            e1 = e0 + 4;
+            e0 = u * E;
+            e1 = e0 + E / 2;
             turned = e0 < rot;
         } else {
-            const int half = rot / 2, units = half / 4;
+            const int half = rot / 2, units = half / (E / 2);
             turned = u < units;
-            e0 = turned ? u * 4 : rot + (u - units) * 4;
-            e1 = turned ? half + u * 4 : e0 + (D - rot) / 2;
+            e0 = turned ? u * (E / 2) : rot + (u - units) * (E / 2);
+            e1 = turned ? half + u * (E / 2) : e0 + (D - rot) / 2;
         }
     }
 };
 
-__device__ __forceinline__ void load4(const uint16_t* p, float* x) {
-    const uint2 w = *reinterpret_cast<const uint2*>(p);
-    const float2 a = unpack_bf16x2(w.x), b = unpack_bf16x2(w.y);
-    x[0] = a.x;
-    x[1] = a.y;
-    x[2] = b.x;
-    x[3] = b.y;
+// N bf16 numbers (4 or 8, aligned to their size) from and to memory.
+template <int N>
+__device__ __forceinline__ void load_row(const uint16_t* p, float* x) {
+    uint32_t w[N / 2];
+    if constexpr (N == 8) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(p);
+    else *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(p);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        const float2 u = unpack_bf16x2(w[i]);
+        x[2 * i] = u.x;
+        x[2 * i + 1] = u.y;
+    }
+}
+template <int N>
+__device__ __forceinline__ void store_row(uint16_t* p, const float* x) {
+    uint32_t w[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+    if constexpr (N == 8) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(w);
+    else *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(w);
 }
 
-// A row in place: norm (g: the thread's eight gains, or none) and rotation.
-template <int D, bool NB>
-__device__ __forceinline__ void norm_turn(float (&x)[8], bool norm, const float* g, float eps, bool turned, const float (&c)[4], const float (&s)[4]) {
-    if (norm) {
-        float ss = 0.0f;
+// A row in place: norm (with the head's gains, or none) and rotation.
+template <int D, bool NB, int E>
+__device__ __forceinline__ void norm_turn(float (&x)[E], const float* gamma, float eps, const Place8<D, NB, E>& at, const float (&c)[E / 2], const float (&s)[E / 2]) {
+    if (gamma) {
+        float2 s2 = make_float2(0, 0);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+        for (int e = 0; e < E; e += 2) s2 = fma2(make_float2(x[e], x[e + 1]), make_float2(x[e], x[e + 1]), s2);
+        float ss = s2.x + s2.y;
 #pragma unroll
-        for (int o = D / 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        for (int o = D / E / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         const float inv = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(ss * (1.0f / D), eps)));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * g[e];
+        for (int e = 0; e < E; e += 4) {
+            const float4 g = *reinterpret_cast<const float4*>(gamma + (e < E / 2 ? at.e0 + e : at.e1 + e - E / 2));
+            x[e] = x[e] * inv * g.x;
+            x[e + 1] = x[e + 1] * inv * g.y;
+            x[e + 2] = x[e + 2] * inv * g.z;
+            x[e + 3] = x[e + 3] * inv * g.w;
+        }
     }
-    if (turned) {
+    if (!at.turned) return;
+    if constexpr (NB) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float& a = x[NB ? 2 * i : i];
-            float& b = x[NB ? 2 * i + 1 : 4 + i];
-            const float y = fmaf(a, c[i], -b * s[i]);
-            b = fmaf(b, c[i], a * s[i]);
-            a = y;
+        for (int i = 0; i < E / 2; ++i) {
+            const float a = x[2 * i], b = x[2 * i + 1];
+            x[2 * i] = fmaf(a, c[i], -b * s[i]);
+            x[2 * i + 1] = fmaf(b, c[i], a * s[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < E / 2; i += 2) {
+            const float2 a = make_float2(x[i], x[i + 1]), b = make_float2(x[E / 2 + i], x[E / 2 + i + 1]);
+            const float2 c2 = make_float2(c[i], c[i + 1]), s2 = make_float2(s[i], s[i + 1]), bs = mul2(b, s2);
+            const float2 y = fma2(a, c2, make_float2(-bs.x, -bs.y)), z = fma2(b, c2, mul2(a, s2));
+            x[i] = y.x;
+            x[i + 1] = y.y;
+            x[E / 2 + i] = z.x;
+            x[E / 2 + i + 1] = z.y;
         }
     }
 }
 
-template <int D, bool NB>
-__global__ void __launch_bounds__(kRows8* D / 8) paged8_store_kernel(const __grid_constant__ Store8Params p) {
-    constexpr int kLanes = D / 8;
+// (three CTAs per SM: without the bound two fit, and 15600 tokens of 10 heads of 256 with eight elements a thread took 79 us, so 60)
+template <int D, bool NB, int E>
+__global__ void __launch_bounds__(kStoreThreads, 3) paged8_store_kernel(const __grid_constant__ Store8Params p) {
+    constexpr int kLanes = D / E, kRows = kStoreThreads / kLanes, kPasses = kRows < 2 * kWindow8 ? 2 * kWindow8 / kRows : 1;
     const Store8Args& a = p.a;
+    // of the block that token i of the window begins: the bits of the largest magnitude and its places
+    __shared__ uint32_t run_top[kWindow8], run_places[kWindow8];
     const int tid = threadIdx.x, row = tid / kLanes, u = tid % kLanes;
+    if (tid < kWindow8) run_top[tid] = run_places[tid] = 0;
     ptx::griddep_launch_dependents();
+    __syncthreads();
     ptx::griddep_wait();
-    const Place8<D, NB> at(u, a.rot_dim);
-
-    // the pairs' turns and axes
-    uint64_t turns[4] = {0, 0, 0, 0};
-    int axis[4] = {0, 0, 0, 0};
-    if (at.turned)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            turns[i] = a.turns[u * 4 + i];
-            if (a.axis_of_pair) axis[i] = min(int(a.axis_of_pair[u * 4 + i]), a.n_axes - 1);
-        }
-    auto angles = [&](int64_t t, float (&c)[4], float (&s)[4]) {
+    const Place8<D, NB, E> at(u, a.rot_dim);
+    auto angles = [&](int64_t t, float (&c)[E / 2], float (&s)[E / 2]) {
         if (!at.turned) return;
+        const int pair = u * (E / 2);
+        if (!a.axis_of_pair) {
+            const int32_t pos = a.positions[t];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) angle_of(a.positions[axis[i] * a.pos_stride + t], turns[i], a.factor, c[i], s[i]);
-    };
-    auto gains = [&](const float* gamma, float (&g)[8]) {
-        if (!gamma) return;
-        *reinterpret_cast<float4*>(g) = *reinterpret_cast<const float4*>(gamma + at.e0);
-        *reinterpret_cast<float4*>(g + 4) = *reinterpret_cast<const float4*>(gamma + at.e1);
-    };
-
-    const int kv_ctas = p.kv_windows * a.n_kv_heads;
-    if (int(blockIdx.x) >= kv_ctas) {
-        // ---------------------------------------------------------------------------- queries
-        const int id = int(blockIdx.x) - kv_ctas, group = id % p.head_groups, hw = kRows8 >> p.log_tokens;
-        const int64_t t = (int64_t(id / p.head_groups) << p.log_tokens) + (row & ((1 << p.log_tokens) - 1));
-        const int h0 = group * hw * kHeads8 + (row >> p.log_tokens);
-        const bool live = t < a.n_tokens;
-        float x[kHeads8][8];
+            for (int i = 0; i < E / 2; ++i) angle_of(pos, a.turns[pair + i], a.factor, c[i], s[i]);
+        } else {
 #pragma unroll
-        for (int k = 0; k < kHeads8; ++k) {
-            const int h = h0 + k * hw;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[k][e] = 0.0f;
-            if (live && h < a.n_heads) {
-                const uint16_t* q = a.q + t * a.q_stride + h * D;
-                load4(q + at.e0, x[k]);
-                load4(q + at.e1, x[k] + 4);
-            }
+            for (int i = 0; i < E / 2; ++i)
+                angle_of(a.positions[min(int(a.axis_of_pair[pair + i]), a.n_axes - 1) * a.pos_stride + t], a.turns[pair + i], a.factor, c[i], s[i]);
         }
-        float c[4], s[4], g[8];
-        if (live) angles(t, c, s);
-        gains(a.q_gamma, g);
+    };
+    const unsigned all = 0xffffffffu;
+
+    if (int(blockIdx.x) >= p.kv_ctas) {
+        // ---------------------------------------------------------------------------- queries, two heads at a time
+        const int id = int(blockIdx.x) - p.kv_ctas, group = id % p.head_groups, hw = kRows >> p.log_tokens;
+        const int64_t t = (int64_t(id / p.head_groups) << p.log_tokens) + (row & ((1 << p.log_tokens) - 1));
+        const bool live = t < a.n_tokens;
+        int h = group * hw * 2 * p.rounds + (row >> p.log_tokens);
+        const uint16_t* q = a.q + t * a.q_stride;
+        uint16_t* out = a.q_out + t * a.n_heads * D;
+        float c[E / 2], s[E / 2];
+        for (int r = 0; r < p.rounds; ++r, h += 2 * hw) {
+            const bool in[2] = {live && h < a.n_heads, live && h + hw < a.n_heads};
+            float x[2][E];
 #pragma unroll
-        for (int k = 0; k < kHeads8; ++k) {
-            const int h = h0 + k * hw;
-            norm_turn<D, NB>(x[k], a.q_gamma != nullptr, g, a.eps, at.turned, c, s);
-            if (live && h < a.n_heads) {
-                uint16_t* o = a.q_out + (t * a.n_heads + h) * D;
-                *reinterpret_cast<uint2*>(o + at.e0) = make_uint2(pack_bf16x2(x[k][0], x[k][1]), pack_bf16x2(x[k][2], x[k][3]));
-                *reinterpret_cast<uint2*>(o + at.e1) = make_uint2(pack_bf16x2(x[k][4], x[k][5]), pack_bf16x2(x[k][6], x[k][7]));
+            for (int k = 0; k < 2; ++k) {
+                if (in[k]) {
+                    load_row<E / 2>(q + (h + k * hw) * D + at.e0, x[k]);
+                    load_row<E / 2>(q + (h + k * hw) * D + at.e1, x[k] + E / 2);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) x[k][e] = 0.0f;
+                }
+            }
+            if (r == 0 && live) angles(t, c, s);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                norm_turn<D, NB, E>(x[k], a.q_gamma, a.eps, at, c, s);
+                if (in[k]) {
+                    store_row<E / 2>(out + (h + k * hw) * D + at.e0, x[k]);
+                    store_row<E / 2>(out + (h + k * hw) * D + at.e1, x[k] + E / 2);
+                }
             }
         }
         return;
     }
 
-    // ------------------------------------------------------------------------- keys and values
-    __shared__ int64_t slot_of[32];
-    __shared__ float top[2][32];          // of a token's key and value row
-    __shared__ int exp_of[2][kRows8];     // of the run that token i of the window begins: its block's exponents,
-    __shared__ int exp_was[2][kRows8];    // what they were,
-    __shared__ uint32_t written[kRows8];  // and its places
-    const int g = int(blockIdx.x) % a.n_kv_heads, Hk = a.n_kv_heads;
-    const int64_t t0 = int64_t(int(blockIdx.x) / a.n_kv_heads) * kRows8;
-    // Tokens t0 .. t0 + 31, a lane each in every warp: which share a block. A run, the tokens of a block, is this CTA's if the
-    // first of them is in its window and none is in the window before.
-    const int lane = tid & 31;
+    // ------------------------------------------------------------------------- keys or values
+    const int Hk = a.n_kv_heads, lane = tid & 31;
+    const bool is_k = int(blockIdx.x) % 2 == 0;
+    const int g = int(blockIdx.x) / 2 % Hk;
+    const int64_t t0 = int64_t(int(blockIdx.x) / 2 / Hk) * kWindow8;
+    uint8_t* codes = is_k ? a.k_codes : a.v_codes;
+    uint8_t* exps = is_k ? a.k_exp : a.v_exp;
+    // Tokens t0 .. t0 + 31, a lane each. The first token of a token's block is the furthest of those up to 15 before it that share
+    // the block; the block is this CTA's if that lies in the window. (By comparisons: matching 64-bit numbers over a
+    // warp takes 2 us where each token has a block of its own.)
+    __shared__ int64_t block_of[kStoreThreads / 32][3 * kWindow8];  // a warp's copy: of tokens t0 - 16 .. t0 + 31
     auto slot_at = [&](int64_t t) {
         const int64_t s = t >= 0 && t < a.n_tokens ? a.slots[t] : -1;
         return s >= 0 && s < a.n_slots ? s : int64_t(-1);
     };
-    auto block_of = [&](int64_t s) { return s >= 0 ? s / kBlock8 : -1 - int64_t(lane); };  // (no slot: a block by itself)
-    const int64_t mine = slot_at(t0 + lane), shifted = slot_at(t0 - kRows8 + lane);
-    const uint32_t members = __match_any_sync(0xffffffffu, block_of(mine));
-    const uint32_t around = __match_any_sync(0xffffffffu, block_of(shifted));  // of tokens t0 - 16 .. t0 + 15
-    const bool older = __shfl_sync(0xffffffffu, int((around & 0xFFFFu) != 0), (lane & 15) + 16) != 0;  // of token lane % 16
-    const int head = __ffs(members) - 1;
-    const uint32_t begun = __ballot_sync(0xffffffffu, mine >= 0 && head == lane && lane < kRows8 && !older);
+    const int64_t mine = slot_at(t0 + lane), before = lane < kWindow8 ? slot_at(t0 - kWindow8 + lane) : -1;
+    const int64_t block = mine >= 0 ? mine / kBlock8 : -1;
+    int64_t* blocks = block_of[tid / 32] + kWindow8;
+    blocks[lane] = block;
+    if (lane < kWindow8) blocks[lane - kWindow8] = before >= 0 ? before / kBlock8 : -1;
+    __syncwarp();
+    int head = lane;
+#pragma unroll
+    for (int d = 1; d < kBlock8; ++d)
+        if (blocks[lane - d] == block) head = lane - d;
+    const uint32_t begun = __ballot_sync(all, mine >= 0 && head == lane && lane < kWindow8);
     if (begun == 0) return;  // (the CTA as a whole)
-    if (tid < 32) slot_of[lane] = mine;
-    // the run that token j belongs to, by its first token, or -1: no slot, or not this CTA's
-    const int own_run = mine >= 0 && (begun >> head & 1u) ? head : -1;
+    const bool own = mine >= 0 && head >= 0 && head < kWindow8;
+    const int64_t exp_at = block * Hk + g;
+    const int was = own ? exp_of_byte(exps[exp_at]) : 0;
+    const uint32_t owned = __ballot_sync(all, own);
+    if (tid < 32 && own) atomicOr(&run_places[head], 1u << (mine & (kBlock8 - 1)));
 
-    // this thread's rows: tokens `row` and `row + 16` of the window
-    float x[2][2][8];  // [key, value][token]
-    int run[2];
+    // this thread's rows: tokens `row` of each pass; a warp's rows of a pass that are none of the CTA's are left out together
+    auto token = [&](int i) { return row + i * kRows; };
+    auto is_own = [&](int i) { return token(i) < 2 * kWindow8 && (owned >> token(i) & 1u) != 0; };
+    auto any_own = [&](int i) { return __any_sync(all, is_own(i)); };
+    float x[kPasses][E];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        run[i] = __shfl_sync(0xffffffffu, own_run, row + i * kRows8);
-        const int64_t t = t0 + row + i * kRows8;
-        if (run[i] < 0) {
+    for (int i = 0; i < kPasses; ++i) {
+        const uint16_t* from = (is_k ? a.k + (t0 + token(i)) * a.k_stride : a.v + (t0 + token(i)) * a.v_stride) + g * D;
+        if (is_own(i)) {
+            load_row<E / 2>(from + at.e0, x[i]);
+            load_row<E / 2>(from + at.e1, x[i] + E / 2);
+        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[0][i][e] = x[1][i][e] = 0.0f;
-            continue;
+            for (int e = 0; e < E; ++e) x[i][e] = 0.0f;
         }
-        const uint16_t* k = a.k + t * a.k_stride + g * D;
-        const uint16_t* v = a.v + t * a.v_stride + g * D;
-        load4(k + at.e0, x[0][i]);
-        load4(k + at.e1, x[0][i] + 4);
-        load4(v + at.e0, x[1][i]);
-        load4(v + at.e1, x[1][i] + 4);
     }
-    // the exponents before, of the runs that begin here
-    int was[2] = {0, 0};
-    if (tid < 32 && (begun >> lane & 1u)) {
-        const int64_t at8 = (mine / kBlock8) * Hk + g;
-        was[0] = exp_of_byte(a.k_exp[at8]);
-        was[1] = exp_of_byte(a.v_exp[at8]);
-    }
-    float gk[8];
-    gains(a.k_gamma, gk);
     const float limit = kCodeMost * pow2i(kExpMost);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        float c[4], s[4];
-        if (run[i] >= 0) angles(t0 + row + i * kRows8, c, s);
-        norm_turn<D, NB>(x[0][i], a.k_gamma != nullptr, gk, a.eps, at.turned, c, s);
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-            float m = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = fabsf(x[kv][i][e]);
-                m = v <= limit ? fmaxf(m, v) : m;
-            }
-#pragma unroll
-            for (int o = kLanes / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-            if (u == 0) top[kv][row + i * kRows8] = m;
+    for (int i = 0; i < kPasses; ++i) {
+        if (!any_own(i)) continue;
+        if (is_k) {
+            float c[E / 2], s[E / 2];
+            if (is_own(i)) angles(t0 + token(i), c, s);
+            norm_turn<D, NB, E>(x[i], a.k_gamma, a.eps, at, c, s);
         }
+        float m = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float v = fabsf(x[i][e]);
+            m = v <= limit ? fmaxf(m, v) : m;
+        }
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(all, m, o));
+        const int h = __shfl_sync(all, head, token(i) & 31);
+        if (u == 0 && is_own(i)) atomicMax(&run_top[h], __float_as_uint(m));  // (magnitudes compare as their bits do)
     }
     __syncthreads();
-    if (tid < 32 && (begun >> lane & 1u)) {
-        const int64_t at8 = (mine / kBlock8) * Hk + g;
-        uint32_t places = 0;
-        for (uint32_t m = members; m != 0; m &= m - 1) places |= 1u << (slot_of[__ffs(m) - 1] & (kBlock8 - 1));
-        written[lane] = places;
+    // the blocks' exponents, in the lanes of their tokens
+    const uint32_t bits = own ? run_top[head] : 0, places = own ? run_places[head] : 0;
+    // 448 = 1.75 * 2^8: the least e with the maximum <= 448 * 2^e by its exponent and mantissa
+    const int need = int(bits >> 23) - 127 - 8 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    const int now = max(places & 1u ? -kExpMost : was, min(max(need, -kExpMost), kExpMost));
+    if (tid < 32 && (begun >> lane & 1u)) exps[exp_at] = uint8_t(now + kExpBias);
+    __syncwarp();
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-            float m = 0.0f;
-            for (uint32_t left = members; left != 0; left &= left - 1) m = fmaxf(m, top[kv][__ffs(left) - 1]);
-            // 448 = 1.75 * 2^8: the least e with m <= 448 * 2^e by m's exponent and mantissa
-            const uint32_t bits = __float_as_uint(m);
-            const int need = int(bits >> 23) - 127 - 8 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-            const int e = max(places & 1u ? -kExpMost : was[kv], min(max(need, -kExpMost), kExpMost));
-            exp_of[kv][lane] = e;
-            exp_was[kv][lane] = was[kv];
-            (kv ? a.v_exp : a.k_exp)[at8] = uint8_t(e + kExpBias);
+    for (int i = 0; i < kPasses; ++i) {
+        if (!any_own(i)) continue;
+        const float unit = pow2i(-__shfl_sync(all, now, token(i) & 31));
+        const int64_t slot = __shfl_sync(all, mine, token(i) & 31);
+        if (!is_own(i)) continue;
+        uint32_t w[E / 4];
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+            w[e / 4] = codes_of(x[i][e] * unit, x[i][e + 1] * unit) | codes_of(x[i][e + 2] * unit, x[i][e + 3] * unit) << 16;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (!(fabsf(x[i][e + k]) <= limit)) w[e / 4] = (w[e / 4] & ~(0xFFu << (8 * k))) | 0x7Fu << (8 * k);
         }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if (run[i] < 0) continue;
-        const int64_t to = (slot_of[row + i * kRows8] * Hk + g) * D;
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-            const float by = pow2i(-exp_of[kv][run[i]]);
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                uint32_t two = codes_of(x[kv][i][e] * by, x[kv][i][e + 1] * by);
-                if (!(fabsf(x[kv][i][e]) <= limit)) two = (two & 0xFF00u) | 0x7Fu;
-                if (!(fabsf(x[kv][i][e + 1]) <= limit)) two = (two & 0xFFu) | 0x7F00u;
-                w[e / 2] = two;
-            }
-            uint8_t* codes = (kv ? a.v_codes : a.k_codes) + to;
-            *reinterpret_cast<uint32_t*>(codes + at.e0) = w[0] | w[1] << 16;
-            *reinterpret_cast<uint32_t*>(codes + at.e1) = w[2] | w[3] << 16;
+        uint8_t* to = codes + (slot * Hk + g) * D;
+        if constexpr (E == 16) {
+            *reinterpret_cast<uint2*>(to + at.e0) = make_uint2(w[0], w[1]);
+            *reinterpret_cast<uint2*>(to + at.e1) = make_uint2(w[2], w[3]);
+        } else {
+            *reinterpret_cast<uint32_t*>(to + at.e0) = w[0];
+            *reinterpret_cast<uint32_t*>(to + at.e1) = w[1];
         }
     }
     // the other places of the blocks: zeros in a block that starts anew, re-encoded where the exponent grew
-    for (uint32_t left = begun; left != 0; left &= left - 1) {
+    __syncwarp();
+    const bool more = (begun >> lane & 1u) && places != 0xFFFFu && ((places & 1u) || now > was);
+    for (uint32_t left = __ballot_sync(all, more); left != 0; left &= left - 1) {
         const int h = __ffs(left) - 1;
-        const int64_t block = slot_of[h] & ~int64_t(kBlock8 - 1);
-        const uint32_t places = written[h];
-        if (places >> row & 1u) continue;
-        const int64_t to = ((block + row) * Hk + g) * D + u * 8;
+        const int64_t first = __shfl_sync(all, block, h) * kBlock8;
+        const uint32_t written = __shfl_sync(all, places, h);
+        const float by = pow2i(max(__shfl_sync(all, was - now, h), -126));  // (of a block that starts anew it is not used)
+        for (int place = row; place < kBlock8; place += kRows) {
+            if (written >> place & 1u) continue;
+            uint2* to = reinterpret_cast<uint2*>(codes + ((first + place) * Hk + g) * D + u * E);
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-            uint2* codes = reinterpret_cast<uint2*>((kv ? a.v_codes : a.k_codes) + to);
-            if (places & 1u) {
-                *codes = make_uint2(0u, 0u);
-            } else if (exp_of[kv][h] > exp_was[kv][h]) {
-                const float by = pow2i(exp_was[kv][h] - exp_of[kv][h]);
-                const uint2 old = *codes;
-                uint32_t w[2] = {old.x, old.y};
+            for (int k = 0; k < E / 8; ++k) {
+                if (written & 1u) {
+                    to[k] = make_uint2(0u, 0u);
+                    continue;
+                }
+                uint32_t w[2] = {to[k].x, to[k].y};
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     uint32_t lo, hi;
@@ -289,7 +311,7 @@ __global__ void __launch_bounds__(kRows8* D / 8) paged8_store_kernel(const __gri
                     const float2 f0 = __half22float2(*reinterpret_cast<__half2*>(&lo)), f1 = __half22float2(*reinterpret_cast<__half2*>(&hi));
                     w[i] = codes_of(f0.x * by, f0.y * by) | codes_of(f1.x * by, f1.y * by) << 16;
                 }
-                *codes = make_uint2(w[0], w[1]);
+                to[k] = make_uint2(w[0], w[1]);
             }
         }
     }
@@ -340,9 +362,9 @@ __global__ void __launch_bounds__(kReadThreads) paged8_read_kernel(const __grid_
     }
 }
 
-template <int D>
+template <int D, int E>
 const void* store_kernel(bool neighbours) {
-    return neighbours ? reinterpret_cast<const void*>(paged8_store_kernel<D, true>) : reinterpret_cast<const void*>(paged8_store_kernel<D, false>);
+    return neighbours ? reinterpret_cast<const void*>(paged8_store_kernel<D, true, E>) : reinterpret_cast<const void*>(paged8_store_kernel<D, false, E>);
 }
 
 }  // namespace
@@ -350,19 +372,24 @@ const void* store_kernel(bool neighbours) {
 cudaError_t launch_paged8_store(const Store8Args& a, cudaStream_t s) {
     Store8Params p;
     p.a = a;
-    p.kv_windows = int((a.n_tokens + kRows8 - 1) / kRows8);
-    // a thread takes up to four heads of its token; few tokens leave rows for more heads at once
+    const int each = a.rot_dim % 16 == 0 ? 16 : 8, rows = kStoreThreads / (a.head_dim / each);
+    const int64_t kv_ctas = (a.n_tokens + kWindow8 - 1) / kWindow8 * a.n_kv_heads * 2, sms = std::max(1, device_sm_count());
+    // A thread takes up to eight heads of its token, so that its angles serve them all: fewer where that leaves SMs without work;
+    // few tokens leave rows for more heads at once.
     p.log_tokens = 0;
-    while (p.log_tokens < 4 && (int64_t(1) << p.log_tokens) < a.n_tokens) ++p.log_tokens;
-    const int heads = (kRows8 >> p.log_tokens) * kHeads8;
-    p.head_groups = (a.n_heads + heads - 1) / heads;
-    const int64_t q_ctas = ((a.n_tokens - 1) >> p.log_tokens) * p.head_groups + p.head_groups;
-    const int64_t grid = q_ctas + int64_t(p.kv_windows) * a.n_kv_heads;
-    if (grid > 2147483647) return cudaErrorInvalidValue;
-    p.q_ctas = int(q_ctas);
+    while ((2 << p.log_tokens) <= std::min(rows, 16) && (int64_t(1) << p.log_tokens) < a.n_tokens) ++p.log_tokens;
+    const int64_t tokens = ((a.n_tokens - 1) >> p.log_tokens) + 1, pairs = 2 * (rows >> p.log_tokens);
+    p.rounds = int(std::min<int64_t>(kMostRounds, (a.n_heads + pairs - 1) / pairs));
+    while (p.rounds > 1 && tokens * ((a.n_heads + pairs * p.rounds - 1) / (pairs * p.rounds)) < 3 * sms) --p.rounds;
+    p.head_groups = int((a.n_heads + pairs * p.rounds - 1) / (pairs * p.rounds));
+    const int64_t q_ctas = tokens * p.head_groups;
+    if (q_ctas + kv_ctas > 2147483647) return cudaErrorInvalidValue;
+    p.kv_ctas = int(kv_ctas);
     void* args[] = {&p};
-    const void* fn = a.head_dim == 64 ? store_kernel<64>(a.neighbours) : a.head_dim == 128 ? store_kernel<128>(a.neighbours) : store_kernel<256>(a.neighbours);
-    return launch_serialised(fn, unsigned(grid), unsigned(kRows8 * a.head_dim / 8), 0, s, args);
+    const bool nb = a.neighbours;
+    const void* fn = each == 16 ? (a.head_dim == 64 ? store_kernel<64, 16>(nb) : a.head_dim == 128 ? store_kernel<128, 16>(nb) : store_kernel<256, 16>(nb))
+                                : (a.head_dim == 64 ? store_kernel<64, 8>(nb) : a.head_dim == 128 ? store_kernel<128, 8>(nb) : store_kernel<256, 8>(nb));
+    return launch_serialised(fn, unsigned(q_ctas + kv_ctas), kStoreThreads, 0, s, args);
 }
 
 cudaError_t launch_paged8_read(const Read8Args& a, cudaStream_t s) {

@@ -321,7 +321,7 @@ emb_status emb_paged8_store(const uint16_t* q, int64_t q_stride, const uint16_t*
     if (q_stride >= k46 / n_tokens || k_stride >= k46 / n_tokens || v_stride >= k46 / n_tokens || n_pages * page_size >= k46 / kw)
         return EMB_EINVAL;
     // (its CTAs stay within a launch's grid)
-    if (n_tokens * (n_heads + n_kv_heads) >= (int64_t(1) << 34)) return EMB_EUNSUPPORTED;
+    if (n_tokens * (n_heads + n_kv_heads) >= (int64_t(1) << 33)) return EMB_EUNSUPPORTED;
     if (!q || !k || !v || !positions || (rot_dim > 0 && !turns) || !slots || !q_out || !k_codes || !v_codes || !k_exp || !v_exp)
         return EMB_EINVAL;
     const void* rows[] = {q, k, v, q_gamma, k_gamma, q_out, k_codes, v_codes};
