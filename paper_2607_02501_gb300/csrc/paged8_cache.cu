@@ -20,12 +20,12 @@ namespace {
 // the blocks of all 32 tokens by itself, a lane a token, so there is one barrier.
 constexpr int kStoreThreads = 256;
 constexpr int kWindow8 = 16;  // tokens
-constexpr int kMostRounds = 4;  // pairs of heads that a thread takes of its token, at most
+constexpr int kMostRounds = 8;  // heads that a thread takes of its token, at most
 
 struct Store8Params {
     Store8Args a;
     int kv_ctas;                         // the first CTAs: keys and values
-    int log_tokens, rounds, head_groups; // queries: a CTA's tokens 2^n, a thread's pairs of heads, CTAs to share a token's heads
+    int log_tokens, rounds, head_groups; // queries: a CTA's tokens 2^n, a thread's heads, CTAs to share a token's heads
 };
 
 // Cosine and sine of `factor` times a pair's angle. The product of position and turns wraps at 2^64, one turn, so the
@@ -61,16 +61,21 @@ struct Place8 {
 
 // N bf16 numbers (4 or 8, aligned to their size) from and to memory.
 template <int N>
-__device__ __forceinline__ void load_row(const uint16_t* p, float* x) {
+struct alignas(2 * N) RawRow {
     uint32_t w[N / 2];
-    if constexpr (N == 8) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(p);
-    else *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(p);
+};
+template <int N>
+__device__ __forceinline__ void unpack_row(const RawRow<N>& r, float* x) {
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) {
-        const float2 u = unpack_bf16x2(w[i]);
+        const float2 u = unpack_bf16x2(r.w[i]);
         x[2 * i] = u.x;
         x[2 * i + 1] = u.y;
     }
+}
+template <int N>
+__device__ __forceinline__ void load_row(const uint16_t* p, float* x) {
+    unpack_row<N>(*reinterpret_cast<const RawRow<N>*>(p), x);
 }
 template <int N>
 __device__ __forceinline__ void store_row(uint16_t* p, const float* x) {
@@ -152,34 +157,36 @@ __global__ void __launch_bounds__(kStoreThreads, 3) paged8_store_kernel(const __
     const unsigned all = 0xffffffffu;
 
     if (int(blockIdx.x) >= p.kv_ctas) {
-        // ---------------------------------------------------------------------------- queries, two heads at a time
+        // -------------------------------------------------- queries: head after head of a token, the next two on their way
         const int id = int(blockIdx.x) - p.kv_ctas, group = id % p.head_groups, hw = kRows >> p.log_tokens;
         const int64_t t = (int64_t(id / p.head_groups) << p.log_tokens) + (row & ((1 << p.log_tokens) - 1));
-        const bool live = t < a.n_tokens;
-        int h = group * hw * 2 * p.rounds + (row >> p.log_tokens);
+        const int h0 = group * hw * p.rounds + (row >> p.log_tokens), h_end = t < a.n_tokens ? min(a.n_heads, h0 + hw * p.rounds) : 0;
         const uint16_t* q = a.q + t * a.q_stride;
         uint16_t* out = a.q_out + t * a.n_heads * D;
-        float c[E / 2], s[E / 2];
-        for (int r = 0; r < p.rounds; ++r, h += 2 * hw) {
-            const bool in[2] = {live && h < a.n_heads, live && h + hw < a.n_heads};
-            float x[2][E];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                if (in[k]) {
-                    load_row<E / 2>(q + (h + k * hw) * D + at.e0, x[k]);
-                    load_row<E / 2>(q + (h + k * hw) * D + at.e1, x[k] + E / 2);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) x[k][e] = 0.0f;
-                }
+        RawRow<E / 2> raw[2][2];
+        auto fetch = [&](int h, RawRow<E / 2> (&to)[2]) {
+            if (h < h_end) {
+                to[0] = *reinterpret_cast<const RawRow<E / 2>*>(q + h * D + at.e0);
+                to[1] = *reinterpret_cast<const RawRow<E / 2>*>(q + h * D + at.e1);
             }
-            if (r == 0 && live) angles(t, c, s);
+        };
+        raw[0][0] = raw[0][1] = raw[1][0] = raw[1][1] = RawRow<E / 2>{};
+        fetch(h0, raw[0]);
+        fetch(h0 + hw, raw[1]);
+        float c[E / 2], s[E / 2];
+        if (h_end > 0) angles(t, c, s);
+        for (int r = 0; r < p.rounds; r += 2) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                norm_turn<D, NB, E>(x[k], a.q_gamma, a.eps, at, c, s);
-                if (in[k]) {
-                    store_row<E / 2>(out + (h + k * hw) * D + at.e0, x[k]);
-                    store_row<E / 2>(out + (h + k * hw) * D + at.e1, x[k] + E / 2);
+                const int h = h0 + (r + k) * hw;
+                float x[E];
+                unpack_row<E / 2>(raw[k][0], x);
+                unpack_row<E / 2>(raw[k][1], x + E / 2);
+                fetch(h + 2 * hw, raw[k]);
+                norm_turn<D, NB, E>(x, a.q_gamma, a.eps, at, c, s);
+                if (h < h_end) {
+                    store_row<E / 2>(out + h * D + at.e0, x);
+                    store_row<E / 2>(out + h * D + at.e1, x + E / 2);
                 }
             }
         }
@@ -320,7 +327,6 @@ __global__ void __launch_bounds__(kStoreThreads, 3) paged8_store_kernel(const __
 // ------------------------------------------------------------------ rows of the cache as bf16
 // HBM bounds it. A thread takes 16 codes of a key row and of a value row: 32 bytes in, 64 out.
 constexpr int kReadThreads = 256;
-constexpr int kReadChunks = 1024;  // of 16 codes of a CTA, about
 
 __device__ __forceinline__ void read16(const uint8_t* codes, const uint8_t* exp, int64_t slot, int Hk, int c, int log_d, uint4 (&out)[2]) {
     const int g = (c * 16) >> log_d;
@@ -338,23 +344,24 @@ __device__ __forceinline__ void read16(const uint8_t* codes, const uint8_t* exp,
     }
 }
 
-__global__ void __launch_bounds__(kReadThreads) paged8_read_kernel(const __grid_constant__ Read8Args p, int rows, int log_d) {
+__global__ void __launch_bounds__(kReadThreads) paged8_read_kernel(const __grid_constant__ Read8Args p, int rounds, int log_d) {
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
     const int Hk = p.n_kv_heads, per = (Hk << log_d) / 16;  // chunks of a row
-    const int64_t r0 = int64_t(blockIdx.x) * rows;
-    const int n = int(min(int64_t(rows), p.n_rows - r0)) * per;
-    for (int e = threadIdx.x; e < n; e += kReadThreads) {
-        const int r = e / per, c = e - r * per;
+    const int64_t chunks = p.n_rows * per, c0 = int64_t(blockIdx.x) * (kReadThreads * rounds);
+    // (a CTA's first row by a division of 64 bits, the rest by ones of 32)
+    const int64_t r0 = c0 / per;
+    const int first = int(c0 - r0 * per), n = int(min(int64_t(kReadThreads * rounds), chunks - c0));
+    for (int i = threadIdx.x; i < n; i += kReadThreads) {
+        const int r = (first + i) / per, c = first + i - r * per;
         const int64_t slot = p.slots[r0 + r];
         uint4 k[2] = {}, v[2] = {};
         if (slot >= 0 && slot < p.n_slots) {
             read16(p.k_codes, p.k_exp, slot, Hk, c, log_d, k);
             read16(p.v_codes, p.v_exp, slot, Hk, c, log_d, v);
         }
-        const int64_t to = (r0 + r) * per + c;
-        uint4* ko = reinterpret_cast<uint4*>(p.k_out) + 2 * to;
-        uint4* vo = reinterpret_cast<uint4*>(p.v_out) + 2 * to;
+        uint4* ko = reinterpret_cast<uint4*>(p.k_out) + 2 * (c0 + i);
+        uint4* vo = reinterpret_cast<uint4*>(p.v_out) + 2 * (c0 + i);
         ko[0] = k[0];
         ko[1] = k[1];
         vo[0] = v[0];
@@ -378,10 +385,11 @@ cudaError_t launch_paged8_store(const Store8Args& a, cudaStream_t s) {
     // few tokens leave rows for more heads at once.
     p.log_tokens = 0;
     while ((2 << p.log_tokens) <= std::min(rows, 16) && (int64_t(1) << p.log_tokens) < a.n_tokens) ++p.log_tokens;
-    const int64_t tokens = ((a.n_tokens - 1) >> p.log_tokens) + 1, pairs = 2 * (rows >> p.log_tokens);
-    p.rounds = int(std::min<int64_t>(kMostRounds, (a.n_heads + pairs - 1) / pairs));
-    while (p.rounds > 1 && tokens * ((a.n_heads + pairs * p.rounds - 1) / (pairs * p.rounds)) < 3 * sms) --p.rounds;
-    p.head_groups = int((a.n_heads + pairs * p.rounds - 1) / (pairs * p.rounds));
+    const int64_t tokens = ((a.n_tokens - 1) >> p.log_tokens) + 1, side = rows >> p.log_tokens;  // heads side by side
+    auto groups = [&](int64_t rounds) { return (a.n_heads + side * rounds - 1) / (side * rounds); };
+    p.rounds = int(std::min<int64_t>(kMostRounds, (a.n_heads + side - 1) / side));
+    while (p.rounds > 2 && tokens * groups(p.rounds) < 6 * sms) p.rounds = (p.rounds + 1) / 2;
+    p.head_groups = int(groups(p.rounds));
     const int64_t q_ctas = tokens * p.head_groups;
     if (q_ctas + kv_ctas > 2147483647) return cudaErrorInvalidValue;
     p.kv_ctas = int(kv_ctas);
@@ -396,10 +404,12 @@ cudaError_t launch_paged8_read(const Read8Args& a, cudaStream_t s) {
     Read8Args p = a;
     int log_d = 0;
     while ((1 << log_d) < a.head_dim) ++log_d;
-    const int per = a.n_kv_heads * a.head_dim / 16;
-    int rows = std::max(1, kReadChunks / per);
-    const int64_t grid = (a.n_rows + rows - 1) / rows;
-    void* args[] = {&p, &rows, &log_d};
+    const int64_t chunks = a.n_rows * (int64_t(a.n_kv_heads) * a.head_dim / 16);
+    // several rounds where that leaves every SM its eight CTAs (25 MB 7 us, with four rounds 13; 830 MB 134 and 129)
+    int rounds = chunks >= int64_t(kReadThreads) * 4 * 8 * std::max(1, device_sm_count()) ? 4 : 1;
+    const int64_t each = int64_t(kReadThreads) * rounds, grid = (chunks + each - 1) / each;
+    if (grid > 2147483647) return cudaErrorInvalidValue;
+    void* args[] = {&p, &rounds, &log_d};
     return launch_serialised(reinterpret_cast<const void*>(paged8_read_kernel), unsigned(grid), kReadThreads, 0, s, args);
 }
 

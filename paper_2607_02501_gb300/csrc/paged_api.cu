@@ -376,6 +376,7 @@ emb_status emb_paged8_read(const uint8_t* k_codes, const uint8_t* v_codes, const
     if (!cache8_supported(head_dim, page_size)) return EMB_EUNSUPPORTED;
     const int64_t kw = n_kv_heads * head_dim;
     if (n_pages * page_size >= k46 / kw || n_rows >= k46 / kw) return EMB_EINVAL;
+    if (n_rows * kw >= int64_t(1) << 42) return EMB_EUNSUPPORTED;  // (its CTAs stay within a launch's grid)
     if (!k_codes || !v_codes || !k_exp || !v_exp || (n_rows > 0 && (!slots || !k_out || !v_out))) return EMB_EINVAL;
     const void* rows[] = {k_codes, v_codes, k_out, v_out};
     for (const void* w : rows)

@@ -24,6 +24,36 @@ decltype(&emb_paged8_read) f_read8;
 decltype(&emb_paged8_attention) f_attention8;
 PyObject *s_data_ptr, *s_shape, *s_stride, *s_nbytes, *s_itemsize, *s_is_contiguous;
 
+// An attribute, or a method without arguments, of a tensor: found in its type once, for the type that came first (torch.Tensor), and
+// then without a lookup by name. Objects of other types are asked by name.
+struct Ask {
+    PyObject** name;
+    bool method;
+    PyObject* found = nullptr;  // descriptor of the type `of`
+    PyTypeObject* of = nullptr;
+    Ask(PyObject** n, bool m) : name(n), method(m) {}
+    PyObject* operator()(PyObject* o) {
+        if (!of) {
+            PyObject* d = PyObject_GetAttr(reinterpret_cast<PyObject*>(Py_TYPE(o)), *name);
+            if (!d) PyErr_Clear();
+            const bool fits = d && PyObject_TypeCheck(d, method ? &PyMethodDescr_Type : &PyGetSetDescr_Type) &&
+                              PyType_IsSubtype(Py_TYPE(o), reinterpret_cast<PyDescrObject*>(d)->d_type);
+            if (fits) {
+                found = d;
+                of = reinterpret_cast<PyTypeObject*>(Py_NewRef(reinterpret_cast<PyObject*>(Py_TYPE(o))));
+            } else {
+                Py_XDECREF(d);
+            }
+        }
+        if (Py_TYPE(o) != of) return method ? PyObject_CallMethodNoArgs(o, *name) : PyObject_GetAttr(o, *name);
+        if (method) return PyObject_Vectorcall(found, &o, 1, nullptr);
+        const PyGetSetDef* d = reinterpret_cast<PyGetSetDescrObject*>(found)->d_getset;
+        return d->get(o, d->closure);
+    }
+};
+Ask ask_data_ptr(&s_data_ptr, true), ask_stride(&s_stride, true), ask_is_contiguous(&s_is_contiguous, true);
+Ask ask_shape(&s_shape, false), ask_nbytes(&s_nbytes, false), ask_itemsize(&s_itemsize, false);
+
 // Reads arguments one after another; `ok` turns false, with a Python exception set, at the first that cannot be read.
 struct Reader {
     bool ok = true;
@@ -42,7 +72,7 @@ struct Reader {
     }
     void* address(PyObject* o) {  // of a tensor; of an integer, itself; NULL for None
         if (!ok || o == Py_None) return nullptr;
-        PyObject* v = PyLong_Check(o) ? Py_NewRef(o) : PyObject_CallMethodNoArgs(o, s_data_ptr);
+        PyObject* v = PyLong_Check(o) ? Py_NewRef(o) : ask_data_ptr(o);
         void* p = v ? PyLong_AsVoidPtr(v) : nullptr;
         Py_XDECREF(v);
         if (PyErr_Occurred()) ok = false;
@@ -51,7 +81,7 @@ struct Reader {
     // The sizes of a tensor of `n` dimensions.
     void sizes(PyObject* o, int n, int64_t* out) {
         if (!ok) return;
-        PyObject* v = PyObject_GetAttr(o, s_shape);
+        PyObject* v = ask_shape(o);
         if (!v || !PyTuple_Check(v) || PyTuple_GET_SIZE(v) != n) {
             if (!PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "a tensor of %d dimensions is expected", n);
             ok = false;
@@ -63,7 +93,7 @@ struct Reader {
     // Elements between the rows of a tensor of two dimensions; those of a row lie side by side.
     int64_t row_stride(PyObject* o, const char* name, int64_t columns) {
         if (!ok) return 0;
-        PyObject* v = PyObject_CallMethodNoArgs(o, s_stride);
+        PyObject* v = ask_stride(o);
         int64_t s[2] = {};
         if (!v || !PyTuple_Check(v) || PyTuple_GET_SIZE(v) != 2) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a tensor of 2 dimensions is expected");
@@ -81,9 +111,9 @@ struct Reader {
     void refuse(const char* format, A... a) {
         if (!why[0]) std::snprintf(why, sizeof(why), format, a...);
     }
-    int64_t attribute(PyObject* o, PyObject* name) {
+    int64_t attribute(PyObject* o, Ask& ask) {
         if (!ok) return 0;
-        PyObject* v = PyObject_GetAttr(o, name);
+        PyObject* v = ask(o);
         const int64_t n = v ? integer(v) : 0;
         if (!v) ok = false;
         Py_XDECREF(v);
@@ -91,7 +121,7 @@ struct Reader {
     }
     void contiguous(PyObject* o, const char* name) {
         if (!ok) return;
-        PyObject* v = PyObject_CallMethodNoArgs(o, s_is_contiguous);
+        PyObject* v = ask_is_contiguous(o);
         if (!v) ok = false;
         if (v == Py_False) refuse("%s is not contiguous", name);
         Py_XDECREF(v);
@@ -99,7 +129,7 @@ struct Reader {
     // The tensor holds `count` elements of `size` bytes, side by side.
     void holds(PyObject* o, const char* name, int64_t count, int64_t size) {
         if (!ok || o == Py_None || PyLong_Check(o)) return;
-        const int64_t bytes = attribute(o, s_nbytes), each = attribute(o, s_itemsize);
+        const int64_t bytes = attribute(o, ask_nbytes), each = attribute(o, ask_itemsize);
         if (!ok) return;
         if (each != size) refuse("%s: elements of %lld bytes, %lld expected", name, static_cast<long long>(each), static_cast<long long>(size));
         else if (bytes / size < count) refuse("%s has %lld elements, %lld needed", name, static_cast<long long>(bytes / size), static_cast<long long>(count));
@@ -108,7 +138,7 @@ struct Reader {
     // Positions of T tokens, [tokens] or [axes][tokens]: their axes and the elements between those. False: an exception is set.
     bool positions(PyObject* o, int64_t T, int64_t& axes, int64_t& pos_stride) {
         if (!ok) return true;
-        PyObject* shape = PyObject_GetAttr(o, s_shape);
+        PyObject* shape = ask_shape(o);
         const bool several = shape && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 2;
         Py_XDECREF(shape);
         if (!shape) return false;
@@ -122,7 +152,7 @@ struct Reader {
         pos_stride = row_stride(o, "positions", T);
         if (axes == 1 && pos_stride < T) pos_stride = T;  // (of one row it says nothing)
         if (at[1] < T) refuse("positions has %lld columns, %lld needed", static_cast<long long>(at[1]), static_cast<long long>(T));
-        if (attribute(o, s_itemsize) != 4) refuse("positions: elements of 4 bytes expected");
+        if (attribute(o, ask_itemsize) != 4) refuse("positions: elements of 4 bytes expected");
         return true;
     }
     // Codes and exponents of an 8-bit cache of the sizes pages, page size, heads, head dim.
@@ -296,7 +326,7 @@ PyObject* store8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* p[14];
     for (int i = 0; i < 14; ++i) p[i] = r.address(a[i]);
     const int64_t qs = r.row_stride(a[0], "q", q[1]), ks = r.row_stride(a[1], "k", k[1]), vs = r.row_stride(a[2], "v", v[1]);
-    if (r.attribute(a[0], s_itemsize) != 2 || r.attribute(a[1], s_itemsize) != 2 || r.attribute(a[2], s_itemsize) != 2)
+    if (r.attribute(a[0], ask_itemsize) != 2 || r.attribute(a[1], ask_itemsize) != 2 || r.attribute(a[2], ask_itemsize) != 2)
         r.refuse("q, k, v: elements of 2 bytes expected");
     if (d > 0 && q[1] % d != 0) r.refuse("q: rows of %lld elements are no whole heads of %lld", static_cast<long long>(q[1]), static_cast<long long>(d));
     if (k[0] < T || k[1] < kw) r.refuse("k: fewer rows than q, or heads than the cache");
