@@ -11,7 +11,10 @@ Each step takes the new tokens of every request (a prompt, a chunk, a decoded to
 on one stream, with no host synchronisation in between; the lengths stay on the device, and a step of fixed
 size (a decode step) can be recorded once and replayed (`record_decode`).
 
-    python examples/paged_serving.py [--steps 8]
+With `bits=8` the cache is held in 8 bits, half the bytes: emb_paged8_store and emb_paged8_attention then take the places of
+emb_qk_norm_rope and emb_paged_attention.
+
+    python examples/paged_serving.py [--steps 8] [--bits 8]
 """
 from __future__ import annotations
 
@@ -34,7 +37,7 @@ class PagedLayer:
     """One layer (width, heads, key/value heads, head dim) with random Q8_0 weights, and the cache and bookkeeping of
     `requests` requests with up to `max_tokens` tokens each."""
 
-    def __init__(self, width=1024, heads=8, kv_heads=1, head_dim=128, requests=4, max_tokens=2048, page=16, seed=0):
+    def __init__(self, width=1024, heads=8, kv_heads=1, head_dim=128, requests=4, max_tokens=2048, page=16, seed=0, bits=16):
         self.width, self.heads, self.kv_heads, self.head_dim, self.requests, self.page = width, heads, kv_heads, head_dim, requests, page
         g = torch.Generator(device="cuda")
         g.manual_seed(seed)
@@ -48,8 +51,13 @@ class PagedLayer:
         self.k_gamma = 1.0 + 0.1 * torch.randn(head_dim, generator=g, **dev)
         pages = -(-max_tokens // page)
         n_pages = requests * pages
-        self.k_cache = torch.zeros(n_pages, page, kv_heads, head_dim, dtype=torch.bfloat16, **dev)
-        self.v_cache = torch.zeros_like(self.k_cache)
+        self.bits = bits
+        if bits == 8:
+            self.cache = emb.paged8_cache(n_pages, page, kv_heads, head_dim)
+            self.turns = emb.emb_rotary_turns(head_dim, BASE).cuda()
+        else:
+            self.k_cache = torch.zeros(n_pages, page, kv_heads, head_dim, dtype=torch.bfloat16, **dev)
+            self.v_cache = torch.zeros_like(self.k_cache)
         self.table = torch.full((requests, pages), -1, dtype=torch.int32, **dev)
         # pages are handed out in an order of their own
         self.free_pages = torch.randperm(n_pages, generator=g, **dev).to(torch.int32)
@@ -79,10 +87,16 @@ class PagedLayer:
                             b["slots"], b["positions"], self.used[1:], self.page, stream=stream)
         emb.emb_rmsnorm(b["x"], self.norm, b["h"], EPS, stream=stream)
         emb.emb_qlayer_seq([(emb.EMB_Q8_0, w[n], *self.shapes[n], b["h"], b[n], emb.EMB_EPI_BF16) for n in "qkv"], T, stream=stream)
-        emb.emb_qk_norm_rope(b["q"], b["k"], b["v"], b["qr"], self.k_cache, self.v_cache, b["slots"], b["positions"],
-                             q_gamma=self.q_gamma, k_gamma=self.k_gamma, eps=EPS, base=BASE, stream=stream)
-        emb.emb_paged_attention(b["qr"], self.k_cache, self.v_cache, self.table, b["q_start"], b["kv_len"], b["a"], d ** -0.5,
-                                max_q, self.workspace, prefix=prefix, cap=cap, window=window, stream=stream)
+        if self.bits == 8:
+            emb.emb_paged8_store(b["q"], b["k"], b["v"], b["qr"], *self.cache, b["slots"], b["positions"], self.turns,
+                                 q_gamma=self.q_gamma, k_gamma=self.k_gamma, eps=EPS, stream=stream)
+            emb.emb_paged8_attention(b["qr"], *self.cache, self.table, b["q_start"], b["kv_len"], b["a"], d ** -0.5, max_q,
+                                     self.workspace, prefix=prefix, cap=cap, window=window, stream=stream)
+        else:
+            emb.emb_qk_norm_rope(b["q"], b["k"], b["v"], b["qr"], self.k_cache, self.v_cache, b["slots"], b["positions"],
+                                 q_gamma=self.q_gamma, k_gamma=self.k_gamma, eps=EPS, base=BASE, stream=stream)
+            emb.emb_paged_attention(b["qr"], self.k_cache, self.v_cache, self.table, b["q_start"], b["kv_len"], b["a"], d ** -0.5,
+                                    max_q, self.workspace, prefix=prefix, cap=cap, window=window, stream=stream)
         emb.emb_qlayer_seq([(emb.EMB_Q8_0, w["o"], *self.shapes["o"], b["a"], b["x"], emb.EMB_EPI_ADD)], T, stream=stream)
 
     def advance(self, b):
@@ -112,8 +126,9 @@ class PagedLayer:
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--steps", type=int, default=8)
-    steps = ap.parse_args().steps
-    layer = PagedLayer(requests=4)
+    ap.add_argument("--bits", type=int, choices=(8, 16), default=16, help="of the cache")
+    args = ap.parse_args()
+    steps, layer = args.steps, PagedLayer(requests=4, bits=args.bits)
     prompts = [816, 50, 300, 7]
     x = torch.randn(sum(prompts), layer.width, device="cuda")
     layer.run(x, prompts)

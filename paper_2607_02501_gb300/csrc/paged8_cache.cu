@@ -130,7 +130,7 @@ __device__ __forceinline__ void norm_turn(float (&x)[E], const float* gamma, flo
 
 // (three CTAs per SM: without the bound two fit, and 15600 tokens of 10 heads of 256 with eight elements a thread took 79 us, so 60)
 template <int D, bool NB, int E>
-__global__ void __launch_bounds__(kStoreThreads, 3) paged8_store_kernel(const __grid_constant__ Store8Params p) {
+__global__ void __launch_bounds__(kStoreThreads, 3) paged_codes_store_kernel(const __grid_constant__ Store8Params p) {
     constexpr int kLanes = D / E, kRows = kStoreThreads / kLanes, kPasses = kRows < 2 * kWindow8 ? 2 * kWindow8 / kRows : 1;
     const Store8Args& a = p.a;
     // of the block that token i of the window begins: the bits of the largest magnitude and its places
@@ -344,7 +344,7 @@ __device__ __forceinline__ void read16(const uint8_t* codes, const uint8_t* exp,
     }
 }
 
-__global__ void __launch_bounds__(kReadThreads) paged8_read_kernel(const __grid_constant__ Read8Args p, int rounds, int log_d) {
+__global__ void __launch_bounds__(kReadThreads) paged_codes_read_kernel(const __grid_constant__ Read8Args p, int rounds, int log_d) {
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
     const int Hk = p.n_kv_heads, per = (Hk << log_d) / 16;  // chunks of a row
@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(kReadThreads) paged8_read_kernel(const __grid_
 
 template <int D, int E>
 const void* store_kernel(bool neighbours) {
-    return neighbours ? reinterpret_cast<const void*>(paged8_store_kernel<D, true, E>) : reinterpret_cast<const void*>(paged8_store_kernel<D, false, E>);
+    return neighbours ? reinterpret_cast<const void*>(paged_codes_store_kernel<D, true, E>) : reinterpret_cast<const void*>(paged_codes_store_kernel<D, false, E>);
 }
 
 }  // namespace
@@ -410,7 +410,7 @@ cudaError_t launch_paged8_read(const Read8Args& a, cudaStream_t s) {
     const int64_t each = int64_t(kReadThreads) * rounds, grid = (chunks + each - 1) / each;
     if (grid > 2147483647) return cudaErrorInvalidValue;
     void* args[] = {&p, &rounds, &log_d};
-    return launch_serialised(reinterpret_cast<const void*>(paged8_read_kernel), unsigned(grid), kReadThreads, 0, s, args);
+    return launch_serialised(reinterpret_cast<const void*>(paged_codes_read_kernel), unsigned(grid), kReadThreads, 0, s, args);
 }
 
 }  // namespace emb

@@ -69,7 +69,7 @@ struct Few8Traits {
 };
 
 template <int D, int CAP, bool CL>
-__global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_kernel(const __grid_constant__ Paged8Params p) {
+__global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged_codes_few_kernel(const __grid_constant__ Paged8Params p) {
     using T = Few8Traits<D>;
     constexpr int KS = D / 16, NT = D / 8, ROWS = kFewRows;
     constexpr bool QS = D == 256;  // queries stay in shared memory: their fragments would not fit the registers
@@ -132,7 +132,8 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged8_few_
             // block's page one round ahead of its exponent, and that a round before it is used. Boxes that no query sees, and
             // pages that do not exist, are fetched from behind the cache: zeros.
             constexpr int kRound = 32 / (2 * kFewBlocks);
-            auto key_of = [&](int j) { return (it.t0 + j + lane / (2 * kFewBlocks)) * kFewTile + (lane & (kFewBlocks - 1)) * kBlock8; };
+            // (unsigned: a few tiles behind the longest request's end it may wrap, and is not used)
+            auto key_of = [&](int j) { return int(uint32_t(it.t0 + j + lane / (2 * kFewBlocks)) * kFewTile + (lane & (kFewBlocks - 1)) * kBlock8); };
             auto page_of = [&](int j) {
                 const int key = key_of(j), key_box = key & ~(box - 1);
                 int page = p.n_pages;
@@ -670,11 +671,11 @@ cudaError_t few8_resident(int& ctas) {
         ctas = known[dev];
         return cudaSuccess;
     }
-    auto* kernel = paged8_few_kernel<D, CAP, false>;
+    auto* kernel = paged_codes_few_kernel<D, CAP, false>;
     int per_sm = 0;
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Few8Traits<D>::kSmem);
     if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(paged8_few_kernel<D, CAP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Few8Traits<D>::kSmemCluster);
+        e = cudaFuncSetAttribute(paged_codes_few_kernel<D, CAP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Few8Traits<D>::kSmemCluster);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kFewThreads, Few8Traits<D>::kSmem);
     if (e != cudaSuccess) return e;
     // a partial result per item border: two per CTA, within the workspace
@@ -715,11 +716,11 @@ cudaError_t launch_few8(Paged8Params& p, const PagedAttnArgs& a, cudaStream_t s)
     p.side = few8_blocks(a);
     p.cluster = few8_cluster(a);
     if (p.cluster > 0)
-        return launch_serialised(reinterpret_cast<const void*>(paged8_few_kernel<D, CAP, true>), unsigned(a.n_req * a.n_kv_heads * p.side * p.cluster),
+        return launch_serialised(reinterpret_cast<const void*>(paged_codes_few_kernel<D, CAP, true>), unsigned(a.n_req * a.n_kv_heads * p.side * p.cluster),
                                  kFewThreads, Few8Traits<D>::kSmemCluster, s, args, unsigned(p.cluster));
     const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, kFewTile))));
     set_grid(p, grid, 2);
-    return launch_serialised(reinterpret_cast<const void*>(paged8_few_kernel<D, CAP, false>), grid, kFewThreads, Few8Traits<D>::kSmem, s, args, 1, true);
+    return launch_serialised(reinterpret_cast<const void*>(paged_codes_few_kernel<D, CAP, false>), grid, kFewThreads, Few8Traits<D>::kSmem, s, args, 1, true);
 }
 
 template <int D>
@@ -741,8 +742,18 @@ cudaError_t launch_paged8_attention(const Paged8AttnArgs& args, cudaStream_t s) 
     static_cast<PagedParams&>(p) = paged_params(a);
     p.k_exp = args.k_exp;
     p.v_exp = args.v_exp;
-    // (the bf16 cache's rule, see launch_paged_attention)
-    const bool few = p.G <= 16 && (a.max_q * p.G <= 16 || few8_cluster(a) > 0);
+    // Rows of a request: up to 16 go to the mma.sync kernel, and more where all its blocks of 16 have a cluster at once. Up to 32 do
+    // too, though their keys come twice: the second time from L2, and every CTA of two takes a stretch of its own (us, mma.sync and
+    // tcgen05: 32 requests of 4 queries of 16 heads on 2 of 128 over 8000 keys 62 and 66, one over 16000 19 and 25, of 64 15 and 23); but
+    // heads of 256, and up to 64 rows, only where the call has few blocks to share out (one request of 8 queries of 16 heads
+    // on 2 over 16000 keys, heads of 64, 128 and 256: 17 and 23, 23 and 25, 27 and 42; 4 requests 23 and 26, 33 and 28, 75 and 54; 24
+    // requests of 4 queries of heads of 256 over 1500 keys 40 and 32). The rest goes to the tcgen05 kernel.
+    bool few = false;
+    if (p.G <= 16) {
+        const int64_t rows = std::min(a.max_q, a.n_tokens) * p.G;
+        const bool fine = double(a.n_req * a.n_kv_heads) * few8_blocks(a) <= 16.0;
+        few = rows <= 16 || few8_cluster(a) > 0 || (rows <= 32 && a.head_dim < 256) || (rows <= 64 && fine);
+    }
     if (!few) {
         p.negate = a.scale < 0.0f;
         p.scale2 = std::max(std::fabs(p.scale2), 1e-37f);  // (hidden scores are the lowest there are times this)

@@ -151,7 +151,7 @@ __device__ __forceinline__ float split_row(uint8_t* tile, int row, bool negate) 
 }
 
 template <int D, int CAP>
-__global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kernel(const __grid_constant__ Paged8Params p) {
+__global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_kernel(const __grid_constant__ Paged8Params p) {
     using T = Many8Traits<D>;
     constexpr int NQ = T::NQ, KT = T::KT, NB = T::NB;
     constexpr int kRows = 128 * NQ;
@@ -252,7 +252,8 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
             // block's page one round ahead of its exponent, and that a round before it is used. Boxes that no query sees, and pages
             // that do not exist, are fetched from behind the cache: zeros.
             constexpr int kRound = 32 / (2 * NB);
-            auto key_of = [&](int j) { return (j + lane / (2 * NB)) * KT + (lane & (NB - 1)) * kBlock8; };
+            // (unsigned: a few tiles behind the longest request's end it may wrap, and is not used)
+            auto key_of = [&](int j) { return int(uint32_t(j + lane / (2 * NB)) * KT + (lane & (NB - 1)) * kBlock8); };
             auto page_of = [&](int j) {
                 const int key = key_of(j), key_box = key & ~(box - 1);
                 int page = p.n_pages;
@@ -427,8 +428,8 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged8_many_kerne
         // a thread's first key and chunk, keys to its next one, steps over the keys (heads of 256: twice)
         constexpr int kStep = D == 64 ? 16 : 8, kSteps = KT / kStep, kEach = KT * D / 16 / 64;
         // Chunks in flight: more of them hold up the softmax, whose accesses stand behind these in the load and store unit (4096 tokens
-        // over 16384 keys: 2 793 us, 4 843, 8 936).
-        constexpr int kBatch = 2;
+        // over 16384 keys: 1 808 us, 2 818, 4 843, 8 936; 816 of two requests with heads of 256: 1 41.3, 2 38.8, 4 41.3).
+        constexpr int kBatch = D == 256 ? 2 : 1;
         const int key_first = (lane & 7) + (D == 64 ? (warp & 1) * 8 : 0), c_first = (D == 64 ? 0 : (warp & 1) * 4) + lane / 8;
         uint32_t n = 0;
         RingPlace<T::kVals> from;
@@ -792,7 +793,7 @@ cudaError_t launch_many8(Paged8Params& p, const PagedAttnArgs& a, cudaStream_t s
     {
         std::lock_guard<std::mutex> lock(mu);
         if (dev < 0 || dev >= 64 || !done[dev]) {
-            e = cudaFuncSetAttribute(paged8_many_kernel<D, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::kSmem);
+            e = cudaFuncSetAttribute(paged_codes_many_kernel<D, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::kSmem);
             if (e != cudaSuccess) return e;
             if (dev >= 0 && dev < 64) done[dev] = true;
         }
@@ -815,7 +816,7 @@ cudaError_t launch_many8(Paged8Params& p, const PagedAttnArgs& a, cudaStream_t s
     void* args[] = {&p};
     const unsigned grid = unsigned(std::max(2.0, std::min(double(ctas), unit_bound(a, p.QB, T::KT))));
     set_grid(p, grid, D == 256 ? 8 : 2);
-    return launch_serialised(reinterpret_cast<const void*>(paged8_many_kernel<D, CAP>), grid, T::kThreads, T::kSmem, s, args, 1, true);
+    return launch_serialised(reinterpret_cast<const void*>(paged_codes_many_kernel<D, CAP>), grid, T::kThreads, T::kSmem, s, args, 1, true);
 }
 
 template <int D>
