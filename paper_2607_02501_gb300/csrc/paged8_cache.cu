@@ -3,6 +3,7 @@
 // Both kernels are launched with programmatic stream serialisation and read device memory only after
 // griddepcontrol.wait, with ordinary loads.
 #include <algorithm>
+#include <type_traits>
 
 #include "paged8.cuh"
 
@@ -28,13 +29,17 @@ struct Store8Params {
     int log_tokens, rounds, head_groups; // queries: a CTA's tokens 2^n, a thread's heads, CTAs to share a token's heads
 };
 
-// Cosine and sine of `factor` times a pair's angle. The product of position and turns wraps at 2^64, one turn, so the
-// angle's fraction is exact; its upper 32 bits go to the hardware's sine and cosine in +-pi (error below 2^-21).
+// Cosine and sine of a pair's angle, times `factor`. The product of position and turns wraps at 2^64, one turn, so the angle's
+// fraction is exact; of its upper 32 bits fp32 keeps 24. Queries, which bf16 rounds, take the hardware's sine and cosine in +-pi
+// (error below 2^-21); keys exact ones: next to a border between two codes an error of fp32's size is an eighth of the value.
+// (15600 tokens of 10 heads of 256: 38.9 us with the hardware's for keys too, 39.4 so.)
+template <bool EXACT>
 __device__ __forceinline__ void angle_of(int32_t at, uint64_t turns, float factor, float& c, float& s) {
     // (the upper half of the product modulo 2^64, from the 32-bit halves)
     const uint32_t lo = uint32_t(turns), hi = uint32_t(turns >> 32), p = uint32_t(at);
-    const uint32_t top = __umulhi(p, lo) + p * hi - (at < 0 ? lo : 0u);
-    __sincosf(float(int32_t(top)) * (6.283185307179586f / 4294967296.0f), &s, &c);
+    const float half_turns = float(int32_t(__umulhi(p, lo) + p * hi - (at < 0 ? lo : 0u))) * (1.0f / 2147483648.0f);
+    if constexpr (EXACT) sincospif(half_turns, &s, &c);
+    else __sincosf(half_turns * 3.1415926535897931f, &s, &c);
     c *= factor;
     s *= factor;
 }
@@ -141,17 +146,18 @@ __global__ void __launch_bounds__(kStoreThreads, 3) paged_codes_store_kernel(con
     __syncthreads();
     ptx::griddep_wait();
     const Place8<D, NB, E> at(u, a.rot_dim);
-    auto angles = [&](int64_t t, float (&c)[E / 2], float (&s)[E / 2]) {
+    auto angles = [&](auto exact, int64_t t, float (&c)[E / 2], float (&s)[E / 2]) {
+        constexpr bool kExact = decltype(exact)::value;
         if (!at.turned) return;
         const int pair = u * (E / 2);
         if (!a.axis_of_pair) {
             const int32_t pos = a.positions[t];
 #pragma unroll
-            for (int i = 0; i < E / 2; ++i) angle_of(pos, a.turns[pair + i], a.factor, c[i], s[i]);
+            for (int i = 0; i < E / 2; ++i) angle_of<kExact>(pos, a.turns[pair + i], a.factor, c[i], s[i]);
         } else {
 #pragma unroll
             for (int i = 0; i < E / 2; ++i)
-                angle_of(a.positions[min(int(a.axis_of_pair[pair + i]), a.n_axes - 1) * a.pos_stride + t], a.turns[pair + i], a.factor, c[i], s[i]);
+                angle_of<kExact>(a.positions[min(int(a.axis_of_pair[pair + i]), a.n_axes - 1) * a.pos_stride + t], a.turns[pair + i], a.factor, c[i], s[i]);
         }
     };
     const unsigned all = 0xffffffffu;
@@ -174,7 +180,7 @@ __global__ void __launch_bounds__(kStoreThreads, 3) paged_codes_store_kernel(con
         fetch(h0, raw[0]);
         fetch(h0 + hw, raw[1]);
         float c[E / 2], s[E / 2];
-        if (h_end > 0) angles(t, c, s);
+        if (h_end > 0) angles(std::false_type{}, t, c, s);
         for (int r = 0; r < p.rounds; r += 2) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -248,7 +254,7 @@ __global__ void __launch_bounds__(kStoreThreads, 3) paged_codes_store_kernel(con
         if (!any_own(i)) continue;
         if (is_k) {
             float c[E / 2], s[E / 2];
-            if (is_own(i)) angles(t0 + token(i), c, s);
+            if (is_own(i)) angles(std::true_type{}, t0 + token(i), c, s);
             norm_turn<D, NB, E>(x[i], a.k_gamma, a.eps, at, c, s);
         }
         float m = 0.0f;

@@ -5,9 +5,9 @@
 // into tensor memory, a warpgroup of softmax per row tile with a thread a row, O += P V with P in the place of its
 // scores. What differs:
 // - Keys stay codes: they are the B operand of kind::f8f6f4 as TMA brings them. A row of queries, times a power of two, is
-//   split into two e4m3 numbers per element, the nearest and the rest, by its softmax thread and in place when the tile has arrived:
-//   8 bits of significand together, as bf16 has, so the split is exact but for elements below 2^-9 of the row's largest
-//   (within 2^-17 of it). Two products at twice the f16 rate cost what one would, the keys need no conversion, and shared
+//   split into two e4m3 numbers per element, the nearest and the rest, by its softmax thread when the tile has arrived: 8 bits
+//   of significand together, as bf16 has, so the split is exact but for elements below 2^-9 of the row's largest (within
+//   2^-17 of it). Two products at twice the f16 rate cost what one would, the keys need no conversion, and shared
 //   memory, whose bandwidth f16 operands of this shape use up, has less to move.
 // - Values become f16 tiles in shared memory by two warps of their own. Weights are f16 (as e4m3, also in two parts, tails of
 //   many small ones would be lost).
@@ -40,6 +40,11 @@ struct Many8Traits {
     static constexpr int kSub = KT * 128;              // bytes of 64 dims of an f16 tile, and of 128 of a code tile
     // columns of tensor memory: scores (two places), outputs
     static constexpr int kO = 2 * KT;
+    // and, where there is room (not with heads of 128), the split queries: as an operand in shared memory they take as much of its
+    // bandwidth as the keys and more (816 tokens of two requests, heads of 256: 38.8 us, so 35.2)
+    static constexpr bool kQTmem = D != 128;
+    static constexpr int kQ = kO + NQ * D, kQCols = D / 2;
+    static_assert(!kQTmem || kQ + NQ * kQCols <= 512, "columns");
     // Byte offset of 16-byte chunk c of row r in a code tile as TMA swizzles it.
     static __device__ __forceinline__ uint32_t place(int r, int c) {
         if constexpr (D == 64) return uint32_t(r * 64 + ((c ^ (r >> 1 & 3)) << 4));
@@ -106,16 +111,16 @@ __device__ __forceinline__ Segment<D> segment_of(const PagedParams& p, int r, in
     return s;
 }
 
-// Row `row` of a tile of bf16 queries (rows of 64 dims, 128 bytes, swizzled), split in place: the nearest codes of 64-dim parts 0 ..
-// D / 128 - 1 in those, the rests' behind them (D = 64: both in the one row). Returns the power that takes the scores back.
+// Row `row` of a tile of bf16 queries (rows of 64 dims, 128 bytes, swizzled): 16-byte chunk c of it, the largest magnitude.
+__device__ __forceinline__ uint4* query_chunk(uint8_t* tile, int row, int c) {
+    return reinterpret_cast<uint4*>(tile + (c >> 3) * 16384 + row * 128 + (((c & 7) ^ (row & 7)) << 4));
+}
 template <int D>
-__device__ __forceinline__ float split_row(uint8_t* tile, int row, bool negate) {
-    constexpr int C = D / 8;  // 16-byte chunks of the row
-    auto chunk = [&](int c) { return reinterpret_cast<uint4*>(tile + (c >> 3) * 16384 + row * 128 + (((c & 7) ^ (row & 7)) << 4)); };
+__device__ __forceinline__ float query_top(uint8_t* tile, int row) {
     float top = 0.0f;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const uint4 w = *chunk(c);
+    for (int c = 0; c < D / 8; ++c) {
+        const uint4 w = *query_chunk(tile, row, c);
         const uint32_t h[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -123,30 +128,52 @@ __device__ __forceinline__ float split_row(uint8_t* tile, int row, bool negate) 
             top = max3(top, fabsf(u.x), fabsf(u.y));
         }
     }
-    const RowPower pr = row_power(top);
-    const float by = pr.to * (negate ? -0.0078125f : 0.0078125f);  // below 2^8
-    // (the nearest codes take the place of what has been read, the rests wait until all has been)
-    uint4 rest[C / 2];
+    return top;
+}
+// Sixteen elements (chunks c and c + 1) times `by` as nearest codes and rests.
+__device__ __forceinline__ void split16(uint8_t* tile, int row, int c, float by, uint32_t* hi, uint32_t* lo) {
+    const uint4 w0 = *query_chunk(tile, row, c), w1 = *query_chunk(tile, row, c + 1);
+    const uint32_t h[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
-    for (int c = 0; c < C; c += 2) {
-        const uint4 w0 = *chunk(c), w1 = *chunk(c + 1);
-        const uint32_t h[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const float2 x = unpack_bf16x2(h[2 * q]), y = unpack_bf16x2(h[2 * q + 1]);
-            const float f[4] = {x.x * by, x.y * by, y.x * by, y.y * by};
-            hi[q] = codes_of(f[0], f[1]) | codes_of(f[2], f[3]) << 16;
-            uint32_t h0, h1;
-            codes_to_f16x4(hi[q], h0, h1);
-            const float2 g0 = __half22float2(*reinterpret_cast<__half2*>(&h0)), g1 = __half22float2(*reinterpret_cast<__half2*>(&h1));
-            lo[q] = codes_of(f[0] - g0.x, f[1] - g0.y) | codes_of(f[2] - g1.x, f[3] - g1.y) << 16;
-        }
-        *chunk(c / 2) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        rest[c / 2] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    for (int q = 0; q < 4; ++q) {
+        const float2 x = unpack_bf16x2(h[2 * q]), y = unpack_bf16x2(h[2 * q + 1]);
+        const float f[4] = {x.x * by, x.y * by, y.x * by, y.y * by};
+        hi[q] = codes_of(f[0], f[1]) | codes_of(f[2], f[3]) << 16;
+        uint32_t h0, h1;
+        codes_to_f16x4(hi[q], h0, h1);
+        const float2 g0 = __half22float2(*reinterpret_cast<__half2*>(&h0)), g1 = __half22float2(*reinterpret_cast<__half2*>(&h1));
+        lo[q] = codes_of(f[0] - g0.x, f[1] - g0.y) | codes_of(f[2] - g1.x, f[3] - g1.y) << 16;
     }
+}
+// Splits a row: into tensor memory from column q_col on (called by whole warps), nearest codes first; or in place, the nearest codes in
+// the first parts of 64 dims, the rests in the others. Returns the power that takes the scores back.
+template <int D, bool TMEM>
+__device__ __forceinline__ float split_row(uint8_t* tile, int row, bool negate, uint32_t q_col) {
+    constexpr int C = D / 8;
+    const RowPower pr = row_power(query_top<D>(tile, row));
+    const float by = pr.to * (negate ? -0.0078125f : 0.0078125f);  // below 2^8
+    if constexpr (TMEM) {
+#pragma unroll 1
+        for (int c = 0; c < C; c += 8) {
+            uint32_t hi[16], lo[16];
 #pragma unroll
-    for (int c = 0; c < C / 2; ++c) *chunk(C / 2 + c) = rest[c];
+            for (int i = 0; i < 4; ++i) split16(tile, row, c + 2 * i, by, hi + 4 * i, lo + 4 * i);
+            ptx::tmem_st_16(q_col + c * 2, hi);
+            ptx::tmem_st_16(q_col + D / 4 + c * 2, lo);
+        }
+        ptx::tmem_st_wait();
+    } else {
+        // (the nearest codes take the place of what has been read, the rests wait until all has been)
+        uint32_t rest[C / 2][4];
+#pragma unroll
+        for (int c = 0; c < C; c += 2) {
+            uint32_t hi[4];
+            split16(tile, row, c, by, hi, rest[c / 2]);
+            *query_chunk(tile, row, c / 2) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        }
+#pragma unroll
+        for (int c = 0; c < C / 2; ++c) *query_chunk(tile, row, C / 2 + c) = make_uint4(rest[c][0], rest[c][1], rest[c][2], rest[c][3]);
+    }
     return pr.back * 128.0f;
 }
 
@@ -186,7 +213,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
         for (int i = 0; i < kScaleTiles; ++i) ptx::mbar_init(&scale_full[i], 1);
         ptx::mbar_init(&q_full, 1);
         ptx::mbar_init(&q_ready, T::kSoftWarps);
-        ptx::mbar_init(&q_empty, 1);
+        ptx::mbar_init(&q_empty, T::kQTmem ? T::kSoftWarps : 1);
         for (int t = 0; t < 2; ++t) {
             ptx::mbar_init(&s_full[t], 1);
             ptx::mbar_init(&p_ready[t], 4);
@@ -336,21 +363,21 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
         bool ok = true, used = false;  // used: a product of the tile's values was issued
         // (operands in a form that the compiler knows to be uniform: see ptx::elect_one)
         auto qk = [&](int t, int place, int slot) {  // S[place] = Q[t] K^T, nearest codes and rests
-            const uint32_t k = ptx::warp_uniform(kring_u + uint32_t(slot * T::kRaw)), q = sq_u + uint32_t(t * T::kQTile);
+            const uint32_t k = ptx::warp_uniform(kring_u + uint32_t(slot * T::kRaw));
+            const uint32_t q = T::kQTmem ? ptx::warp_uniform(tmem + uint32_t(T::kQ + t * T::kQCols)) : sq_u + uint32_t(t * T::kQTile);
             const uint32_t d = ptx::warp_uniform(tmem + uint32_t(place * KT));
 #pragma unroll
             for (int part = 0; part < 2; ++part)
 #pragma unroll
                 for (int ks = 0; ks < D / 32; ++ks) {
-                    uint64_t da, db;
-                    if constexpr (D == 64) {
-                        da = ptx::smem_desc_sw128(q) + 4 * part + 2 * ks;
-                        db = ptx::smem_desc_sw64(k) + 2 * ks;
+                    const uint32_t more = part + ks != 0;
+                    if constexpr (T::kQTmem) {
+                        const uint64_t db = D == 64 ? ptx::smem_desc_sw64(k) + 2 * ks : ptx::smem_desc_sw128(k + (ks / 4) * T::kSub) + 2 * (ks & 3);
+                        ptx::mma_f8_ta(d, q + uint32_t(part * (D / 4) + ks * 8), db, idesc_qk, more);
                     } else {
-                        da = ptx::smem_desc_sw128(q + (part * (D / 128) + ks / 4) * 16384) + 2 * (ks & 3);
-                        db = ptx::smem_desc_sw128(k + (ks / 4) * T::kSub) + 2 * (ks & 3);
+                        ptx::mma_f8_ss(d, ptx::smem_desc_sw128(q + (part * (D / 128) + ks / 4) * 16384) + 2 * (ks & 3),
+                                       ptx::smem_desc_sw128(k + (ks / 4) * T::kSub) + 2 * (ks & 3), idesc_qk, more);
                     }
-                    ptx::mma_f8_ss(d, da, db, idesc_qk, part + ks != 0);
                 }
             ptx::mma_commit(&s_full[place]);
         };
@@ -367,6 +394,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
             const Segment<D> sg = segment_of<D>(p, r, g, b, off, x, st.x1);
             if (sg.j1 > sg.j0) {
                 ok = wait(&q_ready, items++);
+                ptx::tc_fence_after();
                 for (int j = sg.j0; j <= sg.j1 && ok; ++j) {
                     if (j < sg.j1) ok = wait(&k_full[keys.slot], keys.turn);
                     if (!ok) break;
@@ -411,7 +439,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                         ptx::mma_commit(&k_empty[keys.slot]);
                         ++n;
                         keys.next();
-                        if (j == sg.j1 - 1) ptx::mma_commit(&q_empty);
+                        if (!T::kQTmem && j == sg.j1 - 1) ptx::mma_commit(&q_empty);
                     }
                 }
             }
@@ -531,10 +559,16 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
             float back = 1.0f;
             if (sg.j1 > sg.j0) {
                 wait(&q_full, items++);
-                if (live) back = split_row<D>(sq + t * T::kQTile, row, p.negate);
+                // (this row tile's products of the item before have read its queries: their scores were waited for)
+                const float power = split_row<D, T::kQTmem>(sq + t * T::kQTile, row, p.negate, tmem + lanes + uint32_t(T::kQ + t * T::kQCols));
+                if (live) back = power;
+                if constexpr (T::kQTmem) ptx::tc_fence_before();
                 ptx::fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&q_ready);
+                if (lane == 0) {
+                    ptx::mbar_arrive(&q_ready);
+                    if (T::kQTmem) ptx::mbar_arrive(&q_empty);
+                }
             }
             if constexpr (!CAP) back *= p.scale2;
             // whether the row has seen a score, its running maximum of score plus value exponent in base 2 (negated and lifted, so
