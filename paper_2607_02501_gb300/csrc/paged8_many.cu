@@ -59,7 +59,6 @@ static_assert(Many8Traits<64>::kSmem > 114 * 1024 && Many8Traits<128>::kSmem > 1
 constexpr int kScaleTiles = 8;
 constexpr float kLift = 6.0f;     // the running maximum is held that much lower: weights are times 2^6,
 constexpr float kMostLag = 8.0f;  // and it moves when it is exceeded by as much more
-constexpr float kLargeScore = 4194304.0f;  // 2^22
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
@@ -455,8 +454,8 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
         if constexpr (NQ == 2) ptx::regs_down<72>();
         // a thread's first key and chunk, keys to its next one, steps over the keys (heads of 256: twice)
         constexpr int kStep = D == 64 ? 16 : 8, kSteps = KT / kStep, kEach = KT * D / 16 / 64;
-        // Chunks in flight: more of them hold up the softmax, whose accesses stand behind these in the load and store unit (4096 tokens
-        // over 16384 keys: 1 808 us, 2 818, 4 843, 8 936; 816 of two requests with heads of 256: 1 41.3, 2 38.8, 4 41.3).
+        // Chunks in flight: more of them hold up the softmax, whose accesses stand behind these in the load and store unit (when it was
+        // chosen, us: 4096 tokens over 16384 keys 1 808, 2 818, 4 843, 8 936; 816 of two requests with heads of 256 1 41, 2 39, 4 41).
         constexpr int kBatch = D == 256 ? 2 : 1;
         const int key_first = (lane & 7) + (D == 64 ? (warp & 1) * 8 : 0), c_first = (D == 64 ? 0 : (warp & 1) * 4) + lane / 8;
         uint32_t n = 0;
@@ -576,7 +575,6 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
             bool any = false;
             float mc = 0.0f;
             float2 l2 = make_float2(0, 0);
-            bool large = false;  // a maximum is so large that its rounding is felt in f16's range: weights are held below it one by one
             for (int j = sg.j0; j < sg.j1; ++j, ++n) {
                 wait(&scale_full[n % kScaleTiles], n / kScaleTiles);  // (every turn of it, also of tiles that the row tile skips)
                 if (j < a_t || j >= b_t) continue;
@@ -624,18 +622,28 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                     ptx::tmem_ld_wait_32(s + c);
 #pragma unroll
                     for (int h = c; h < c + 32; h += 16) {
-                        // (the maximum is of raw scores: their factor, positive, and a cap keep their order)
+                        if constexpr (!CAP) {
+                            // score plus value exponent, rounded here, so that what exceeds no maximum exceeds no bound below
+                            const float2 f = make_float2(by[h / 16], by[h / 16]), e2 = make_float2(up[h / 16], up[h / 16]);
+#pragma unroll
+                            for (int e = 0; e < 16; e += 2) {
+                                const float2 z = fma2(make_float2(s[h + e], s[h + e + 1]), f, e2);
+                                s[h + e] = z.x;
+                                s[h + e + 1] = z.y;
+                            }
+                        }
                         float top[5];
 #pragma unroll
                         for (int k = 0; k < 5; ++k) top[k] = max3(s[h + 3 * k], s[h + 3 * k + 1], s[h + 3 * k + 2]);
                         const float most = max3(max3(top[0], top[1], top[2]), max3(top[3], top[4], s[h + 15]), -INFINITY);
                         if constexpr (CAP) {
+                            // (the maximum is of raw scores: their factor, positive, and the cap keep their order)
 #pragma unroll
                             for (int e = 0; e < 16; ++e) far = fmaxf(far, s[h + e] == -INFINITY ? 0.0f : fabsf(s[h + e] * by[h / 16]));
                             const float z = capped2<CAP>(make_float2(most * by[h / 16], most * by[h / 16]), p).x + up[h / 16];
                             zt = most == -INFINITY ? zt : fmaxf(zt, z);
                         } else {
-                            zt = fmaxf(zt, fmaf(most, by[h / 16], up[h / 16]));
+                            zt = fmaxf(zt, most);
                         }
                     }
                 }
@@ -663,10 +671,9 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                         any = true;
                         mc = now;
                     }
-                    large = __any_sync(all, any && fabsf(mc) > kLargeScore);
                 }
-                // The weights, 32 at a time, over the scores. base(u, f, m) gives two weights' exponents from raw scores, their
-                // block's factor, and its value exponent less the row's maximum.
+                // The weights, 32 at a time, over the scores. base(u, f, m) gives two weights' exponents from s; f and m, for raw scores
+                // that a cap is still to be put on: their block's factor, and its value exponent less the row's maximum.
                 auto weights = [&](auto base) {
 #pragma unroll
                     for (int c = 0; c < KT; c += 32) {
@@ -689,21 +696,21 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                         ptx::tmem_st_16(s_col + c / 2, w);
                     }
                 };
-                // (NaN stays NaN)
-                auto held = [](float2 z) {
-                    return make_float2(z.x > kLift + kMostLag ? kLift + kMostLag : z.x, z.y > kLift + kMostLag ? kLift + kMostLag : z.y);
-                };
                 if constexpr (!CAP) {
-                    if (!large) weights([&](float2 u, float2 f, float2 m) { return fma2(u, f, m); });
-                    else weights([&](float2 u, float2 f, float2 m) { return held(fma2(u, f, m)); });
+                    const float2 mm = make_float2(mc, mc);
+                    weights([&](float2 u, float2, float2) { return add2(u, mm); });
                 } else {
                     auto shown = [](float2 u, float2 z) {
                         return make_float2(u.x == -INFINITY ? -INFINITY : z.x, u.y == -INFINITY ? -INFINITY : z.y);
                     };
+                    // (a maximum may be so large that its rounding is felt in f16's range. NaN stays NaN)
+                    auto held = [](float2 z) {
+                        return make_float2(z.x > kLift + kMostLag ? kLift + kMostLag : z.x, z.y > kLift + kMostLag ? kLift + kMostLag : z.y);
+                    };
                     // far below the cap one power of two per score, where exponential and reciprocal take two more turns of
                     // the same unit
-                    if (!large && __all_sync(all, !sees || far * p.scale2 < kNearCap))
-                        weights([&](float2 u, float2 f, float2 m) { return shown(u, capped_near2(mul2(u, f), p, m)); });
+                    if (__all_sync(all, !sees || far * p.scale2 < kNearCap))
+                        weights([&](float2 u, float2 f, float2 m) { return shown(u, held(capped_near2(mul2(u, f), p, m))); });
                     else
                         weights([&](float2 u, float2 f, float2 m) { return shown(u, held(add2(capped2<CAP>(mul2(u, f), p), m))); });
                 }
