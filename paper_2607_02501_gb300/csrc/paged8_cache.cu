@@ -146,12 +146,12 @@ __global__ void __launch_bounds__(kStoreThreads, 3) paged_codes_store_kernel(con
     __syncthreads();
     ptx::griddep_wait();
     const Place8<D, NB, E> at(u, a.rot_dim);
-    auto angles = [&](auto exact, int64_t t, float (&c)[E / 2], float (&s)[E / 2]) {
+    // (pos: the token's only position, or anything if there are several axes)
+    auto angles = [&](auto exact, int64_t t, int32_t pos, float (&c)[E / 2], float (&s)[E / 2]) {
         constexpr bool kExact = decltype(exact)::value;
         if (!at.turned) return;
         const int pair = u * (E / 2);
         if (!a.axis_of_pair) {
-            const int32_t pos = a.positions[t];
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) angle_of<kExact>(pos, a.turns[pair + i], a.factor, c[i], s[i]);
         } else {
@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kStoreThreads, 3) paged_codes_store_kernel(con
         fetch(h0, raw[0]);
         fetch(h0 + hw, raw[1]);
         float c[E / 2], s[E / 2];
-        if (h_end > 0) angles(std::false_type{}, t, c, s);
+        if (h_end > 0) angles(std::false_type{}, t, a.positions[t], c, s);
         for (int r = 0; r < p.rounds; r += 2) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -206,6 +206,15 @@ __global__ void __launch_bounds__(kStoreThreads, 3) paged_codes_store_kernel(con
     const int64_t t0 = int64_t(int(blockIdx.x) / 2 / Hk) * kWindow8;
     uint8_t* codes = is_k ? a.k_codes : a.v_codes;
     uint8_t* exps = is_k ? a.k_exp : a.v_exp;
+    auto row_at = [&](int j) { return (is_k ? a.k + (t0 + j) * a.k_stride : a.v + (t0 + j) * a.v_stride) + g * D; };
+    // the window's own rows and positions are on their way while it is found out whose blocks they are
+    RawRow<E / 2> early[2] = {};
+    int32_t early_pos = 0;
+    if (row < kWindow8 && t0 + row < a.n_tokens) {
+        early[0] = *reinterpret_cast<const RawRow<E / 2>*>(row_at(row) + at.e0);
+        early[1] = *reinterpret_cast<const RawRow<E / 2>*>(row_at(row) + at.e1);
+        if (is_k) early_pos = a.positions[t0 + row];
+    }
     // Tokens t0 .. t0 + 31, a lane each. The first token of a token's block is the furthest of those up to 15 before it that share
     // the block; the block is this CTA's if that lies in the window. (By comparisons: matching 64-bit numbers over a
     // warp takes 2 us where each token has a block of its own.)
@@ -239,10 +248,12 @@ __global__ void __launch_bounds__(kStoreThreads, 3) paged_codes_store_kernel(con
     float x[kPasses][E];
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
-        const uint16_t* from = (is_k ? a.k + (t0 + token(i)) * a.k_stride : a.v + (t0 + token(i)) * a.v_stride) + g * D;
-        if (is_own(i)) {
-            load_row<E / 2>(from + at.e0, x[i]);
-            load_row<E / 2>(from + at.e1, x[i] + E / 2);
+        if (is_own(i) && token(i) < kWindow8 && i == 0) {
+            unpack_row<E / 2>(early[0], x[i]);
+            unpack_row<E / 2>(early[1], x[i] + E / 2);
+        } else if (is_own(i)) {
+            load_row<E / 2>(row_at(token(i)) + at.e0, x[i]);
+            load_row<E / 2>(row_at(token(i)) + at.e1, x[i] + E / 2);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) x[i][e] = 0.0f;
@@ -254,7 +265,7 @@ __global__ void __launch_bounds__(kStoreThreads, 3) paged_codes_store_kernel(con
         if (!any_own(i)) continue;
         if (is_k) {
             float c[E / 2], s[E / 2];
-            if (is_own(i)) angles(std::true_type{}, t0 + token(i), c, s);
+            if (is_own(i)) angles(std::true_type{}, t0 + token(i), i == 0 && token(i) < kWindow8 ? early_pos : a.positions[t0 + token(i)], c, s);
             norm_turn<D, NB, E>(x[i], a.k_gamma, a.eps, at, c, s);
         }
         float m = 0.0f;
