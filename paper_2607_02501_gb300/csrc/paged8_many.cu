@@ -587,7 +587,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
 #pragma unroll
                 for (int k = 0; k < NB; ++k) {
                     const float2 bl = block[k];
-                    by[k] = fminf(fmaxf(back * bl.x, 1e-37f), 1.2676506e30f);
+                    by[k] = fminf(fmaxf(back * bl.x, 1e-37f), 3.0e38f);
                     up[k] = bl.y;
                 }
                 wait(&s_full[place], seen[place]++);

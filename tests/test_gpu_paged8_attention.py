@@ -294,3 +294,20 @@ def test_cache_beyond_32_bits(cuda_device, new):
     ko, vo = torch.empty_like(x), torch.empty_like(x)
     emb.emb_paged8_read(*cache, slots, ko, vo)
     assert torch.equal(ko, vo) and ((ko.float() - x.float()).abs() <= 2.0 ** -4 * x.float().abs() + 1e-3).all()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("new", [1, 5, 150])
+def test_scores_near_the_largest_numbers(cuda_device, d, new):
+    """Scores of up to 2^125 whose order hangs on the blocks' powers: one key has all the weight."""
+    s = Paged8([new], [new + 60], 2, 1, d, 16, seed=23)
+    s.q = np.full_like(s.q, 2.0 ** 97)
+    s.k = np.zeros_like(s.k)
+    far, near = s.at(0, 5), s.at(0, 40)
+    s.k[far][0, 0] = 2.0 ** 28          # by a large block's smallest code: 2^125
+    s.k[far[0], (far[1] + 1) % 16, 0, 1] = 2.0 ** 34
+    s.k[near][0, :4] = 2.0 ** 24        # by a small block's largest: 2^123
+    s.scale = 1.0
+    s.q[:, 1::d] = 0.0                  # (the element that makes the first block large does not count)
+    O = host(s.run())
+    assert np.array_equal(O, np.tile(oracle.paged8_values(s.codes[1], s.codes[3])[far][0], (new, 2)))
