@@ -260,6 +260,7 @@ __global__ void __launch_bounds__(kStoreThreads, 3) paged_codes_store_kernel(con
         }
     }
     const float limit = kCodeMost * pow2i(kExpMost);
+    bool odd[kPasses] = {};
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
         if (!any_own(i)) continue;
@@ -268,11 +269,19 @@ __global__ void __launch_bounds__(kStoreThreads, 3) paged_codes_store_kernel(con
             if (is_own(i)) angles(std::true_type{}, t0 + token(i), i == 0 && token(i) < kWindow8 ? early_pos : a.positions[t0 + token(i)], c, s);
             norm_turn<D, NB, E>(x[i], a.k_gamma, a.eps, at, c, s);
         }
+        // (zero times an infinity or NaN is NaN: elements that become NaN codes are looked for one by one only then)
         float m = 0.0f;
+        float2 zeros = make_float2(0, 0);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float v = fabsf(x[i][e]);
-            m = v <= limit ? fmaxf(m, v) : m;
+        for (int e = 0; e < E; e += 2) {
+            m = fmaxf(m, fmaxf(fabsf(x[i][e]), fabsf(x[i][e + 1])));
+            zeros = fma2(make_float2(x[i][e], x[i][e + 1]), make_float2(0, 0), zeros);
+        }
+        odd[i] = !(m <= limit) || zeros.x + zeros.y != 0.0f;
+        if (odd[i]) {
+            m = 0.0f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) m = fabsf(x[i][e]) <= limit ? fmaxf(m, fabsf(x[i][e])) : m;
         }
 #pragma unroll
         for (int o = kLanes / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(all, m, o));
@@ -294,12 +303,16 @@ __global__ void __launch_bounds__(kStoreThreads, 3) paged_codes_store_kernel(con
         const int64_t slot = __shfl_sync(all, mine, token(i) & 31);
         if (!is_own(i)) continue;
         uint32_t w[E / 4];
+        const float2 unit2 = make_float2(unit, unit);
 #pragma unroll
         for (int e = 0; e < E; e += 4) {
-            w[e / 4] = codes_of(x[i][e] * unit, x[i][e + 1] * unit) | codes_of(x[i][e + 2] * unit, x[i][e + 3] * unit) << 16;
+            const float2 y = mul2(make_float2(x[i][e], x[i][e + 1]), unit2), z = mul2(make_float2(x[i][e + 2], x[i][e + 3]), unit2);
+            w[e / 4] = codes_of(y.x, y.y) | codes_of(z.x, z.y) << 16;
+        }
+        if (odd[i]) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (!(fabsf(x[i][e + k]) <= limit)) w[e / 4] = (w[e / 4] & ~(0xFFu << (8 * k))) | 0x7Fu << (8 * k);
+            for (int e = 0; e < E; ++e)
+                if (!(fabsf(x[i][e]) <= limit)) w[e / 4] = (w[e / 4] & ~(0xFFu << (8 * (e & 3)))) | 0x7Fu << (8 * (e & 3));
         }
         uint8_t* to = codes + (slot * Hk + g) * D;
         if constexpr (E == 16) {
