@@ -599,6 +599,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                 // Votes are taken among rows that see a key of the tile. A tile's other rows are not of this request, or not
                 // even filled (3 heads: 126 of 128 rows), and what they hold may not decide how a warp computes.
                 const bool sees = max(lo, 0) < min(hi, KT);
+                float zt = -INFINITY, far = 0.0f;  // far, for a cap: the largest magnitude of q.k that the row sees
                 if (edge) {
                     // scores that the row does not see, in tensor memory: rolled up and away from the path of most tiles
 #pragma unroll 1
@@ -608,7 +609,11 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                         ptx::tmem_ld_32(s_col + c, v);
                         ptx::tmem_ld_wait_32(v);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(c + e >= lo && c + e < hi ? v[e] : -INFINITY);
+                        for (int e = 0; e < 32; ++e) {
+                            const bool in = c + e >= lo && c + e < hi;
+                            if (CAP && in) far = fmaxf(far, fabsf(v[e]) * (back * block[c / 16 + e / 16].x));
+                            w[e] = __float_as_uint(in ? v[e] : -INFINITY);
+                        }
                         ptx::tmem_st_32(s_col + c, w);
                     }
                     ptx::tmem_st_wait();
@@ -616,31 +621,34 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                 float s[KT];
 #pragma unroll
                 for (int c = 0; c < KT; c += 32) ptx::tmem_ld_32(s_col + c, s + c);
-                float zt = -INFINITY, far = 0.0f;  // far, for a cap: the largest magnitude of q.k that the row sees
 #pragma unroll
                 for (int c = 0; c < KT; c += 32) {
                     ptx::tmem_ld_wait_32(s + c);
 #pragma unroll
                     for (int h = c; h < c + 32; h += 16) {
-                        if constexpr (!CAP) {
-                            // score plus value exponent, rounded here, so that what exceeds no maximum exceeds no bound below
-                            const float2 f = make_float2(by[h / 16], by[h / 16]), e2 = make_float2(up[h / 16], up[h / 16]);
+                        // score plus value exponent, rounded here, so that what exceeds no maximum exceeds no bound below; or for a
+                        // cap q.k yet
+                        const float2 f = make_float2(by[h / 16], by[h / 16]), e2 = make_float2(up[h / 16], up[h / 16]);
 #pragma unroll
-                            for (int e = 0; e < 16; e += 2) {
-                                const float2 z = fma2(make_float2(s[h + e], s[h + e + 1]), f, e2);
-                                s[h + e] = z.x;
-                                s[h + e + 1] = z.y;
-                            }
+                        for (int e = 0; e < 16; e += 2) {
+                            const float2 u = make_float2(s[h + e], s[h + e + 1]), z = CAP ? mul2(u, f) : fma2(u, f, e2);
+                            s[h + e] = z.x;
+                            s[h + e + 1] = z.y;
                         }
                         float top[5];
 #pragma unroll
                         for (int k = 0; k < 5; ++k) top[k] = max3(s[h + 3 * k], s[h + 3 * k + 1], s[h + 3 * k + 2]);
                         const float most = max3(max3(top[0], top[1], top[2]), max3(top[3], top[4], s[h + 15]), -INFINITY);
                         if constexpr (CAP) {
-                            // (the maximum is of raw scores: their factor, positive, and the cap keep their order)
+                            // (the maximum is of what the cap is put on: it keeps their order)
+                            if (!edge) {
+                                float low[5];
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) far = fmaxf(far, s[h + e] == -INFINITY ? 0.0f : fabsf(s[h + e] * by[h / 16]));
-                            const float z = capped2<CAP>(make_float2(most * by[h / 16], most * by[h / 16]), p).x + up[h / 16];
+                                for (int k = 0; k < 5; ++k) low[k] = fminf(fminf(s[h + 3 * k], s[h + 3 * k + 1]), s[h + 3 * k + 2]);
+                                const float least = fminf(fminf(fminf(low[0], low[1]), fminf(low[2], low[3])), fminf(low[4], s[h + 15]));
+                                far = max3(far, fabsf(most), fabsf(least));
+                            }
+                            const float z = capped2<CAP>(make_float2(most, most), p).x + up[h / 16];
                             zt = most == -INFINITY ? zt : fmaxf(zt, z);
                         } else {
                             zt = fmaxf(zt, most);
@@ -672,8 +680,8 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                         mc = now;
                     }
                 }
-                // The weights, 32 at a time, over the scores. base(u, f, m) gives two weights' exponents from s; f and m, for raw scores
-                // that a cap is still to be put on: their block's factor, and its value exponent less the row's maximum.
+                // The weights, 32 at a time, over the scores. base(u, m) gives two weights' exponents from s, and for q.k that a cap is still to be
+                // put on m, their block's value exponent less the row's maximum.
                 auto weights = [&](auto base) {
 #pragma unroll
                     for (int c = 0; c < KT; c += 32) {
@@ -684,7 +692,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                             float2 sum = make_float2(0, 0);
 #pragma unroll
                             for (int e = 0; e < 16; e += 2) {
-                                float2 u = base(make_float2(s[h + e], s[h + e + 1]), make_float2(by[h / 16], by[h / 16]), make_float2(m, m));
+                                float2 u = base(make_float2(s[h + e], s[h + e + 1]), make_float2(m, m));
                                 u.x = exp2_fast(u.x);
                                 u.y = exp2_fast(u.y);
                                 sum = add2(sum, u);
@@ -698,21 +706,22 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                 };
                 if constexpr (!CAP) {
                     const float2 mm = make_float2(mc, mc);
-                    weights([&](float2 u, float2, float2) { return add2(u, mm); });
+                    weights([&](float2 u, float2) { return add2(u, mm); });
                 } else {
                     auto shown = [](float2 u, float2 z) {
                         return make_float2(u.x == -INFINITY ? -INFINITY : z.x, u.y == -INFINITY ? -INFINITY : z.y);
                     };
-                    // (a maximum may be so large that its rounding is felt in f16's range. NaN stays NaN)
+                    // (under a large cap a maximum's rounding may be felt in f16's range. NaN stays NaN)
                     auto held = [](float2 z) {
+                        if constexpr (CAP == kLowCap) return z;
                         return make_float2(z.x > kLift + kMostLag ? kLift + kMostLag : z.x, z.y > kLift + kMostLag ? kLift + kMostLag : z.y);
                     };
                     // far below the cap one power of two per score, where exponential and reciprocal take two more turns of
-                    // the same unit
+                    // the same unit (the series runs away to -infinity at what stands for a hidden score)
                     if (__all_sync(all, !sees || far * p.scale2 < kNearCap))
-                        weights([&](float2 u, float2 f, float2 m) { return shown(u, held(capped_near2(mul2(u, f), p, m))); });
+                        weights([&](float2 u, float2 m) { return held(capped_near2(u, p, m)); });
                     else
-                        weights([&](float2 u, float2 f, float2 m) { return shown(u, held(add2(capped2<CAP>(mul2(u, f), p), m))); });
+                        weights([&](float2 u, float2 m) { return shown(u, held(add2(capped2<CAP>(u, p), m))); });
                 }
                 // every phase of o_done is waited for, so that a wait cannot take the one before the last for the last:
                 // with two score places the last scores do not tell that the product before theirs is in
