@@ -279,3 +279,29 @@ def test_recorded_and_on_another_stream(cuda_device):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, [s.q_out] + s.cache))
     rec.close()
+
+
+def test_tokens_of_a_block_in_any_order(cuda_device):
+    """Within 16 consecutive tokens: each block's tokens backwards, and two blocks' tokens in turns."""
+    s = Step([5, 0], [60, 40], 2, 2, 128, 32, seed=13).norm().rotate(64)
+    order, blocks = [], s.slots // BLOCK
+    for b in dict.fromkeys(blocks.tolist()):
+        order += np.flatnonzero(blocks == b)[::-1].tolist()
+    s.slots, s.positions = s.slots[order], s.positions[:, order]
+    s.check("backwards")
+    s = Step([9, 9], [7, 7], 2, 1, 64, 16, seed=14)
+    order = np.arange(14).reshape(2, 7).T.reshape(-1)
+    s.slots, s.positions = s.slots[order], s.positions[:, order]
+    s.check("in turns")
+
+
+def test_positions_wider_than_the_tokens(cuda_device):
+    """Positions of several axes cut out of a wider table."""
+    s = Step([3], [21], 2, 1, 64, 16, seed=15).rotate(64, axes=3).device()
+    emb.emb_paged8_store(*s.args, **s.kw)
+    want = [x.clone() for x in [s.q_out] + s.cache]
+    s.device()
+    wide = torch.full((3, 50), 10 ** 6, dtype=torch.int32, device="cuda")
+    wide[:, :s.T] = s.args[9]
+    emb.emb_paged8_store(*s.args[:9], wide, *s.args[10:], **s.kw)
+    assert all(torch.equal(a, b) for a, b in zip(want, [s.q_out] + s.cache))
