@@ -5,7 +5,7 @@
 // (queries times heads), and each of four warps takes a quarter of a tile's keys; the warps' results are merged at the
 // item's end. What differs:
 // - Tiles of 128 keys: twice the keys for the same steps of a warp, which are a chain of latencies (64 requests of up to 16384 keys
-//   with tiles of 64: 252 us, whatever the stages).
+//   of 8 heads of 128 with tiles of 64 252 us, whatever the stages, 241 with 128).
 // - A warp's 32 keys are two blocks of the cache, with a key power and a value power each. The producer looks them up two
 //   rounds ahead and lays them beside the tile.
 // - Codes become f16 in registers, after ldmatrix, by the hardware's conversion of two at a time. A key's 16 bytes give a lane four
@@ -14,7 +14,8 @@
 // - Softmax with the values' powers: with z the score in base 2 and e the exponent of its key's values, the running maximum m is that
 //   of z + e, the weight w = 2^(z + e - m) <= 1 multiplies the bare codes, and the sum of weights adds w 2^-e. So w is in f16's
 //   range whatever the blocks' powers are: times 2^14, those above 2^-28 of the largest are rounded to 11 bits.
-// HBM bounds long histories, latency and the joins small calls.
+// HBM bounds long histories: those 64 requests' 1.09 GB take 202 to 211 us now, 0.77 to 0.80 of the measured copy rate, and 181 if nothing
+// is computed. Latency and the joins bound small calls: one token over 867 keys 6.2 us.
 #include <algorithm>
 #include <cmath>
 #include <mutex>
@@ -692,7 +693,9 @@ int few8_blocks(const PagedAttnArgs& a) {
     return int((std::min(a.max_q, a.n_tokens) + qb - 1) / qb);
 }
 // CTAs of the cluster that takes a block, or 0 where equal stretches of all the work are sooner done: the rule of the bf16
-// cache's kernel (paged_attention.cu), whose tiles take about the time of these.
+// cache's kernel (paged_attention.cu, where its measurements stand), in keys: tiles here have twice as many, so its limits are halved.
+// With it, where more than 16 rows have clusters (us, and the tcgen05 kernel): 24 requests of 4 queries of 16 heads on 2 over 1500 keys 11.5 and 19.3
+// (heads of 64), 15.8 and 21.8 (128), one of 8 queries over 4000 keys 8.8 and 16.8, 11.4 and 16.9, 14.7 and 25.2 (256).
 int few8_cluster(const PagedAttnArgs& a) {
     double keys = double(a.max_pages * a.page_size);
     if (a.window > 0) keys = std::min(keys, double(a.window) + kFewRows + kFewTile);
