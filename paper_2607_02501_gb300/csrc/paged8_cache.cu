@@ -19,8 +19,8 @@ namespace {
 // is in its window, up to 15 tokens beyond it, and leaves those that began before. So no two CTAs meet in a block, nothing is
 // exchanged between CTAs, and a token's rows stay in registers between the block's maximum and the rounding. Every warp works out
 // the blocks of all 32 tokens by itself, a lane a token, so there is one barrier.
-// Measured (us replayed): 15600 tokens of 10 heads of 256 (136 MB) 37.5, 0.54 of the measured copy rate; 256 decoded tokens of 48 heads of
-// 128 4.9, one of 10 heads 3.2. Rows and keys' and values' CTAs of eight elements a thread, one CTA for both, took 86, 8.7 and 4.5.
+// Measured (us replayed): 15600 tokens of 10 heads of 256 (152 MB) 37.5, 0.60 of the measured copy rate; 256 decoded tokens of 48 heads of
+// 128 4.9, one of 10 heads 3.2. With eight elements a thread and keys and values in one CTA 86, 8.7 and 4.5.
 constexpr int kStoreThreads = 256;
 constexpr int kWindow8 = 16;  // tokens
 constexpr int kMostRounds = 8;  // heads that a thread takes of its token, at most
