@@ -57,9 +57,13 @@ struct Many8Traits {
 constexpr uint32_t kTmemAll = 512;
 static_assert(Many8Traits<64>::kSmem > 114 * 1024 && Many8Traits<128>::kSmem > 114 * 1024 && Many8Traits<256>::kSmem > 114 * 1024,
               "one CTA per SM: tensor memory is allocated whole (see ptx::tmem_alloc)");
-// Tiles whose exponents are held: the producer is at most five ahead of the softmax, as keys' places are handed back behind the
-// products of a tile, and those wait for the softmax of the tile before it.
+// Tiles whose exponents are held. A softmax warp reads those of the tiles that its rows have products of. There the producer cannot
+// lap it: it writes those of tile n + kKeys + 1 only behind products that wait for the warp's weights of tile n. Tiles that its rows
+// do not see hold nobody up, so the warp waits for none of theirs; behind them it may be ahead of the producer by more than a
+// round, which a parity cannot tell, so there the tile's scores are awaited first.
 constexpr int kScaleTiles = 8;
+static_assert(Many8Traits<64>::kKeys < kScaleTiles && Many8Traits<128>::kKeys < kScaleTiles && Many8Traits<256>::kKeys < kScaleTiles,
+              "exponents outlast the wait for their tile's weights");
 constexpr float kLift = 6.0f;     // the running maximum is held that much lower: weights are times 2^6,
 constexpr float kMostLag = 8.0f;  // and it moves when it is exceeded by as much more
 
@@ -578,10 +582,15 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
             bool any = false;
             float mc = 0.0f;
             float2 l2 = make_float2(0, 0);
-            for (int j = sg.j0; j < sg.j1; ++j, ++n) {
-                wait(&scale_full[n % kScaleTiles], n / kScaleTiles);  // (every turn of it, also of tiles that the row tile skips)
-                if (j < a_t || j >= b_t) continue;
+            const uint32_t behind = n + uint32_t(sg.j1 - sg.j0);
+            if (b_t > a_t) {
+                n += uint32_t(a_t - sg.j0);
                 const int place = NQ == 2 ? t : int(n & 1);
+                wait(&s_full[place], seen[place]);  // (see kScaleTiles)
+            }
+            for (int j = a_t; j < b_t; ++j, ++n) {
+                const int place = NQ == 2 ? t : int(n & 1);
+                wait(&scale_full[n % kScaleTiles], n / kScaleTiles);
                 // The factors of the blocks' raw scores, held so that a product neither overflows nor makes NaN of what is hidden,
                 // and the values' exponents: read while the scores are still being made. (A load from shared memory between scores
                 // and weights costs its latency in every tile, more registers than these spill.)
@@ -735,6 +744,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                 if (lane == 0) ptx::mbar_arrive(&p_ready[place]);
                 ++outs;
             }
+            n = behind;
             // the segment's result: outputs, or this CTA's part of them
             const bool has = b_t > a_t;
             const float l = l2.x + l2.y;
