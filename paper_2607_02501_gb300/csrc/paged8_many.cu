@@ -18,6 +18,7 @@
 // bf16 cache's kernel 600 to 640): a tile's chain of scores, softmax and product, of which the blocks' powers lengthen the softmax; without the
 // values' conversion 745. Heads of 256: 816 tokens of two requests 35 us, shared memory's bandwidth (values are read, written and read).
 #include <algorithm>
+#include <cfloat>
 #include <mutex>
 
 #include "paged8.cuh"
@@ -596,10 +597,11 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                 // and weights costs its latency in every tile, more registers than these spill.)
                 const float2* block = scales[n % kScaleTiles];
                 float by[NB], up[NB];
+                auto factor = [&](float power) { return fminf(fmaxf(back * power, 1e-37f), 3.0e38f); };
 #pragma unroll
                 for (int k = 0; k < NB; ++k) {
                     const float2 bl = block[k];
-                    by[k] = fminf(fmaxf(back * bl.x, 1e-37f), 3.0e38f);
+                    by[k] = factor(bl.x);
                     up[k] = bl.y;
                 }
                 wait(&s_full[place], seen[place]++);
@@ -612,8 +614,12 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                 // even filled (3 heads: 126 of 128 rows), and what they hold may not decide how a warp computes.
                 const bool sees = max(lo, 0) < min(hi, KT);
                 float zt = -INFINITY, far = 0.0f;  // far, for a cap: the largest magnitude of q.k that the row sees
+                // What stands for a score that the row does not see: of a tile without any, nothing. (A product q.k of -infinity is a score
+                // of -cap and counts.)
+                const float gone = edge ? -INFINITY : NAN;
                 if (edge) {
-                    // scores that the row does not see, in tensor memory: rolled up and away from the path of most tiles
+                    // Scores that the row does not see, in tensor memory: rolled up and away from the path of most tiles. Under a cap the
+                    // others become the products q.k here, held above what stands for those.
 #pragma unroll 1
                     for (int c = 0; c < KT; c += 32) {
                         float v[32];
@@ -623,12 +629,21 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
 #pragma unroll
                         for (int e = 0; e < 32; ++e) {
                             const bool in = c + e >= lo && c + e < hi;
-                            if (CAP && in) far = fmaxf(far, fabsf(v[e]) * (back * block[c / 16 + e / 16].x));
-                            w[e] = __float_as_uint(in ? v[e] : -INFINITY);
+                            float u = v[e];
+                            if constexpr (CAP) {
+                                u *= factor(block[c / 16 + e / 16].x);
+                                if (in) far = fmaxf(far, fabsf(u));
+                                u = u < -FLT_MAX ? -FLT_MAX : u;  // (NaN stays NaN)
+                            }
+                            w[e] = __float_as_uint(in ? u : -INFINITY);
                         }
                         ptx::tmem_st_32(s_col + c, w);
                     }
                     ptx::tmem_st_wait();
+                    if constexpr (CAP) {
+#pragma unroll
+                        for (int k = 0; k < NB; ++k) by[k] = 1.0f;
+                    }
                 }
                 float s[KT];
 #pragma unroll
@@ -661,7 +676,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                                 far = max3(far, fabsf(most), fabsf(least));
                             }
                             const float z = capped2<CAP>(make_float2(most, most), p).x + up[h / 16];
-                            zt = most == -INFINITY ? zt : fmaxf(zt, z);
+                            zt = most == gone ? zt : fmaxf(zt, z);
                         } else {
                             zt = fmaxf(zt, most);
                         }
@@ -720,8 +735,8 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                     const float2 mm = make_float2(mc, mc);
                     weights([&](float2 u, float2) { return add2(u, mm); });
                 } else {
-                    auto shown = [](float2 u, float2 z) {
-                        return make_float2(u.x == -INFINITY ? -INFINITY : z.x, u.y == -INFINITY ? -INFINITY : z.y);
+                    auto shown = [gone](float2 u, float2 z) {
+                        return make_float2(u.x == gone ? -INFINITY : z.x, u.y == gone ? -INFINITY : z.y);
                     };
                     // (under a large cap a maximum's rounding may be felt in f16's range. NaN stays NaN)
                     auto held = [](float2 z) {
