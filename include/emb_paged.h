@@ -217,7 +217,8 @@ EMB_API emb_status emb_paged8_read(const uint8_t* k_codes, const uint8_t* v_code
  * Queries enter the score product times a power of two per query and head, up to 16 query rows (max_q queries times heads per
  * key/value head) as f16: exact, but for elements below 2^-28 of the row's largest magnitude, which are within 2^-39 of that; above,
  * they may be two e4m3 numbers added up: exact, but for elements below 2^-9 of the largest, which are within 2^-17 of it. A query
- * row with an infinite element or a NaN gives NaN. The scores of a block are multiplied by its power of two in fp32. A
+ * row with an infinite element or a NaN gives NaN. A block's products are multiplied by its power of two and the scale in fp32
+ * (above 2^50 in magnitude, a scale may take that factor out of its range; it is then held at the range's end). A
  * weight, times its block's power for the values, enters the value product rounded once to f16: within a relative 2^-11, or within
  * 2^-31 of the row's largest such product. A page id outside [0, n_pages) is a page of zeros. A NaN code in a visible key makes
  * its queries' outputs NaN, one in a visible value that element of them. One workspace serves this call and emb_paged_attention

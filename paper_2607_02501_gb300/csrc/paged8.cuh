@@ -106,6 +106,15 @@ __device__ __forceinline__ RowPower row_power(float top) {
     const int e = max(int(__float_as_uint(top) >> 23) - 127, -100);  // floor(log2(top))
     return RowPower{top == INFINITY ? NAN : pow2i(14 - e), pow2i(e - 14)};
 }
+// The factor of a row's raw products over a block is row power x block power, without a cap times the scale. Its part that is the
+// row's may then pass fp32's range where the factor does not, so the block powers count from their least (2^48 larger, CAP == 0) and the
+// row's part is as much smaller; what falls below the subnormal numbers here is below 2^-20 in a score, |scale| <= 2^50.
+template <int CAP>
+__device__ __forceinline__ float block_power(int e) { return pow2i(CAP ? e : e + kExpMost); }
+__device__ __forceinline__ float row_factor(float back, float scale2) {
+    const float least = pow2i(-kExpMost);
+    return back >= 1.0f ? back * least * scale2 : back * scale2 * least;
+}
 // A block's factor of the raw products, held within fp32's range (a product of 0 stays 0 under the largest of them).
 __device__ __forceinline__ float score_factor(float x) { return fminf(fmaxf(x, -3.0e38f), 3.0e38f); }
 

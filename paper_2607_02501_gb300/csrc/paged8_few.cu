@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged_codes
     using PL = PartLayout<D, ROWS>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full[T::kStages], empty[T::kStages];
-    __shared__ float4 powers[T::kStages][kFewBlocks];  // of a block: 2^e of its keys; e of its values, 2^-e
+    __shared__ float4 powers[T::kStages][kFewBlocks];  // of a block: block_power of its keys; e of its values, 2^-e
     __shared__ int abort_flag, joined;
     __shared__ PagedJoin cut[2];
     __shared__ float warp_m[kFewWarps][16], warp_l[kFewWarps][16], row_back[16];
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged_codes
                     if (lane / (2 * kFewBlocks) == in) {
                         float4& to = powers[s][lane & (kFewBlocks - 1)];
                         if (lane & kFewBlocks) to.y = float(e), to.z = pow2i(-e);
-                        else to.x = pow2i(e);
+                        else to.x = block_power<CAP>(e);
                     }
                     __syncwarp();
                     if (ptx::elect_one()) ptx::mbar_arrive_expect_tx(&full[s], T::kStage);
@@ -306,8 +306,8 @@ __global__ void __launch_bounds__(kFewThreads, Few8Traits<D>::kCtas) paged_codes
             backB = row_back[rB];
         }
         if constexpr (!CAP) {
-            backA *= p.scale2;
-            backB *= p.scale2;
+            backA = row_factor(backA, p.scale2);
+            backB = row_factor(backB, p.scale2);
         }
 
         float o[NT][4];  // of n-tiles 2 c and 2 c + 1: dims 16 c + 4 qc + {0, 2} and + {1, 3}

@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t k_full[T::kKeys], k_empty[T::kKeys], raw_full[T::kVals], raw_empty[T::kVals], v_full[T::kConvs], v_empty[T::kConvs];
     __shared__ uint64_t q_full, q_ready, q_empty, scale_full[kScaleTiles], s_full[2], p_ready[2], o_done[2], o_free[2], drain;
-    __shared__ float2 scales[kScaleTiles][NB];  // of a block: 2^e of its keys, e of its values
+    __shared__ float2 scales[kScaleTiles][NB];  // of a block: block_power of its keys, e of its values
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag, joined, odd_seen;
     __shared__ PagedJoin cut[2];
@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                 const int e = exp_of_byte(ex), s = int(keys % kScaleTiles);
                 if (lane / (2 * NB) == turn) {
                     if (lane & NB) scales[s][lane & (NB - 1)].y = float(e);
-                    else scales[s][lane & (NB - 1)].x = pow2i(e);
+                    else scales[s][lane & (NB - 1)].x = block_power<CAP>(e);
                 }
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&scale_full[s]);
@@ -577,7 +577,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                     if (T::kQTmem) ptx::mbar_arrive(&q_empty);
                 }
             }
-            if constexpr (!CAP) back *= p.scale2;
+            if constexpr (!CAP) back = row_factor(back, p.scale2);
             // whether the row has seen a score, its running maximum of score plus value exponent in base 2 (negated and lifted, so
             // that it is added), sums of weights without the values' powers
             bool any = false;
