@@ -162,7 +162,8 @@ EMB_API emb_status emb_paged_selftest_wait_timeout(void* workspace, size_t ws_by
  * f_i = base^(-2 i / rot_dim) radians a position. For contexts longer than the `original` one that the model was made for
  * (stretch > 1): f_i * (k + (1 - k) / stretch), with k = 0 if original = 0 (every position is divided by stretch), else
  * k = clamp((original * f_i / 2 pi - low) / (high - low), 0, 1): pairs that turn `high` times within the original context
- * keep their rate, those that turn `low` times or less are stretched.
+ * keep their rate, those that turn `low` times or less are stretched, and between them k grows with the turns (not with the pair's
+ * number). turns[i] is within one unit of these formulas' value for f_i of up to 2^24 and high - low of at least 2^-20 high.
  * rot_dim even, 2..256; base > 0; stretch >= 1; original >= 0; 0 <= low < high. Errors: EMB_EINVAL. */
 EMB_API emb_status emb_rotary_turns(int64_t rot_dim, double base, double stretch, double original, double low, double high,
                                     uint64_t* turns);
@@ -188,8 +189,8 @@ EMB_API emb_status emb_rotary_turns(int64_t rot_dim, double base, double stretch
  * q, k, v: bf16, heads of a token contiguous, tokens q_stride, k_stride, v_stride elements apart, multiples of 8 and at least a
  * token's elements. gammas: fp32 [head_dim]. positions: int32 [n_axes][pos_stride], 1 <= n_axes <= 4, any value.
  * turns: device, uint64 [rot_dim / 2] (emb_rotary_turns), may be NULL if rot_dim is 0; axis_of_pair: device, uint8 [rot_dim / 2], entries of
- * n_axes or more count as n_axes - 1; NULL: axis 0 for every pair. The angle is exact modulo a turn but for the rounding of turns[i]
- * (2^-65 turns a position); cosine and sine are within 1e-6.
+ * n_axes or more count as n_axes - 1; NULL: axis 0 for every pair. The angle is exact modulo a turn for the given turns[i]
+ * (those of emb_rotary_turns are within 2^-64 turns a position of the formula's); cosine and sine are within 1e-6.
  * 1 <= n_tokens < 2^31; head_dim 64, 128 or 256, page_size 16, 32, 64, 128 or 256 (else EMB_EUNSUPPORTED); rot_dim % 8 == 0,
  * 0..head_dim; n_heads, n_kv_heads 1..4096; eps >= 0 and factor finite. Device pointers 16-byte aligned, but positions (4), slots and
  * turns (8), exponents and axis_of_pair (1). No output may overlap another buffer. Errors: EMB_EINVAL, EMB_EALIGN, EMB_EUNSUPPORTED,

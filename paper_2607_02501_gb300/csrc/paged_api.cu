@@ -57,6 +57,50 @@ bool clash(const Span* outs, int n_out, const Span* ins, int n_in) {
 emb_status from_cuda(cudaError_t e) { return e == cudaSuccess ? EMB_OK : EMB_ECUDA; }
 cudaStream_t stream_of(emb_stream_t s) { return reinterpret_cast<cudaStream_t>(s); }
 
+// A number as the sum of two fp64 ones, the second below half a unit of the first's last place: about 2^-104 of it (Dekker, 1971;
+// Knuth, The Art of Computer Programming, volume 2, 4.2.2). `volatile`: no product is contracted with a sum, on any machine.
+struct Twofold {
+    double hi, lo;
+};
+Twofold sum_of(double a, double b) {
+    const volatile double s = a + b, t = s - a;
+    const volatile double u = s - t;
+    return {s, (a - u) + (b - t)};
+}
+Twofold operator+(Twofold a, Twofold b) {
+    const Twofold s = sum_of(a.hi, b.hi);
+    return sum_of(s.hi, s.lo + (a.lo + b.lo));
+}
+Twofold operator*(Twofold a, Twofold b) {
+    const volatile double p = a.hi * b.hi;
+    const double e = std::fma(a.hi, b.hi, -p);
+    return sum_of(p, std::fma(a.hi, b.lo, std::fma(a.lo, b.hi, e)));
+}
+Twofold operator/(Twofold a, Twofold b) {  // two steps of long division, and the rest's rest
+    const double q0 = a.hi / b.hi;
+    const Twofold r = a + Twofold{-q0, 0.0} * b;
+    const double q1 = r.hi / b.hi;
+    const Twofold s = r + Twofold{-q1, 0.0} * b;
+    return sum_of(q0, q1) + Twofold{s.hi / b.hi, 0.0};
+}
+Twofold power(Twofold x, int64_t n) {
+    Twofold y{1.0, 0.0};
+    for (; n > 0; n >>= 1) {
+        if (n & 1) y = y * x;
+        if (n > 1) x = x * x;
+    }
+    return y;
+}
+// x^(-1 / n), x in [1/2, 2]: Newton's step on x y^n = 1, which doubles the digits of the first guess.
+Twofold inverse_root(double x, int64_t n) {
+    Twofold y{std::pow(x, -1.0 / double(n)), 0.0};
+    for (int k = 0; k < 2; ++k) {
+        const Twofold off = Twofold{1.0, 0.0} + Twofold{-x, 0.0} * power(y, n);
+        y = y + y * (off / Twofold{double(n), 0.0});
+    }
+    return y;
+}
+
 bool cache8_supported(int64_t head_dim, int64_t page_size) {
     return (head_dim == 64 || head_dim == 128 || head_dim == 256) &&
            (page_size == 16 || page_size == 32 || page_size == 64 || page_size == 128 || page_size == 256);
@@ -286,16 +330,28 @@ emb_status emb_rotary_turns(int64_t rot_dim, double base, double stretch, double
         !std::isfinite(stretch) || !(original >= 0.0) || !std::isfinite(original) || !(low >= 0.0) || !(high > low) ||
         !std::isfinite(high) || !turns)
         return EMB_EINVAL;
-    constexpr double kTurn = 6.283185307179586476925;
-    for (int64_t i = 0; i < rot_dim / 2; ++i) {
-        double f = std::pow(base, -2.0 * double(i) / double(rot_dim)) / kTurn;  // turns a position
+    // base^(-i / n) for base = m 2^e, i e = q n + j: m^(-i / n) 2^(-j / n) 2^-q, the first two of which are near one
+    const int64_t n = rot_dim / 2;
+    int e = 0;
+    const double m = std::frexp(base, &e);
+    const Twofold root = inverse_root(m, n), half = inverse_root(2.0, n), one{1.0, 0.0};
+    const Twofold per_radian{0x1.45f306dc9c883p-3, -0x1.6b01ec5417056p-57};  // 1 / (2 pi)
+    for (int64_t i = 0; i < n; ++i) {
+        const int64_t q = i * e >= 0 ? i * e / n : -((-i * e + n - 1) / n), j = i * e - q * n;
+        Twofold t = power(root, i) * power(half, j) * per_radian;  // turns a position
+        t = {std::ldexp(t.hi, int(-q)), std::ldexp(t.lo, int(-q))};
         if (stretch > 1.0) {
-            const double keep = original > 0.0 ? std::min(1.0, std::max(0.0, (original * f - low) / (high - low))) : 0.0;
-            f *= keep + (1.0 - keep) / stretch;
+            const double turned = original * t.hi;
+            Twofold keep{turned >= 2.0 * high ? 1.0 : 0.0, 0.0};
+            if (turned < 2.0 * high && turned > 0.5 * low) keep = (Twofold{original, 0.0} * t + Twofold{-low, 0.0}) / sum_of(high, -low);
+            if (!(keep.hi > 0.0)) keep = {0.0, 0.0};
+            if (!(keep.hi < 1.0)) keep = one;
+            t = t * (keep + (one + Twofold{-keep.hi, -keep.lo}) / Twofold{stretch, 0.0});
         }
-        f -= std::floor(f);  // whole turns are none
-        const double units = std::floor(std::ldexp(f, 64) + 0.5);
-        turns[i] = units >= 18446744073709551616.0 ? 0 : uint64_t(units);
+        // whole turns are none; whole units and the rest of both parts
+        const double a = std::ldexp(std::fmod(t.hi, 1.0), 64), b = std::ldexp(std::fmod(t.lo, 1.0), 64);
+        const double down = std::floor(b), rest = (a - std::floor(a)) + (b - down);
+        turns[i] = uint64_t(std::floor(a)) + (down < 0.0 ? 0 - uint64_t(-down) : uint64_t(down)) + uint64_t(std::floor(rest + 0.5));
     }
     return EMB_OK;
 }
