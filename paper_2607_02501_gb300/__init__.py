@@ -467,7 +467,7 @@ def emb_rotary_turns(rot_dim: int, base: float = 10000.0, stretch: float = 1.0, 
     """How fast the pairs of a rotary embedding turn, for emb_paged8_store: an int64 tensor [rot_dim / 2] in host memory
     (the bits of unsigned numbers)."""
     import torch
-    turns = torch.zeros(max(rot_dim, 0) // 2, dtype=torch.int64)
+    turns = torch.zeros(min(max(rot_dim, 0), 256) // 2, dtype=torch.int64)  # (others are refused)
     _check(paged_lib().emb_rotary_turns(rot_dim, base, stretch, original, low, high, _ptr(turns)), "emb_rotary_turns")
     return turns
 

@@ -33,3 +33,10 @@ def test_turns_are_those_of_the_formula(rot_dim, base, long):
     want = exact_units(rot_dim, base, **long)
     off = [abs((Decimal(g) - w + 2 ** 63) % 2 ** 64 - 2 ** 63) for g, w in zip(got, want)]
     assert len(got) == rot_dim // 2 and max(off) <= 1, (max(off), off.index(max(off)))
+
+
+@pytest.mark.parametrize("rot_dim", [258, 2 ** 40, 2 ** 62, -2 ** 62])
+def test_sizes_beyond_a_head_are_refused(rot_dim):
+    with pytest.raises(emb.EmbError) as e:
+        emb.emb_rotary_turns(rot_dim)
+    assert e.value.status == emb.EMB_EINVAL
