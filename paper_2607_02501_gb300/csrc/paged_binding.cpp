@@ -22,7 +22,7 @@ decltype(&emb_paged_attention) f_attention;
 decltype(&emb_paged8_store) f_store8;
 decltype(&emb_paged8_read) f_read8;
 decltype(&emb_paged8_attention) f_attention8;
-PyObject *s_data_ptr, *s_shape, *s_stride, *s_nbytes, *s_itemsize, *s_is_contiguous;
+PyObject *s_data_ptr, *s_shape, *s_stride, *s_nbytes, *s_itemsize, *s_is_contiguous, *s_is_cuda;
 
 // An attribute, or a method without arguments, of a tensor: found in its type once, for the type that came first (torch.Tensor), and
 // then without a lookup by name. Objects of other types are asked by name.
@@ -52,7 +52,7 @@ struct Ask {
     }
 };
 Ask ask_data_ptr(&s_data_ptr, true), ask_stride(&s_stride, true), ask_is_contiguous(&s_is_contiguous, true);
-Ask ask_shape(&s_shape, false), ask_nbytes(&s_nbytes, false), ask_itemsize(&s_itemsize, false);
+Ask ask_shape(&s_shape, false), ask_nbytes(&s_nbytes, false), ask_itemsize(&s_itemsize, false), ask_is_cuda(&s_is_cuda, false);
 
 // Reads arguments one after another; `ok` turns false, with a Python exception set, at the first that cannot be read.
 struct Reader {
@@ -134,6 +134,11 @@ struct Reader {
         if (each != size) refuse("%s: elements of %lld bytes, %lld expected", name, static_cast<long long>(each), static_cast<long long>(size));
         else if (bytes / size < count) refuse("%s has %lld elements, %lld needed", name, static_cast<long long>(bytes / size), static_cast<long long>(count));
         contiguous(o, name);
+    }
+    // The tensor is on the device, as `like` is: its maker leaves it in host memory, or another call wants it there.
+    void on_device(PyObject* o, const char* name, PyObject* like) {
+        if (!ok || o == Py_None || PyLong_Check(o)) return;
+        if (attribute(like, ask_is_cuda) != 0 && ok && attribute(o, ask_is_cuda) == 0) refuse("%s is in host memory", name);
     }
     // Positions of T tokens, [tokens] or [axes][tokens]: their axes and the elements between those. False: an exception is set.
     bool positions(PyObject* o, int64_t T, int64_t& axes, int64_t& pos_stride) {
@@ -338,6 +343,8 @@ PyObject* store8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     r.holds(a[11], "q_gamma", d, 4);
     r.holds(a[12], "k_gamma", d, 4);
     r.holds(a[13], "axis_of_pair", pairs, 1);
+    r.on_device(a[10], "turns", a[0]);
+    r.on_device(a[13], "axis_of_pair", a[0]);
     const float eps = float(r.real(a[14])), factor = float(r.real(a[16]));
     const int64_t neighbours = r.integer(a[15]);
     void* stream = r.address(a[17]);
@@ -431,5 +438,6 @@ PyMODINIT_FUNC PyInit__paged_binding(void) {
     s_nbytes = PyUnicode_InternFromString("nbytes");
     s_itemsize = PyUnicode_InternFromString("itemsize");
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    s_is_cuda = PyUnicode_InternFromString("is_cuda");
     return PyModule_Create(&module);
 }
