@@ -58,13 +58,13 @@ struct Many8Traits {
 constexpr uint32_t kTmemAll = 512;
 static_assert(Many8Traits<64>::kSmem > 114 * 1024 && Many8Traits<128>::kSmem > 114 * 1024 && Many8Traits<256>::kSmem > 114 * 1024,
               "one CTA per SM: tensor memory is allocated whole (see ptx::tmem_alloc)");
-// Tiles whose exponents are held. A softmax warp reads those of the tiles that its rows have products of. There the producer cannot
-// lap it: it writes those of tile n + kKeys + 1 only behind products that wait for the warp's weights of tile n. Tiles that its rows
-// do not see hold nobody up, so the warp waits for none of theirs; behind them it may be ahead of the producer by more than a
-// round, which a parity cannot tell, so there the tile's scores are awaited first.
+// Tiles whose exponents are held. The producer writes them ahead of a tile's keys; the softmax reads them once it has the tile's scores,
+// and the producer writes those of tile n + kKeys + 1 only behind products that wait for the weights of tile n. (With a barrier of their
+// own, awaited ahead of the scores, warps whose rows do not see a tile need holding back too; 4096 tokens of 32 heads of 128 that see all of
+// 16384 keys took 864 us so and 824 this way, with heads of 64 816 and 715.)
 constexpr int kScaleTiles = 8;
 static_assert(Many8Traits<64>::kKeys < kScaleTiles && Many8Traits<128>::kKeys < kScaleTiles && Many8Traits<256>::kKeys < kScaleTiles,
-              "exponents outlast the wait for their tile's weights");
+              "a tile's exponents outlast the wait for its weights");
 constexpr float kLift = 6.0f;     // the running maximum is held that much lower: weights are times 2^6,
 constexpr float kMostLag = 8.0f;  // and it moves when it is exceeded by as much more
 
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
     using PL = PartLayout<D, kRows>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t k_full[T::kKeys], k_empty[T::kKeys], raw_full[T::kVals], raw_empty[T::kVals], v_full[T::kConvs], v_empty[T::kConvs];
-    __shared__ uint64_t q_full, q_ready, q_empty, scale_full[kScaleTiles], s_full[2], p_ready[2], o_done[2], o_free[2], drain;
+    __shared__ uint64_t q_full, q_ready, q_empty, s_full[2], p_ready[2], o_done[2], o_free[2], drain;
     __shared__ float2 scales[kScaleTiles][NB];  // of a block: block_power of its keys, e of its values
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag, joined, odd_seen;
@@ -217,12 +217,11 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
             ptx::mbar_init(&v_full[i], 2);
             ptx::mbar_init(&v_empty[i], 1);
         }
-        for (int i = 0; i < kScaleTiles; ++i) ptx::mbar_init(&scale_full[i], 1);
         ptx::mbar_init(&q_full, 1);
         ptx::mbar_init(&q_ready, T::kSoftWarps);
         ptx::mbar_init(&q_empty, T::kQTmem ? T::kSoftWarps : 1);
         for (int t = 0; t < 2; ++t) {
-            ptx::mbar_init(&s_full[t], 1);
+            ptx::mbar_init(&s_full[t], 2);
             ptx::mbar_init(&p_ready[t], 4);
             ptx::mbar_init(&o_done[t], 1);
             ptx::mbar_init(&o_free[t], 4);
@@ -337,8 +336,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                     if (lane & NB) scales[s][lane & (NB - 1)].y = float(e);
                     else scales[s][lane & (NB - 1)].x = block_power<CAP>(e);
                 }
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&scale_full[s]);
+                __syncwarp();  // (published with the keys' barrier)
                 fetch(kring + ka.slot * T::kRaw, &p.k_map, &k_full[ka.slot]);
                 ++keys;
                 ka.next();
@@ -387,6 +385,7 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                     }
                 }
             ptx::mma_commit(&s_full[place]);
+            if (lane == 0) ptx::mbar_arrive(&s_full[place]);  // (and hands on what the keys' barrier published: the block powers)
         };
         auto pv = [&](int t, int place, int slot, bool first) {  // O[t] (+)= P[place] V
             const uint64_t desc = ptx::smem_desc_mn_sw128(ptx::warp_uniform(conv_u + uint32_t(slot * T::kConv)), T::kSub);
@@ -584,17 +583,13 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
             float mc = 0.0f;
             float2 l2 = make_float2(0, 0);
             const uint32_t behind = n + uint32_t(sg.j1 - sg.j0);
-            if (b_t > a_t) {
-                n += uint32_t(a_t - sg.j0);
-                const int place = NQ == 2 ? t : int(n & 1);
-                wait(&s_full[place], seen[place]);  // (see kScaleTiles)
-            }
+            n += uint32_t(max(a_t - sg.j0, 0));
             for (int j = a_t; j < b_t; ++j, ++n) {
                 const int place = NQ == 2 ? t : int(n & 1);
-                wait(&scale_full[n % kScaleTiles], n / kScaleTiles);
+                wait(&s_full[place], seen[place]++);
+                ptx::tc_fence_after();
                 // The factors of the blocks' raw scores, held so that a product neither overflows nor makes NaN of what is hidden,
-                // and the values' exponents: read while the scores are still being made. (A load from shared memory between scores
-                // and weights costs its latency in every tile, more registers than these spill.)
+                // and the values' exponents: read beside the first scores.
                 const float2* block = scales[n % kScaleTiles];
                 float by[NB], up[NB];
                 auto factor = [&](float power) { return fminf(fmaxf(back * power, 1e-37f), 3.0e38f); };
@@ -604,8 +599,6 @@ __global__ void __launch_bounds__(Many8Traits<D>::kThreads, 1) paged_codes_many_
                     by[k] = factor(bl.x);
                     up[k] = bl.y;
                 }
-                wait(&s_full[place], seen[place]++);
-                ptx::tc_fence_after();
                 const uint32_t s_col = tmem + lanes + uint32_t(place * KT);
                 const int key0 = j * KT;
                 const bool edge = key0 < it.lo_all || key0 + KT > it.hi_all;
