@@ -14,7 +14,7 @@
 // - Softmax with the values' powers: with z the score in base 2 and e the exponent of its key's values, the running maximum m is that
 //   of z + e, the weight w = 2^(z + e - m) <= 1 multiplies the bare codes, and the sum of weights adds w 2^-e. So w is in f16's
 //   range whatever the blocks' powers are: times 2^14, those above 2^-28 of the largest are rounded to 11 bits.
-// HBM bounds long histories: those 64 requests' 1.09 GB take 202 to 211 us now, 0.77 to 0.80 of the measured copy rate, and 181 if nothing
+// HBM bounds long histories: those 64 requests' 1.09 GB take 199 to 211 us now, 0.77 to 0.81 of the measured copy rate, and 181 if nothing
 // is computed. Latency and the joins bound small calls: one token over 867 keys 6.2 us.
 #include <algorithm>
 #include <cmath>
@@ -694,8 +694,8 @@ int few8_blocks(const PagedAttnArgs& a) {
 }
 // CTAs of the cluster that takes a block, or 0 where equal stretches of all the work are sooner done: the rule of the bf16
 // cache's kernel (paged_attention.cu, where its measurements stand), in keys: tiles here have twice as many, so its limits are halved.
-// With it, where more than 16 rows have clusters (us, and the tcgen05 kernel): 24 requests of 4 queries of 16 heads on 2 over 1500 keys 11.5 and 19.3
-// (heads of 64), 15.8 and 21.8 (128), one of 8 queries over 4000 keys 8.8 and 16.8, 11.4 and 16.9, 14.7 and 25.2 (256).
+// With it, where more than 16 rows have clusters (us, and the tcgen05 kernel): 24 requests of 4 queries of 16 heads on 2 over 1500 keys 11.4 and 19.0
+// (heads of 64), 15.6 and 21.5 (128), one of 8 queries over 4000 keys 8.9 and 14.9, 11.5 and 16.9, 14.8 and 23.2 (256).
 int few8_cluster(const PagedAttnArgs& a) {
     double keys = double(a.max_pages * a.page_size);
     if (a.window > 0) keys = std::min(keys, double(a.window) + kFewRows + kFewTile);
@@ -747,10 +747,10 @@ cudaError_t launch_paged8_attention(const Paged8AttnArgs& args, cudaStream_t s) 
     p.v_exp = args.v_exp;
     // Rows of a request: up to 16 go to the mma.sync kernel, and more where all its blocks of 16 have a cluster at once. Up to 32 do
     // too, though their keys come twice: the second time from L2, and every CTA of two takes a stretch of its own (us, mma.sync and
-    // tcgen05: 32 requests of 4 queries of 16 heads on 2 of 128 over 8000 keys 62 and 66, one over 16000 19 and 25, of 64 15 and 23); but
+    // tcgen05: 32 requests of 4 queries of 16 heads on 2 of 128 over 8000 keys 62 and 67, one over 16000 18 and 25, of 64 15 and 23); but
     // heads of 256, and up to 64 rows, only where the call has few blocks to share out (one request of 8 queries of 16 heads
-    // on 2 over 16000 keys, heads of 64, 128 and 256: 17 and 23, 23 and 25, 27 and 42; 4 requests 23 and 26, 33 and 28, 75 and 54; 24
-    // requests of 4 queries of heads of 256 over 1500 keys 40 and 32). The rest goes to the tcgen05 kernel.
+    // on 2 over 16000 keys, heads of 64, 128 and 256: 17 and 23, 22 and 25, 27 and 39; 4 requests 22 and 24, 33 and 27, 75 and 46; 24
+    // requests of 4 queries of heads of 256 over 1500 keys 39 and 29). The rest goes to the tcgen05 kernel.
     bool few = false;
     if (p.G <= 16) {
         const int64_t rows = std::min(a.max_q, a.n_tokens) * p.G;

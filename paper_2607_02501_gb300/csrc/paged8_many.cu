@@ -14,9 +14,10 @@
 // - The blocks' powers: a row's scores of a block are multiplied by its key power, the running maximum is that of score plus value
 //   exponent, and the sum of weights takes the value power out again (see paged8_few.cu). Weights are times 2^6, and
 //   the maximum may lag by 2^8: below f16's largest.
-// What bounds it. Heads of 128: 4096 new tokens of 32 heads over 16384 keys take 793 us (1210 TFLOP/s, 0.63 of the measured matrix rate; the
-// bf16 cache's kernel 600 to 640): a tile's chain of scores, softmax and product, of which the blocks' powers lengthen the softmax; without the
-// values' conversion 745. Heads of 256: 816 tokens of two requests 35 us, shared memory's bandwidth (values are read, written and read).
+// What bounds it. Heads of 128: 4096 new tokens of 32 heads over 16384 keys take 761 us (1260 TFLOP/s, 0.66 of the measured matrix rate; the
+// bf16 cache's kernel 600 to 674): a tile's chain of scores, softmax and product, of which the blocks' powers lengthen the softmax, beside some 272 KB
+// that two row tiles move through shared memory a key tile, half of its time. Heads of 256: 816 tokens of two requests 33 us, shared memory's
+// bandwidth (values are read, written and read).
 #include <algorithm>
 #include <cfloat>
 #include <mutex>
