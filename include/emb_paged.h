@@ -192,7 +192,8 @@ EMB_API emb_status emb_rotary_turns(int64_t rot_dim, double base, double stretch
  * n_axes or more count as n_axes - 1; NULL: axis 0 for every pair. The angle is exact modulo a turn for the given turns[i]
  * (those of emb_rotary_turns are within 2^-64 turns a position of the formula's); cosine and sine are within 1e-6.
  * 1 <= n_tokens < 2^31; head_dim 64, 128 or 256, page_size 16, 32, 64, 128 or 256 (else EMB_EUNSUPPORTED); rot_dim % 8 == 0,
- * 0..head_dim; n_heads, n_kv_heads 1..4096; eps >= 0 and factor finite. Device pointers 16-byte aligned, but positions (4), slots and
+ * 0..head_dim; n_heads, n_kv_heads 1..4096, n_tokens * (n_heads + n_kv_heads) < 2^33 (else EMB_EUNSUPPORTED); eps >= 0 and factor
+ * finite. Device pointers 16-byte aligned, but positions (4), slots and
  * turns (8), exponents and axis_of_pair (1). No output may overlap another buffer. Errors: EMB_EINVAL, EMB_EALIGN, EMB_EUNSUPPORTED,
  * EMB_ECUDA. */
 EMB_API emb_status emb_paged8_store(const uint16_t* q, int64_t q_stride, const uint16_t* k, int64_t k_stride,
@@ -206,7 +207,7 @@ EMB_API emb_status emb_paged8_store(const uint16_t* q, int64_t q_stride, const u
 /* Section 3.1 ("prefix once, head many": what the cache holds, for other uses).
  * Rows of the cache as bf16 (exact): row i of k_out and v_out, [n_rows][n_kv_heads][head_dim], is what slot slots[i] holds;
  * zeros where that is negative or beyond the cache. Slots may repeat.
- * 0 <= n_rows < 2^31; sizes as for emb_paged8_store; codes and outputs 16-byte aligned, slots 8. No output may overlap another
+ * 0 <= n_rows < 2^31, n_rows * n_kv_heads * head_dim < 2^42 (else EMB_EUNSUPPORTED); sizes as for emb_paged8_store; codes and outputs 16-byte aligned, slots 8. No output may overlap another
  * buffer. Errors: EMB_EINVAL, EMB_EALIGN, EMB_EUNSUPPORTED, EMB_ECUDA. */
 EMB_API emb_status emb_paged8_read(const uint8_t* k_codes, const uint8_t* v_codes, const uint8_t* k_exp, const uint8_t* v_exp,
                                    int64_t n_pages, int64_t page_size, int64_t n_kv_heads, int64_t head_dim,
