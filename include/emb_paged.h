@@ -207,8 +207,8 @@ EMB_API emb_status emb_paged8_store(const uint16_t* q, int64_t q_stride, const u
 /* Section 3.1 ("prefix once, head many": what the cache holds, for other uses).
  * Rows of the cache as bf16 (exact): row i of k_out and v_out, [n_rows][n_kv_heads][head_dim], is what slot slots[i] holds;
  * zeros where that is negative or beyond the cache. Slots may repeat.
- * 0 <= n_rows < 2^31, n_rows * n_kv_heads * head_dim < 2^42 (else EMB_EUNSUPPORTED); sizes as for emb_paged8_store; codes and outputs 16-byte aligned, slots 8. No output may overlap another
- * buffer. Errors: EMB_EINVAL, EMB_EALIGN, EMB_EUNSUPPORTED, EMB_ECUDA. */
+ * 0 <= n_rows < 2^31, n_rows * n_kv_heads * head_dim < 2^42 (else EMB_EUNSUPPORTED); sizes as for emb_paged8_store; codes and
+ * outputs 16-byte aligned, slots 8. No output may overlap another buffer. Errors: EMB_EINVAL, EMB_EALIGN, EMB_EUNSUPPORTED, EMB_ECUDA. */
 EMB_API emb_status emb_paged8_read(const uint8_t* k_codes, const uint8_t* v_codes, const uint8_t* k_exp, const uint8_t* v_exp,
                                    int64_t n_pages, int64_t page_size, int64_t n_kv_heads, int64_t head_dim,
                                    const int64_t* slots, int64_t n_rows, uint16_t* k_out, uint16_t* v_out,
